@@ -80,8 +80,10 @@ typedef enum {
     ISO_ERR_UNSUPPORTED = -8,  /* valid request outside this build: K > ISO_MAX_EXPERTS,
                                   a tensor with 2^32 or more entries, GLOBAL scope larger
                                   than the workspace allows */
-    ISO_ERR_TIMEOUT = -9       /* (device) a kernel's wait for its own bulk copies gave up
+    ISO_ERR_TIMEOUT = -9,      /* (device) a kernel's wait for its own bulk copies gave up
                                   after its iteration limit; the outputs are unspecified */
+    ISO_ERR_INDEX = -10        /* (device) a token id outside the embedding table that is not
+                                  the padding id; that token counts as padding */
 } iso_status;
 
 #define ISO_MAX_EXPERTS 8
@@ -430,6 +432,109 @@ int32_t iso_opt_step(double* U, double* V, const double* S0, const iso_tensor* G
  * 4; pointers 16-byte aligned.  Device pointers; enqueued on stream. */
 int32_t iso_gemm_tf32(const float* A, int64_t lda, const float* B, int64_t ldb, float* C, int64_t ldc, int64_t M,
                       int64_t N, int64_t Kc, int64_t a_k0, int64_t b_k0, void* stream);
+
+/* ---- Training step: 8-bit activation checkpoints --------------------------
+ *
+ * What a training step of the parameter lists above needs between the tokens
+ * and the gradients that iso_opt_step takes: a layer's input kept in 8 bits
+ * from the forward to the backward pass, the weight gradient and the SwiGLU
+ * gradients taken from it, and the token embedding with its gradient.  The
+ * paper has no counterpart (its trainer is a library's); the calls are an
+ * interface of this library.
+ *
+ * Matrices are row-major with a row stride (rows are tokens unless said
+ * otherwise).  Any element-aligned address and stride is accepted; rows that
+ * start on 16-byte boundaries (address and row stride multiples of 16 bytes)
+ * take vector loads and stores.  rows and cols are below 2^31.  Two matrices
+ * "overlap" when they share a byte: the halves of one wider buffer (same row
+ * stride, disjoint column ranges) do not.  An empty matrix may have data =
+ * NULL. */
+typedef struct {
+    void*   data;
+    int64_t rows, cols;
+    int64_t ld;        /* elements from one row to the next, >= cols */
+    int32_t dtype;     /* iso_dtype */
+    int32_t reserved;  /* must be 0 */
+} iso_mat;
+
+/* A checkpoint of a rows x cols matrix.  Each group of ISO_ACT_GROUP
+ * consecutive channels of a row holds 8-bit codes q in [-127, 127] and one
+ * exponent byte b; a value stands for q 2^(b - 127), which bfloat16 holds
+ * exactly.  With A the group's largest magnitude, b - 127 is the least integer
+ * >= -126 with A <= 127 2^(b - 127), and q the nearest integer to
+ * x / 2^(b - 127), halves to even (with b = 249, of magnitude 63 at most, so
+ * that no finite x stands for an infinity).  A group with a NaN or an infinity has
+ * b = 255, q = 0 and stands for NaN throughout.  Codes of channels past cols
+ * (up to a multiple of the group) are 0, exponent bytes past the last group
+ * (up to a multiple of 8) are 1.  Rows of a checkpoint are independent, so a
+ * range of rows is a checkpoint too. */
+#define ISO_ACT_GROUP 32
+typedef struct {
+    void*   codes;     /* int8, 16-byte aligned */
+    void*   exps;      /* uint8, 8-byte aligned */
+    int64_t rows, cols;
+    int64_t ld_codes;  /* bytes from row to row: a multiple of 32, >= cols rounded up to one */
+    int64_t ld_exps;   /* bytes from row to row: a multiple of 8, >= ceil(cols / 32) rounded up to one */
+} iso_act;
+
+/* pack <- x (forward pass). */
+int32_t iso_act_pack(const iso_mat* x, const iso_act* pack, void* stream);
+
+/* out <- the values pack stands for (BF16 or F32, both exact). */
+int32_t iso_act_unpack(const iso_act* pack, const iso_mat* out, void* stream);
+
+/* The weight gradient of y = x W^T (W: out_features x in_features) from the
+ * gradient of y and the checkpoint of x, over their rows (tokens):
+ *   out = dY^T X_hat            (accumulate = 0)
+ *   out = out + dY^T X_hat      (accumulate = 1)
+ * dY tokens x out_features, pack tokens x in_features, out out_features x
+ * in_features (BF16 or F32, rounded once).  No tokens: out = 0, or unchanged
+ * when accumulating.  out may overlap neither input.  The products are exact
+ * and sums are binary32.  The workspace is scratch of the size
+ * iso_act_wgrad_workspace_size returns for the same arguments, 256-byte
+ * aligned.  status (device, may be NULL): ISO_OK or ISO_ERR_TIMEOUT. */
+int32_t iso_act_wgrad_workspace_size(const iso_mat* dY, const iso_act* pack, const iso_mat* out, size_t* bytes);
+int32_t iso_act_wgrad(const iso_mat* dY, const iso_act* pack, const iso_mat* out, int32_t accumulate,
+                      void* workspace, size_t ws_bytes, int32_t* status, void* stream);
+
+/* h = silu(gate) * up in binary32 from the inputs themselves, rounded once,
+ * with both inputs kept as checkpoints, in one pass.  gate, up and h share
+ * shape and dtype; h overlaps neither input. */
+int32_t iso_swiglu_pack(const iso_mat* gate, const iso_mat* up, const iso_mat* h, const iso_act* gate_pack,
+                        const iso_act* up_pack, void* stream);
+
+/* The gradients of h = silu(g) u from the checkpoints g, u, and h again from
+ * them (for the weight gradient of the layer that read h), in one pass: with
+ * s = 1 / (1 + exp(-g)),
+ *   d_gate = dh u s (1 + g (1 - s)),   d_up = dh g s,   h = g s u.
+ * dh and the outputs share shape and dtype; h may be NULL (not computed); no
+ * output overlaps dh or another output. */
+int32_t iso_swiglu_grad(const iso_mat* dh, const iso_act* gate_pack, const iso_act* up_pack, const iso_mat* d_gate,
+                        const iso_mat* d_up, const iso_mat* h, void* stream);
+
+/* ---- Training step: token embedding --------------------------------------
+ *
+ * ids holds n token ids (int32, or int64 with ids_i64 = 1), aligned to their
+ * size.  An id equal to pad_id (-1: no padding id; an id of -1 is padding
+ * then) gives a zero row and no gradient; so does any other id outside
+ * [0, table rows), which is also reported as ISO_ERR_INDEX through status
+ * (device, one value, may be NULL; written ISO_OK otherwise). */
+
+/* out[t] = scale * table[ids[t]], in binary32, rounded once; out n x table
+ * cols, BF16 or F32. */
+int32_t iso_embed(const iso_mat* table, const void* ids, int32_t ids_i64, int64_t n, int64_t pad_id, float scale,
+                  const iso_mat* out, int32_t* status, void* stream);
+
+/* grad[v] = scale * (sum of dY[t] over the tokens t with ids[t] = v), zero for
+ * rows without tokens; with accumulate = 1 that sum is added to grad, rows
+ * without tokens unchanged.  dY n x cols; grad table rows x cols, BF16 or
+ * F32.  Tokens are sorted by id and each row's sum is binary32 in an order
+ * that depends on the ids alone, so equal inputs give equal bits; one rounding
+ * to grad's type.  n < 2^31.  grad overlaps neither dY nor ids. */
+int32_t iso_embed_grad_workspace_size(int64_t n, int64_t cols, size_t* bytes);
+int32_t iso_embed_grad(const iso_mat* dY, const void* ids, int32_t ids_i64, int64_t pad_id, float scale,
+                       const iso_mat* grad, int32_t accumulate, void* workspace, size_t ws_bytes, int32_t* status,
+                       void* stream);
 
 /* Static description of a status code. */
 const char* iso_error_string(int32_t status);

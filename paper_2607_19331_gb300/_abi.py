@@ -22,6 +22,7 @@ ISO_ERR_CUDA = -6
 ISO_ERR_NONFINITE = -7
 ISO_ERR_UNSUPPORTED = -8
 ISO_ERR_TIMEOUT = -9
+ISO_ERR_INDEX = -10
 ISO_MAX_EXPERTS = 8
 ISO_NOALLOC_SCRATCH_BYTES = 32 << 20
 
@@ -69,9 +70,22 @@ class IsoAdamwCfg(ctypes.Structure):
                 ("ns_iters", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class IsoMat(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("ld", ctypes.c_int64), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class IsoAct(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("exps", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("ld_codes", ctypes.c_int64), ("ld_exps", ctypes.c_int64)]
+
+
+ISO_ACT_GROUP = 32
+
 # (name, restype, argtypes) for every entry point of include/iso.h
 P = ctypes.c_void_p
 PT = ctypes.POINTER(IsoTensor)
+PM, PA = ctypes.POINTER(IsoMat), ctypes.POINTER(IsoAct)
 I32, I64, SZ = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
 PROTOTYPES = [
     ("iso_num_units", I32, [PT, I32, ctypes.POINTER(IsoTopkCfg), ctypes.POINTER(I64)]),
@@ -100,6 +114,15 @@ PROTOTYPES = [
     ("iso_opt_workspace_size", I32, [I64, I64, ctypes.POINTER(SZ)]),
     ("iso_opt_step", I32, [P, P, P, PT, P, P, P, P, PT, PT, I64, I64, ctypes.POINTER(IsoAdamwCfg), P, SZ,
                            ctypes.POINTER(IsoMergeStats), P]),
+    ("iso_act_pack", I32, [PM, PA, P]),
+    ("iso_act_unpack", I32, [PA, PM, P]),
+    ("iso_act_wgrad_workspace_size", I32, [PM, PA, PM, ctypes.POINTER(SZ)]),
+    ("iso_act_wgrad", I32, [PM, PA, PM, I32, P, SZ, P, P]),
+    ("iso_swiglu_pack", I32, [PM, PM, PM, PA, PA, P]),
+    ("iso_swiglu_grad", I32, [PM, PA, PA, PM, PM, PM, P]),
+    ("iso_embed", I32, [PM, P, I32, I64, I64, ctypes.c_float, PM, P, P]),
+    ("iso_embed_grad_workspace_size", I32, [I64, I64, ctypes.POINTER(SZ)]),
+    ("iso_embed_grad", I32, [PM, P, I32, I64, ctypes.c_float, PM, I32, P, SZ, P, P]),
     ("iso_error_string", ctypes.c_char_p, [I32]),
     ("iso_launch_count", ctypes.c_uint64, []),
     ("iso_force_two_pass", ctypes.c_int32, [ctypes.c_int32]),

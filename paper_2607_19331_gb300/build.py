@@ -16,8 +16,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(BUILD, "libiso_gb300.so")
 SOURCES = ["iso_api.cu", "iso_select.cu", "iso_apply.cu", "iso_merge.cu", "iso_block.cu", "iso_fused.cu",
-           "iso_gemm.cu", "iso_frame.cu", "iso_range.cu"]
-HEADERS = ["iso_internal.cuh", "iso_kernels.cuh", "iso_gemm.cuh"]
+           "iso_gemm.cu", "iso_frame.cu", "iso_range.cu", "iso_act.cu", "iso_wgrad.cu", "iso_embed.cu"]
+HEADERS = ["iso_internal.cuh", "iso_kernels.cuh", "iso_gemm.cuh", "iso_train.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-static-global-template-stub=false", "-Xcompiler", "-fPIC,-ffp-contract=off",
          "--expt-relaxed-constexpr", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
