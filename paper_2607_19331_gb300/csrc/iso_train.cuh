@@ -27,7 +27,7 @@ inline int64_t act_exps_padded(int64_t cols) {
 }
 
 constexpr int64_t EXTENT_LIMIT = 0x7FFFFFFFLL;
-constexpr int64_t STRIDE_LIMIT = 1LL << 40;
+constexpr int64_t STRIDE_LIMIT = 1LL << 36;
 
 inline int check_mat(const iso_mat* m) {
     if (!m || m->reserved != 0) return ISO_ERR_ARG;
