@@ -12,10 +12,22 @@
 //              significant bits each, hi + mid + lo = dY, and G is the sum of
 //              the three products; so every product is exact and sums are
 //              binary32.
-//   k_wgrad    a pair of CTAs per 256 x 256 tile of G, 64 tokens per stage
-//              (16 KB of each operand per CTA, six stages), accumulated in
-//              tensor memory, two accumulators so that one tile's epilogue
-//              overlaps the next tile's products; persistent over the tiles.
+//   k_wgrad    a pair of CTAs per 256 x 256 tile of G, 128 tokens per stage
+//              (32 KB of each operand per CTA, three stages; six stages of 64
+//              tokens have the same bytes in flight and measured 4 % slower,
+//              the waits and commits of a stage costing the same), persistent
+//              over the tiles.  The tensor cores' accumulation cuts low bits
+//              off at every product: the relative error of a binary32 G grows
+//              in proportion to the chain of products (1.1e-6, 4.4e-7 and 2.0e-7 at chains of 4096, 2048 and 1024
+//              tokens of 8192 random ones; a plain binary32 product has
+//              3.1e-7).  So a chain is 1024 tokens; the epilogue warps add the
+//              chains up in registers, 128 sums a thread, rounding to nearest,
+//              while the next chain runs in the other of two accumulators in
+//              tensor memory (chains of 2048 measured 1 % faster).
+//   measured   18944 x 3584 over 8192 tokens (1.11 PFLOP): 579 us alone, 1922
+//              TFLOP/s, with 16 us before it for the decoding; a bf16 library
+//              product of the same operands 559 - 580 us.  The products
+//              themselves bound it, then the copies (about 470 us alone).
 //   split      a G of few tiles under many tokens is cut along the tokens as
 //              well; the parts are binary32 in the workspace and k_wgrad_join
 //              adds them in order.
@@ -29,24 +41,27 @@ namespace {
 
 constexpr int WG_BM = 256;                 // rows of G (dY channels) per CTA pair
 constexpr int WG_BN = 256;                 // columns of G (X channels) per CTA pair
-constexpr int WG_BK = 64;                  // tokens per stage
-constexpr int WG_STAGES = 6;
+constexpr int WG_BK = 128;                 // tokens per stage
+constexpr int WG_STAGES = 3;
 constexpr int WG_BOX = 64;                 // channels of one copy: 128 bytes, the swizzle's row
 constexpr int WG_BOX_BYTES = WG_BOX * WG_BK * 2;
 constexpr int WG_OP_BYTES = 2 * WG_BOX_BYTES;          // 128 channels of an operand: this CTA's half
 constexpr int WG_STAGE_BYTES = 2 * WG_OP_BYTES;
-constexpr int WG_SMEM = 1024 + WG_STAGES * WG_STAGE_BYTES + 256;
 constexpr int WG_EPI_WARPS = 8;
+constexpr int WG_OUT_BYTES = 32 * 32 * 4;  // an epilogue warp's 32 x 32 block on its way out
+constexpr int WG_SMEM = 1024 + WG_STAGES * WG_STAGE_BYTES + WG_EPI_WARPS * WG_OUT_BYTES + 256;
+static_assert(WG_SMEM <= 232448, "shared memory of one CTA");
 constexpr int WG_THREADS = (WG_EPI_WARPS + 2) * 32;    // epilogue warps, a copy warp, a product warp
 constexpr int WG_MAX_PARTS = 3;
 constexpr int WG_MAX_SPLIT = 8;
+constexpr int WG_CHAIN = 8;                // steps accumulated in tensor memory before they are added in registers
 constexpr int WG_BAND = 8;                 // tile rows that are walked together
 
 struct WgradArgs {
     int32_t M, N;
     int32_t m_tiles, n_tiles;
-    int32_t k_tiles;       // steps of the whole contraction: parts x ceil(tokens / 64)
-    int32_t parts;
+    int32_t t_tiles;       // steps over the tokens: ceil(tokens / 128)
+    int32_t k_tiles;       // steps of the whole contraction: parts x t_tiles, part after part
     int32_t split;
     int32_t accumulate;
     void* out;             // split = 1: G
@@ -64,15 +79,11 @@ struct WgradMaps {
 // Shared-memory descriptor of an MN-major operand in the 128-byte swizzle:
 // 64 channels (128 bytes) by eight tokens make an atom of 1024 bytes; the next
 // eight tokens follow it, the next 64 channels are one copy box further on.
-__device__ __forceinline__ uint64_t mn_desc(uint32_t saddr) {
-    uint64_t d = 0;
-    d |= (uint64_t)((saddr >> 4) & 0x3FFFu);
-    d |= (uint64_t)((WG_BOX_BYTES >> 4) & 0x3FFF) << 16;    // leading offset: 64 channels on
-    d |= (uint64_t)((1024u >> 4) & 0x3FFFu) << 32;          // stride offset: eight tokens on
-    d |= (uint64_t)1u << 46;
-    d |= (uint64_t)2u << 61;
-    return d;
-}
+// The start address (in 16-byte words) is the low word's low half, so an
+// operand further on in shared memory is an addition to the low word.
+constexpr uint32_t WG_DESC_LO = (uint32_t)(WG_BOX_BYTES >> 4) << 16;                    // leading offset: 64 channels on
+constexpr uint32_t WG_DESC_HI = (1024u >> 4) | 1u << 14 | 2u << 29;                     // stride offset: eight tokens on
+__device__ __forceinline__ uint32_t mn_desc_lo(uint32_t saddr) { return WG_DESC_LO + (saddr >> 4); }
 
 // kind::f16, fp32 accumulator, bf16 A and B, both MN-major, M = 256 over the
 // pair, N = 256
@@ -99,10 +110,11 @@ __device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* m
                  " [%0], [%1, {%2, %3}], [%4];"
                  :: "r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void umma_bf16_pair(uint32_t tmem_d, uint64_t a, uint64_t b, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 :: "r"(tmem_d), "l"(a), "l"(b), "r"(WG_IDESC), "r"(accumulate) : "memory");
+__device__ __forceinline__ void umma_bf16_pair(uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+                 "mov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
+                 "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %4, p;\n\t}"
+                 :: "r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(WG_DESC_HI), "r"(WG_IDESC), "r"(accumulate) : "memory");
 }
 // arrive on this barrier in both CTAs once the products issued so far are done
 __device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
@@ -114,9 +126,9 @@ __device__ __forceinline__ void arrive_cluster(uint32_t cluster_bar) {
 }
 __device__ __forceinline__ bool try_wait_cluster(uint32_t bar, uint32_t parity) {
     uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
                  "selp.u32 %0, 1, 0, p;\n\t}"
-                 : "=r"(ok) : "r"(bar), "r"(parity), "n"(MBAR_PROBE_NS) : "memory");
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
 // bounded wait; false once the limit is reached or another thread of the CTA gave up
@@ -128,45 +140,74 @@ __device__ __forceinline__ bool wait_pair(uint32_t bar, uint32_t parity, volatil
     *abort_flag = 1;
     return false;
 }
-__device__ __forceinline__ void tmem_load32(uint32_t taddr, float (&v)[32]) {
-    uint32_t r[32];
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+// 16 consecutive columns of this thread's accumulator row
+__device__ __forceinline__ void tmem_load16(uint32_t taddr, float (&v)[16]) {
+    uint32_t r[16];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
                    "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-                   "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
-                   "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-                   "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                   "=r"(r[14]), "=r"(r[15])
                  : "r"(taddr));
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+    for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(r[j]);
 }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-// 32 columns of one row of G from column n
+// A warp's 32 x 32 block of G: lane l holds row l.  Through shared memory
+// (16-byte words swizzled by row), so that a store covers whole runs of a row:
+// one row by 16-byte words of eight (f32) or four (bf16) lanes where G's rows
+// start on 16-byte boundaries, else a row's 32 columns by the 32 lanes.
 template <typename O>
-__device__ __forceinline__ void store_row32(O* row, int n, int N, float (&v)[32], bool vec, int accumulate) {
+__device__ __forceinline__ void store_block(float4* buf, const float (&v)[32], int lane, O* out, long long ldo, int m,
+                                            int n, int M, int N, bool vec, int accumulate) {
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        buf[lane * 8 + (j ^ (lane & 7))] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+    __syncwarp();
+    const int rows = min(32, M - m);
     if (vec && n + 32 <= N) {
-#pragma unroll
-        for (int j = 0; j < 32; j += 8) {
-            float w[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) w[k] = v[j + k];
-            if (accumulate) {
-                float old[8];
-                load8<true>(row, n + j, N, old);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) w[k] += old[k];
+        if constexpr (sizeof(O) == 4) {
+#pragma unroll 2
+            for (int i = 0; i < 8; ++i) {
+                const int r = i * 4 + (lane >> 3), w = lane & 7;
+                if (r >= rows) continue;
+                float4 x = buf[r * 8 + (w ^ (r & 7))];
+                float4* o = reinterpret_cast<float4*>(out + (long long)(m + r) * ldo + n) + w;
+                if (accumulate) {
+                    const float4 old = *o;
+                    x.x += old.x; x.y += old.y; x.z += old.z; x.w += old.w;
+                }
+                *o = x;
             }
-            store8<true>(row, n + j, N, w);
-        }
-    } else {
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
+                const int r = i * 8 + (lane >> 2), w = (lane & 3) * 2;
+                if (r >= rows) continue;
+                const float4 x = buf[r * 8 + (w ^ (r & 7))], y = buf[r * 8 + ((w + 1) ^ (r & 7))];
+                float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                O* o = out + (long long)(m + r) * ldo;
+                if (accumulate) {
+                    float old[8];
+                    load8<true>(o, n + w * 4, N, old);
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (n + j < N) from_f32(accumulate ? to_f32(row[n + j]) + v[j] : v[j], row[n + j]);
+                    for (int k = 0; k < 8; ++k) f[k] += old[k];
+                }
+                store8<true>(o, n + w * 4, N, f);
+            }
+        }
+    } else if (n + lane < N) {
+        const float* flat = reinterpret_cast<const float*>(buf);
+#pragma unroll 1
+        for (int r = 0; r < rows; ++r) {
+            const float x = flat[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)];
+            O* o = out + (long long)(m + r) * ldo + n + lane;
+            from_f32(accumulate ? to_f32(*o) + x : x, *o);
+        }
     }
 }
 
@@ -189,7 +230,8 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
     extern __shared__ unsigned char wg_smem_raw[];
     unsigned char* const smem =
         reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(wg_smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint64_t* const bars = reinterpret_cast<uint64_t*>(smem + WG_STAGES * WG_STAGE_BYTES);
+    uint64_t* const bars =
+        reinterpret_cast<uint64_t*>(smem + WG_STAGES * WG_STAGE_BYTES + WG_EPI_WARPS * WG_OUT_BYTES);
     uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * WG_STAGES + 4);
     volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -227,82 +269,115 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
 
     if (warp == WG_EPI_WARPS && lane == 0) {
         // copies: this CTA's 128 channels of either operand
-        int it = 0;
+        const uint32_t full0 = in_leader(full(0)), own = rank * 128;
+        uint32_t s = 0, ph = 1, done = 0;            // stage, its parity, copies issued
         bool ok = true;
         for (int i = pair; ok && i < items; i += pairs) {
             int m0, n0, k0, k1, part;
             work_item(g, i, m0, n0, k0, k1, part);
-            m0 += (int)rank * 128;
-            n0 += (int)rank * 128;
-            for (int k = k0; k < k1; ++k, ++it) {
-                const int s = it % WG_STAGES;
-                if (!wait_pair(empty(s), ((uint32_t)(it / WG_STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+            m0 += own;
+            n0 += own;
+            int p = k0 / g.t_tiles, t = (k0 - p * g.t_tiles) * WG_BK;
+            for (int k = k0; k < k1; ++k) {
+                if (!wait_pair(empty(s), ph, abort_flag)) { ok = false; break; }
                 if (rank == 0) mbar_arrive_tx(full(s), 2 * WG_STAGE_BYTES);
-                const int kt = k / g.parts, p = k - kt * g.parts, t = kt * WG_BK;
-                const uint32_t fb = in_leader(full(s)), a = st + s * WG_STAGE_BYTES, b = a + WG_OP_BYTES;
-                tma_load_pair(a, &maps.a[p], m0, t, fb);
-                tma_load_pair(a + WG_BOX_BYTES, &maps.a[p], m0 + WG_BOX, t, fb);
+                const CUtensorMap* am = &maps.a[p];
+                const uint32_t fb = full0 + 8u * s, a = st + s * WG_STAGE_BYTES, b = a + WG_OP_BYTES;
+                tma_load_pair(a, am, m0, t, fb);
+                tma_load_pair(a + WG_BOX_BYTES, am, m0 + WG_BOX, t, fb);
                 tma_load_pair(b, &maps.b, n0, t, fb);
                 tma_load_pair(b + WG_BOX_BYTES, &maps.b, n0 + WG_BOX, t, fb);
+                if ((t += WG_BK) >= g.t_tiles * WG_BK) { t = 0; ++p; }
+                if (++s == WG_STAGES) { s = 0; ph ^= 1u; }
+                ++done;
             }
         }
         // every copy into this CTA has been consumed before it may exit: the
         // products that read a stage free it in both CTAs
-        for (int q = max(0, it - WG_STAGES); q < it; ++q)
+        for (uint32_t q = 0; q < min(done, (uint32_t)WG_STAGES); ++q) {
+            if (s == 0) { s = WG_STAGES; ph ^= 1u; }
+            --s;
             for (int spin = 0; spin < MBAR_SPIN_LIMIT; ++spin)
-                if (try_wait_cluster(empty(q % WG_STAGES), (uint32_t)(q / WG_STAGES) & 1u) || *abort_flag) break;
+                if (try_wait_cluster(empty(s), ph ^ 1u) || *abort_flag) break;
+        }
     } else if (warp == WG_EPI_WARPS + 1 && lane == 0 && rank == 0) {
-        // products of the pair
-        int it = 0, n_acc = 0;
+        // products of the pair, chain by chain
+        const uint32_t a0 = mn_desc_lo(st), b0 = mn_desc_lo(st + WG_OP_BYTES);
+        uint32_t s = 0, ph = 0, acc = 0, acc_ph = 1;
         bool ok = true;
-        for (int i = pair; ok && i < items; i += pairs, ++n_acc) {
+        for (int i = pair; ok && i < items; i += pairs) {
             int m0, n0, k0, k1, part;
             work_item(g, i, m0, n0, k0, k1, part);
-            const int acc = n_acc & 1;
-            if (!wait_pair(acc_empty(acc), ((uint32_t)(n_acc >> 1) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-            tc_after();
-            const uint32_t d = tmem + acc * WG_BN;
-            for (int k = k0; k < k1; ++k, ++it) {
-                const int s = it % WG_STAGES;
-                if (!wait_pair(full(s), (uint32_t)(it / WG_STAGES) & 1u, abort_flag)) { ok = false; break; }
+            for (int kc = k0; ok && kc < k1; kc += WG_CHAIN) {
+                if (!wait_pair(acc_empty(acc), acc_ph, abort_flag)) { ok = false; break; }
                 tc_after();
-                const uint32_t a = st + s * WG_STAGE_BYTES, b = a + WG_OP_BYTES;
+                const uint32_t d = tmem + acc * WG_BN;
+                uint32_t more = 0;
+                for (int k = min(k1 - kc, WG_CHAIN); k > 0; --k) {
+                    if (!wait_pair(full(s), ph, abort_flag)) { ok = false; break; }
+                    tc_after();
+                    const uint32_t a = a0 + s * (WG_STAGE_BYTES >> 4), b = b0 + s * (WG_STAGE_BYTES >> 4);
 #pragma unroll
-                for (int q = 0; q < WG_BK / 16; ++q)   // 16 tokens per product: two atoms of eight
-                    umma_bf16_pair(d, mn_desc(a + 2048u * q), mn_desc(b + 2048u * q), (k > k0 || q > 0) ? 1u : 0u);
-                umma_commit_pair(empty(s));
+                    for (uint32_t q = 0; q < WG_BK / 16; ++q) {   // 16 tokens per product: two atoms of eight
+                        umma_bf16_pair(d, a + (2048u >> 4) * q, b + (2048u >> 4) * q, more);
+                        more = 1;
+                    }
+                    umma_commit_pair(empty(s));
+                    if (++s == WG_STAGES) { s = 0; ph ^= 1u; }
+                }
+                umma_commit_pair(acc_full(acc));
+                acc ^= 1u;
+                if (acc == 0) acc_ph ^= 1u;
             }
-            umma_commit_pair(acc_full(acc));
         }
     } else if (warp < WG_EPI_WARPS) {
         // epilogue: warp w reads tensor-memory lanes 32 (w mod 4) ..., 128 of the 256 columns
         const int quad = warp & 3, half = warp >> 2;
+        float4* const buf = reinterpret_cast<float4*>(smem + WG_STAGES * WG_STAGE_BYTES + warp * WG_OUT_BYTES);
         int n_acc = 0;
-        for (int i = pair; i < items; i += pairs, ++n_acc) {
+        bool ok = true;
+        for (int i = pair; ok && i < items; i += pairs) {
             int m0, n0, k0, k1, part;
             work_item(g, i, m0, n0, k0, k1, part);
-            const int acc = n_acc & 1;
-            if (!wait_pair(acc_full(acc), (uint32_t)(n_acc >> 1) & 1u, abort_flag)) break;
-            __syncwarp();
-            tc_after();
-            const int row = m0 + (int)rank * 128 + quad * 32 + lane;
-#pragma unroll 1
+            float sum[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int j = 0; j < 32; ++j) sum[c][j] = 0.0f;
+            for (int kc = k0; kc < k1; kc += WG_CHAIN, ++n_acc) {
+                const int acc = n_acc & 1;
+                if (!wait_pair(acc_full(acc), (uint32_t)(n_acc >> 1) & 1u, abort_flag)) { ok = false; break; }
+                __syncwarp();
+                tc_after();
+                const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * WG_BN + half * 128);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    float v[16];
+                    tmem_load16(at + c * 16, v);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[c >> 1][(c & 1) * 16 + j] += v[j];
+                }
+                tc_before();
+                __syncwarp();
+                if (lane == 0) arrive_cluster(in_leader(acc_empty(acc)));
+            }
+            if (!ok) break;
+            const int m = m0 + (int)rank * 128 + quad * 32;
+            if (m >= g.M) continue;
+#pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const int n = n0 + half * 128 + c * 32;
-                float v[32];
-                tmem_load32(tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * WG_BN + half * 128 + c * 32), v);
-                if (row < g.M && n < g.N) {
-                    if (g.part)
-                        store_row32(g.part + ((long long)part * g.M + row) * g.ld_part, n, g.N, v, true, 0);
-                    else if (g.out_dtype == ISO_BF16)
-                        store_row32(static_cast<__nv_bfloat16*>(g.out) + row * g.ldo, n, g.N, v, g.out_vec, g.accumulate);
-                    else
-                        store_row32(static_cast<float*>(g.out) + row * g.ldo, n, g.N, v, g.out_vec, g.accumulate);
-                }
+                if (n >= g.N) continue;
+                if (g.part)
+                    store_block(buf, sum[c], lane, g.part + (long long)part * g.M * g.ld_part, g.ld_part, m, n, g.M,
+                                g.N, true, 0);
+                else if (g.out_dtype == ISO_BF16)
+                    store_block(buf, sum[c], lane, static_cast<__nv_bfloat16*>(g.out), g.ldo, m, n, g.M, g.N,
+                                g.out_vec, g.accumulate);
+                else
+                    store_block(buf, sum[c], lane, static_cast<float*>(g.out), g.ldo, m, n, g.M, g.N, g.out_vec,
+                                g.accumulate);
             }
-            tc_before();
-            __syncwarp();
-            if (lane == 0) arrive_cluster(in_leader(acc_empty(acc)));
         }
     }
     __syncwarp();
@@ -457,8 +532,8 @@ WgradPlan plan_wgrad(const iso_mat* dY, const iso_act* pack, const iso_mat* out)
     p.n_tiles = (int)((N + WG_BN - 1) / WG_BN);
     p.k_tiles = (int)((T + WG_BK - 1) / WG_BK) * p.n_parts;
     const long long tiles = (long long)p.m_tiles * p.n_tiles, pairs = std::max(1, train_sms() / 2);
-    // cut the tokens where the tiles leave half the pairs idle, eight steps a part at least
-    p.split = (int)std::max(1LL, std::min({pairs / std::max(1LL, tiles), (long long)p.k_tiles / 8, (long long)WG_MAX_SPLIT}));
+    // cut the tokens where the tiles leave half the pairs idle, four steps a part at least
+    p.split = (int)std::max(1LL, std::min({pairs / std::max(1LL, tiles), (long long)p.k_tiles / 4, (long long)WG_MAX_SPLIT}));
     p.ldx = (N + 7) / 8 * 8;
     p.ldd = (M + 7) / 8 * 8;
     p.ld_part = (N + 7) / 8 * 8;
@@ -525,7 +600,7 @@ int32_t iso_act_wgrad(const iso_mat* dY, const iso_act* pack, const iso_mat* out
     WgradMaps maps;
     ISO_TRY(bf16_map(&maps.b, xb.data, T, N, p.ldx));
     for (int q = 0; q < WG_MAX_PARTS; ++q) {
-        const int part = std::min(q, p.n_parts - 1);
+        const int part = std::max(0, p.n_parts - 1 - q);     // the last part first: small sums before large ones
         if (p.dy_direct)
             ISO_TRY(bf16_map(&maps.a[q], dY->data, T, M, dY->rows == 1 ? (M + 7) / 8 * 8 : dY->ld));
         else
@@ -536,8 +611,8 @@ int32_t iso_act_wgrad(const iso_mat* dY, const iso_act* pack, const iso_mat* out
     g.N = (int)N;
     g.m_tiles = p.m_tiles;
     g.n_tiles = p.n_tiles;
+    g.t_tiles = p.k_tiles / p.n_parts;
     g.k_tiles = p.k_tiles;
-    g.parts = p.n_parts;
     g.split = p.split;
     g.accumulate = accumulate;
     g.out = out->data;
