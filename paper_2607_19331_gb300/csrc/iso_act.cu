@@ -27,7 +27,7 @@ int train_sms() {
 
 namespace {
 
-constexpr int ACT_TPB = 256;
+constexpr int ACT_TPB = 128;
 constexpr int ACT_WPB = ACT_TPB / 32;
 
 struct ActView {
@@ -36,11 +36,11 @@ struct ActView {
     long long ld_codes, ld_exps;
 };
 
-// Segments of a rows x cols matrix, row after row: item i is segment i % segs
-// of row i / segs.
+// Runs of SEGS neighbouring segments of a row, row after row: item i is run
+// i % runs of row i / runs.
 struct Items {
     long long n;
-    int segs;
+    int runs;
 };
 
 // this lane's eight codes at channel c (below the padded width) and the
@@ -67,41 +67,126 @@ __device__ __forceinline__ void act_load(const ActView& a, long long row, int c,
     }
 }
 
+// Four segments of a row to a warp: their addresses are one base and constant
+// offsets, and their loads are all in flight before the first is used.  The
+// issue rate is as near a bound as HBM: with one segment a warp and a
+// persistent grid the packing took 21 instructions an entry and 110 us for
+// 16384 x 8960 bf16, the SwiGLU pair 322 + 352 us for 8192 x 18944.
+// Blocks are small and not persistent, so that those in flight cover one moving
+// window of every operand: blocks of 128 threads measured 74 / 69 / 203 / 248 us
+// (pack, unpack, SwiGLU, its gradients at those sizes: 6.0, 6.4, 6.2, 6.3 TB/s),
+// of 256 threads 78 / 69 / 228 / 253 us, a persistent grid 76 / 74 / 221 / 246 us.
+constexpr int SEGS = 4;
+
+// One run of a warp: row, first channel of this lane, and how many of its
+// segments lie wholly inside rows that start on 16-byte boundaries (those take
+// the fast form; the others check every entry).
+struct Run {
+    long long row;
+    int c, full;
+    __device__ __forceinline__ Run(const Items& it, long long i, int lane, int cols, bool vec) {
+        row = i / it.runs;
+        const int c0 = (int)(i - row * it.runs) * (SEGS * TRAIN_SEG);
+        c = c0 + lane * 8;
+        full = vec ? min(SEGS, (cols - c0) / TRAIN_SEG) : 0;
+    }
+};
+#define ACT_FOR_RUNS                                                                          \
+    const int lane = threadIdx.x & 31;                                                        \
+    for (long long i = (long long)blockIdx.x * ACT_WPB + (threadIdx.x >> 5); i < it.n;        \
+         i += (long long)gridDim.x * ACT_WPB)
+
+// Exponent bytes of a run's full segments: every lane of a group holds all
+// four, and stores the one of its place in the group.
+__device__ __forceinline__ void store_exps(const ActView& a, const Run& r, int lane, const uint32_t (&b)[SEGS]) {
+    const int k = lane & 3;
+    const uint32_t mine = k == 0 ? b[0] : k == 1 ? b[1] : k == 2 ? b[2] : b[3];
+    if (k < r.full)
+        a.exps[r.row * a.ld_exps + r.c / ISO_ACT_GROUP + k * (TRAIN_SEG / ISO_ACT_GROUP)] = (uint8_t)mine;
+}
+
+template <typename T>
+__device__ __forceinline__ uint2 encode_raw(const Raw8<T>& x, const float (&v)[8], uint32_t& b) {
+    b = act_exp_byte(group_max(x.abs_max()));
+    return act_codes(v, b);
+}
+
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(ACT_TPB) k_act_pack(const T* x, long long ld, int cols, ActView out, Items it) {
-    const int lane = threadIdx.x & 31;
-    const long long warps = (long long)gridDim.x * ACT_WPB;
-    for (long long i = (long long)blockIdx.x * ACT_WPB + (threadIdx.x >> 5); i < it.n; i += warps) {
-        const long long row = i / it.segs;
-        const int c = (int)(i - row * it.segs) * TRAIN_SEG + lane * 8;
-        float v[8];
-        load8<VEC>(x + row * ld, c, cols, v);
-        uint2 q;
-        const uint32_t b = act_encode(v, q);
-        act_store(out, row, c, cols, q, b);
+    ACT_FOR_RUNS {
+        const Run r(it, i, lane, cols, VEC);
+        const T* src = x + r.row * ld + r.c;
+        uint8_t* codes = out.codes + r.row * out.ld_codes + r.c;
+        Raw8<T> raw[SEGS];
+#pragma unroll
+        for (int k = 0; k < SEGS; ++k)
+            if (VEC && k < r.full) raw[k].load(src + k * TRAIN_SEG);
+        uint32_t b[SEGS] = {};
+#pragma unroll
+        for (int k = 0; k < SEGS; ++k) {
+            float v[8];
+            if (VEC && k < r.full) {
+                raw[k].get(v);
+                *reinterpret_cast<uint2*>(codes + k * TRAIN_SEG) = encode_raw(raw[k], v, b[k]);
+            } else if (r.c - lane * 8 + k * TRAIN_SEG < cols) {
+                const int c = r.c + k * TRAIN_SEG;
+                load8<false>(x + r.row * ld, c, cols, v);
+                uint2 q;
+                const uint32_t e = act_encode(v, q);
+                act_store(out, r.row, c, cols, q, e);
+            }
+        }
+        store_exps(out, r, lane, b);
     }
 }
 
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(ACT_TPB) k_act_unpack(ActView in, int cols, T* out, long long ld, Items it) {
-    const int lane = threadIdx.x & 31;
-    const long long warps = (long long)gridDim.x * ACT_WPB;
-    for (long long i = (long long)blockIdx.x * ACT_WPB + (threadIdx.x >> 5); i < it.n; i += warps) {
-        const long long row = i / it.segs;
-        const int c = (int)(i - row * it.segs) * TRAIN_SEG + lane * 8;
-        uint2 q;
-        uint32_t b;
-        act_load(in, row, c, cols, q, b);
-        float v[8];
-        act_decode(q, b, v);
-        store8<VEC>(out + row * ld, c, cols, v);
+    ACT_FOR_RUNS {
+        const Run r(it, i, lane, cols, VEC);
+        T* dst = out + r.row * ld + r.c;
+        const uint8_t* codes = in.codes + r.row * in.ld_codes + r.c;
+        const uint8_t* exps = in.exps + r.row * in.ld_exps + r.c / ISO_ACT_GROUP;
+        uint2 q[SEGS];
+        uint32_t b[SEGS];
+#pragma unroll
+        for (int k = 0; k < SEGS; ++k)
+            if (VEC && k < r.full) {
+                q[k] = __ldcs(reinterpret_cast<const uint2*>(codes + k * TRAIN_SEG));
+                b[k] = exps[k * (TRAIN_SEG / ISO_ACT_GROUP)];
+            }
+#pragma unroll
+        for (int k = 0; k < SEGS; ++k) {
+            float v[8];
+            if (VEC && k < r.full) {
+                act_decode(q[k], b[k], v);
+                put8(dst + k * TRAIN_SEG, v);
+            } else if (r.c - lane * 8 + k * TRAIN_SEG < cols) {
+                const int c = r.c + k * TRAIN_SEG;
+                act_load(in, r.row, c, cols, q[k], b[k]);
+                act_decode(q[k], b[k], v);
+                store8<false>(out + r.row * ld, c, cols, v);
+            }
+        }
     }
 }
 
+// x / (1 + exp(-x)).  bfloat16 outputs take the fast exponential and
+// reciprocal (a few binary32 ulps, 1.2 more for every unit of |x|; a bfloat16
+// ulp is 2^16 of them), binary32 outputs CUDA's expf and an IEEE division.
+template <typename T>
+__device__ __forceinline__ float silu(float x) {
+    if (sizeof(T) == 2) return __fdividef(x, 1.0f + __expf(-x));
+    const float e = expf(-fabsf(x)), r = __fdiv_rn(1.0f, 1.0f + e);
+    return x * (x < 0.0f ? e * r : r);
+}
 // s = 1 / (1 + exp(-x)) and 1 - s, both without cancellation and down to the
 // subnormals: with e = exp(-|x|) they are 1 / (1 + e) and e / (1 + e).
+template <typename T>
 __device__ __forceinline__ void sigmoid(float x, float& s, float& rest) {
-    const float e = expf(-fabsf(x)), r = __fdiv_rn(1.0f, 1.0f + e), er = e * r;
+    const float e = sizeof(T) == 2 ? __expf(-fabsf(x)) : expf(-fabsf(x));
+    const float r = sizeof(T) == 2 ? __fdividef(1.0f, 1.0f + e) : __fdiv_rn(1.0f, 1.0f + e);
+    const float er = e * r;
     s = x < 0.0f ? er : r;
     rest = x < 0.0f ? r : er;
 }
@@ -110,26 +195,62 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(ACT_TPB) k_swiglu_pack(const T* gate, long long ldg, const T* up, long long ldu,
                                                          T* h, long long ldh, int cols, ActView gp, ActView up_p,
                                                          Items it) {
-    const int lane = threadIdx.x & 31;
-    const long long warps = (long long)gridDim.x * ACT_WPB;
-    for (long long i = (long long)blockIdx.x * ACT_WPB + (threadIdx.x >> 5); i < it.n; i += warps) {
-        const long long row = i / it.segs;
-        const int c = (int)(i - row * it.segs) * TRAIN_SEG + lane * 8;
-        float g[8], u[8], o[8];
-        load8<VEC>(gate + row * ldg, c, cols, g);
-        load8<VEC>(up + row * ldu, c, cols, u);
+    ACT_FOR_RUNS {
+        const Run r(it, i, lane, cols, VEC);
+        const T* sg = gate + r.row * ldg + r.c;
+        const T* su = up + r.row * ldu + r.c;
+        T* dst = h + r.row * ldh + r.c;
+        uint8_t* cg = gp.codes + r.row * gp.ld_codes + r.c;
+        uint8_t* cu = up_p.codes + r.row * up_p.ld_codes + r.c;
+        Raw8<T> rg[SEGS], ru[SEGS];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float s, rest;
-            sigmoid(g[j], s, rest);
-            o[j] = g[j] * s * u[j];
+        for (int k = 0; k < SEGS; ++k)
+            if (VEC && k < r.full) {
+                rg[k].load(sg + k * TRAIN_SEG);
+                ru[k].load(su + k * TRAIN_SEG);
+            }
+        uint32_t bg[SEGS] = {}, bu[SEGS] = {};
+#pragma unroll
+        for (int k = 0; k < SEGS; ++k) {
+            float g[8], u[8], o[8];
+            if (VEC && k < r.full) {
+                rg[k].get(g);
+                ru[k].get(u);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = silu<T>(g[j]) * u[j];
+                put8(dst + k * TRAIN_SEG, o);
+                *reinterpret_cast<uint2*>(cg + k * TRAIN_SEG) = encode_raw(rg[k], g, bg[k]);
+                *reinterpret_cast<uint2*>(cu + k * TRAIN_SEG) = encode_raw(ru[k], u, bu[k]);
+            } else if (r.c - lane * 8 + k * TRAIN_SEG < cols) {
+                const int c = r.c + k * TRAIN_SEG;
+                load8<false>(gate + r.row * ldg, c, cols, g);
+                load8<false>(up + r.row * ldu, c, cols, u);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = silu<T>(g[j]) * u[j];
+                store8<false>(h + r.row * ldh, c, cols, o);
+                uint2 q;
+                uint32_t b = act_encode(g, q);
+                act_store(gp, r.row, c, cols, q, b);
+                b = act_encode(u, q);
+                act_store(up_p, r.row, c, cols, q, b);
+            }
         }
-        store8<VEC>(h + row * ldh, c, cols, o);
-        uint2 q;
-        uint32_t b = act_encode(g, q);
-        act_store(gp, row, c, cols, q, b);
-        b = act_encode(u, q);
-        act_store(up_p, row, c, cols, q, b);
+        store_exps(gp, r, lane, bg);
+        store_exps(up_p, r, lane, bu);
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void swiglu_grads(const float (&d)[8], const float (&g)[8], const float (&u)[8],
+                                             float (&og)[8], float (&ou)[8], float (&oh)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        float s, rest;
+        sigmoid<T>(g[j], s, rest);
+        const float gs = g[j] * s;
+        ou[j] = d[j] * gs;
+        oh[j] = gs * u[j];
+        og[j] = d[j] * u[j] * (s * (1.0f + g[j] * rest));
     }
 }
 
@@ -137,31 +258,52 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(ACT_TPB) k_swiglu_grad(const T* dh, long long ldd, ActView gp, ActView up_p,
                                                          int cols, T* d_gate, long long ldg, T* d_up, long long ldu,
                                                          T* h, long long ldh, Items it) {
-    const int lane = threadIdx.x & 31;
-    const long long warps = (long long)gridDim.x * ACT_WPB;
-    for (long long i = (long long)blockIdx.x * ACT_WPB + (threadIdx.x >> 5); i < it.n; i += warps) {
-        const long long row = i / it.segs;
-        const int c = (int)(i - row * it.segs) * TRAIN_SEG + lane * 8;
-        uint2 qg, qu;
-        uint32_t bg, bu;
-        float d[8], g[8], u[8], og[8], ou[8], oh[8];
-        act_load(gp, row, c, cols, qg, bg);
-        act_load(up_p, row, c, cols, qu, bu);
-        load8<VEC>(dh + row * ldd, c, cols, d);
-        act_decode(qg, bg, g);
-        act_decode(qu, bu, u);
+    ACT_FOR_RUNS {
+        const Run r(it, i, lane, cols, VEC);
+        const T* sd = dh + r.row * ldd + r.c;
+        T* dg = d_gate + r.row * ldg + r.c;
+        T* du = d_up + r.row * ldu + r.c;
+        T* hh = h + r.row * ldh + r.c;
+        const uint8_t* cg = gp.codes + r.row * gp.ld_codes + r.c;
+        const uint8_t* cu = up_p.codes + r.row * up_p.ld_codes + r.c;
+        const uint8_t* eg = gp.exps + r.row * gp.ld_exps + r.c / ISO_ACT_GROUP;
+        const uint8_t* eu = up_p.exps + r.row * up_p.ld_exps + r.c / ISO_ACT_GROUP;
+        Raw8<T> rd[SEGS];
+        uint2 qg[SEGS], qu[SEGS];
+        uint32_t bg[SEGS], bu[SEGS];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float s, rest;
-            sigmoid(g[j], s, rest);
-            const float gs = g[j] * s;
-            ou[j] = d[j] * gs;
-            oh[j] = gs * u[j];
-            og[j] = d[j] * u[j] * (s * (1.0f + g[j] * rest));
+        for (int k = 0; k < SEGS; ++k)
+            if (VEC && k < r.full) {
+                rd[k].load(sd + k * TRAIN_SEG);
+                qg[k] = __ldcs(reinterpret_cast<const uint2*>(cg + k * TRAIN_SEG));
+                qu[k] = __ldcs(reinterpret_cast<const uint2*>(cu + k * TRAIN_SEG));
+                bg[k] = eg[k * (TRAIN_SEG / ISO_ACT_GROUP)];
+                bu[k] = eu[k * (TRAIN_SEG / ISO_ACT_GROUP)];
+            }
+#pragma unroll
+        for (int k = 0; k < SEGS; ++k) {
+            float d[8], g[8], u[8], og[8], ou[8], oh[8];
+            if (VEC && k < r.full) {
+                rd[k].get(d);
+                act_decode(qg[k], bg[k], g);
+                act_decode(qu[k], bu[k], u);
+                swiglu_grads<T>(d, g, u, og, ou, oh);
+                put8(dg + k * TRAIN_SEG, og);
+                put8(du + k * TRAIN_SEG, ou);
+                if (h) put8(hh + k * TRAIN_SEG, oh);
+            } else if (r.c - lane * 8 + k * TRAIN_SEG < cols) {
+                const int c = r.c + k * TRAIN_SEG;
+                act_load(gp, r.row, c, cols, qg[k], bg[k]);
+                act_load(up_p, r.row, c, cols, qu[k], bu[k]);
+                load8<false>(dh + r.row * ldd, c, cols, d);
+                act_decode(qg[k], bg[k], g);
+                act_decode(qu[k], bu[k], u);
+                swiglu_grads<T>(d, g, u, og, ou, oh);
+                store8<false>(d_gate + r.row * ldg, c, cols, og);
+                store8<false>(d_up + r.row * ldu, c, cols, ou);
+                if (h) store8<false>(h + r.row * ldh, c, cols, oh);
+            }
         }
-        store8<VEC>(d_gate + row * ldg, c, cols, og);
-        store8<VEC>(d_up + row * ldu, c, cols, ou);
-        if (h) store8<VEC>(h + row * ldh, c, cols, oh);
     }
 }
 
@@ -170,11 +312,11 @@ ActView view(const iso_act* a) {
             (long long)a->ld_exps};
 }
 Items items_of(int64_t rows, int64_t cols) {
-    const int segs = (int)((cols + TRAIN_SEG - 1) / TRAIN_SEG);
-    return {(long long)rows * segs, segs};
+    const int runs = (int)((cols + SEGS * TRAIN_SEG - 1) / (SEGS * TRAIN_SEG));
+    return {(long long)rows * runs, runs};
 }
-int act_grid(const Items& it) {
-    return (int)std::max(1LL, std::min((it.n + ACT_WPB - 1) / ACT_WPB, (long long)train_sms() * 8));
+unsigned act_grid(const Items& it) {
+    return (unsigned)std::min((it.n + ACT_WPB - 1) / ACT_WPB, (long long)EXTENT_LIMIT);
 }
 
 template <typename F>

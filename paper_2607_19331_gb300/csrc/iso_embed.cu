@@ -1,24 +1,27 @@
 // iso_embed.cu -- the token embedding and its gradient by sorted tokens.
 //
-// Forward: a gather of table rows, bound by HBM; a warp takes 256 channels of
-// one token at a time (16-byte loads).
+// Forward: a gather of table rows, bound by HBM; a warp takes up to 1024
+// channels of one token, all its loads in flight at once.
 //
 // Gradient: grad[v] = scale * sum of dY[t] over the tokens of id v.
-//   k_sort_fill  one cluster of eight CTAs sorts (id, token) by a stable LSD
-//                radix sort, digits of up to nine bits, while the other CTAs
-//                write the zeros of a gradient that is not accumulated (a
-//                vocabulary has far more rows than a batch has tokens, so the
-//                zeros are the bulk of the traffic and hide the sort; rows
-//                with tokens are written a second time);
-//   k_row_sums   sorted tokens in windows of 32: a warp adds the window's dY
-//                rows over 256 channels and writes the sum of every run of
-//                equal ids that lies inside the window; a run that crosses a
-//                window's edge leaves one partial row per window;
+//   k_sort       one cluster of eight CTAs (one CTA for few tokens) sorts
+//                (id, token) by a stable LSD radix sort, digits of up to nine
+//                bits;
+//   k_fill       writes the zeros of a gradient that is not accumulated.  A
+//                vocabulary has far more rows than a batch has tokens, so this
+//                is the bulk of the traffic; it runs beside the sort (a
+//                programmatic launch) and hides it.  Rows with tokens are
+//                written a second time;
+//   k_row_sums   the sorted tokens in windows of equal length: a warp adds a
+//                window's dY rows over 256 channels and writes the sum of
+//                every run of equal ids that lies inside the window; a run
+//                that crosses a window's edge leaves one partial row a window;
 //   k_row_join   the runs that cross windows: partials added, row written.
-// Sums are binary32 and their order is fixed by the sorted positions: windows
-// of 32 in ascending token order, then the window sums, so equal inputs give
-// equal bits and a frequent id's sum is a short tree, not one long chain.
+// Sums are binary32 and their order is fixed by the sorted positions and the
+// window length (a function of the sizes alone), so equal inputs give equal
+// bits, and a frequent id's sum is a short tree, not one long chain.
 #include "iso_train.cuh"
+#include "iso_internal.cuh"
 
 #include <algorithm>
 #include <cmath>
@@ -29,17 +32,25 @@ namespace cg = cooperative_groups;
 namespace iso {
 namespace {
 
-constexpr int EM_TPB = 256;
+constexpr int EM_TPB = 128;
 constexpr int EM_WPB = EM_TPB / 32;
+constexpr int EM_SEGS = 4;                              // segments of one token a warp takes
 
 constexpr int SORT_CLUSTER = 8;
 constexpr int SORT_TPB = 1024;
 constexpr int SORT_WARPS = SORT_TPB / 32;
 constexpr int SORT_BITS = 9;
 constexpr int SORT_BINS = 1 << SORT_BITS;
-constexpr int FILL_CHUNK = 16384;                       // bytes of zeros a warp writes at a time
-constexpr int WIN = 32;                                 // sorted tokens per window
-constexpr int JOIN_TPB = 512;
+constexpr long long SORT_ONE_CTA = 4096;                // up to this many tokens one CTA sorts alone
+constexpr int SORT_SMEM = (SORT_WARPS * SORT_BINS + SORT_BINS + 32 + 4) * (int)sizeof(uint32_t);
+constexpr int FILL_TPB = 256;
+constexpr int FILL_CHUNK = 8192;                        // bytes of zeros a warp writes
+constexpr int SUM_TPB = 256;
+constexpr int SUM_WPB = SUM_TPB / 32;
+constexpr int SUM_RING = 4096;                          // bytes of dY rows in flight per warp
+constexpr int SUM_WARPS_PER_SM = 24;                    // windows are as long as leaves this many warps a SM
+constexpr int WIN_MIN = 8, WIN_MAX = 256;
+constexpr int JOIN_TPB = 128;
 constexpr int JOIN_COLS = 128;
 
 struct Ids {
@@ -58,23 +69,37 @@ __device__ __forceinline__ long long load_id(const Ids& ids, long long t) {
 // ---------------------------------------------------------------------------
 template <typename T, typename O, bool VEC>
 __global__ void __launch_bounds__(EM_TPB) k_embed(const T* table, long long ldt, Ids ids, float scale, O* out,
-                                                  long long ldo, int cols, int segs, int32_t* status) {
+                                                  long long ldo, int cols, int runs, int32_t* status) {
     const int lane = threadIdx.x & 31;
-    const long long items = ids.n * segs, warps = (long long)gridDim.x * EM_WPB;
-    for (long long i = (long long)blockIdx.x * EM_WPB + (threadIdx.x >> 5); i < items; i += warps) {
-        const long long t = i / segs;
-        const int c = (int)(i - t * segs) * TRAIN_SEG + lane * 8;
+    const long long items = ids.n * runs;
+    for (long long i = (long long)blockIdx.x * EM_WPB + (threadIdx.x >> 5); i < items; i += (long long)gridDim.x * EM_WPB) {
+        const long long t = i / runs;
+        const int c0 = (int)(i - t * runs) * (EM_SEGS * TRAIN_SEG), c = c0 + lane * 8;
         const long long id = load_id(ids, t);
-        float v[8] = {};
-        if (id == ids.pad_id) {
-        } else if (id >= 0 && id < ids.rows) {
-            load8<VEC>(table + id * ldt, c, cols, v);
+        const bool in = id != ids.pad_id && id >= 0 && id < ids.rows;
+        if (!in && id != ids.pad_id && status && lane == 0) *status = ISO_ERR_INDEX;
+        const int full = VEC ? min(EM_SEGS, (cols - c0) / TRAIN_SEG) : 0;
+        const T* src = table + (in ? id : 0) * ldt;
+        O* dst = out + t * ldo;
+        Raw8<T> raw[EM_SEGS];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= scale;
-        } else if (status && lane == 0) {
-            *status = ISO_ERR_INDEX;
+        for (int k = 0; k < EM_SEGS; ++k)
+            if (VEC && k < full && in) raw[k].load(src + c + k * TRAIN_SEG);
+#pragma unroll
+        for (int k = 0; k < EM_SEGS; ++k) {
+            float v[8] = {};
+            if (VEC && k < full) {
+                if (in) raw[k].get(v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] *= scale;
+                put8(dst + c + k * TRAIN_SEG, v);
+            } else if (c0 + k * TRAIN_SEG < cols) {
+                if (in) load8<VEC>(src, c + k * TRAIN_SEG, cols, v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] *= scale;
+                store8<VEC>(dst, c + k * TRAIN_SEG, cols, v);
+            }
         }
-        store8<VEC>(out + t * ldo, c, cols, v);
     }
 }
 
@@ -98,12 +123,17 @@ __device__ __forceinline__ void warp_zero(char* p, long long len, int lane) {
     for (long long i = vecs * 16 + 2 * lane; i < len; i += 64) *reinterpret_cast<uint16_t*>(p + i) = 0;
 }
 
-__device__ void fill_zeros(const FillArgs& f, long long warp, long long warps, int lane) {
-    const long long per_row = (f.width + FILL_CHUNK - 1) / FILL_CHUNK;
-    for (long long i = warp; i < f.rows * per_row; i += warps) {
+// zeros in short blocks, in the order of addresses (a persistent grid reaches
+// 6.4 - 6.6 TB/s of writes here, short blocks 7.7)
+__global__ void __launch_bounds__(FILL_TPB) k_fill(FillArgs f) {
+    const int lane = threadIdx.x & 31;
+    const long long per_row = (f.width + FILL_CHUNK - 1) / FILL_CHUNK, warps = (long long)gridDim.x * (FILL_TPB / 32);
+    for (long long i = (long long)blockIdx.x * (FILL_TPB / 32) + (threadIdx.x >> 5); i < f.rows * per_row; i += warps) {
         const long long r = i / per_row, off = (i - r * per_row) * FILL_CHUNK;
         warp_zero(f.base + r * f.stride + off, min((long long)FILL_CHUNK, f.width - off), lane);
     }
+    // this grid is not done before the sort that it started beside
+    if (blockIdx.x == gridDim.x - 1) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 struct SortArgs {
@@ -122,27 +152,29 @@ __device__ __forceinline__ uint2 sort_item(const SortArgs& a, const uint2* src, 
     return make_uint2(!pad && in ? (uint32_t)id : (uint32_t)a.ids.rows, (uint32_t)t);
 }
 
-__global__ void __cluster_dims__(SORT_CLUSTER, 1, 1) __launch_bounds__(SORT_TPB)
-k_sort_fill(SortArgs a, FillArgs f) {
+// CTAS: the CTAs of the one cluster that is launched
+template <int CTAS>
+__global__ void __launch_bounds__(SORT_TPB, 1) k_sort(SortArgs a) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the fill may start
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (blockIdx.x >= SORT_CLUSTER) {
-        fill_zeros(f, (long long)(blockIdx.x - SORT_CLUSTER) * SORT_WARPS + warp,
-                   (long long)(gridDim.x - SORT_CLUSTER) * SORT_WARPS, lane);
-        return;
-    }
     extern __shared__ uint32_t sort_smem[];
     uint32_t* const cnt = sort_smem;                                  // [warp][bin]
     uint32_t* const tot = cnt + SORT_WARPS * SORT_BINS;               // [bin]: this CTA's items
     uint32_t* const scan = tot + SORT_BINS;                           // [warp sums]
     int* const bad_flag = reinterpret_cast<int*>(scan + 32);
     cg::cluster_group cluster = cg::this_cluster();
-    const int me = (int)cluster.block_rank();
+    auto sync_all = [&] { if (CTAS == 1) __syncthreads(); else cluster.sync(); };
+    const int me = CTAS == 1 ? 0 : (int)cluster.block_rank();
     const uint32_t lt = (1u << lane) - 1u;
     // every warp owns a contiguous range of positions, in order, so that ranks
     // counted range by range are stable
     const long long n = a.ids.n;
-    const long long per = ((n + SORT_CLUSTER * SORT_WARPS - 1) / (SORT_CLUSTER * SORT_WARPS) + 31) / 32 * 32;
+    const long long per = ((n + CTAS * SORT_WARPS - 1) / (CTAS * SORT_WARPS) + 31) / 32 * 32;
     const long long t0 = min(n, ((long long)me * SORT_WARPS + warp) * per), t1 = min(n, t0 + per);
+    // warps of this CTA that have items
+    const long long cta0 = min(n, (long long)me * SORT_WARPS * per);
+    const int warps = per ? (int)min((long long)SORT_WARPS, (n - cta0 + per - 1) / per) : 0;
+    const int bins = 1 << a.bits;
     if (threadIdx.x == 0) *bad_flag = 0;
     __syncthreads();
     bool bad = false;
@@ -150,10 +182,11 @@ k_sort_fill(SortArgs a, FillArgs f) {
         const uint2* src = p == 0 ? nullptr : a.buf[(a.passes - p) & 1];
         uint2* dst = a.buf[(a.passes - 1 - p) & 1];
         const int shift = p * a.bits;
-        const uint32_t mask = (1u << a.bits) - 1u;
-        for (int i = threadIdx.x; i < SORT_WARPS * SORT_BINS; i += SORT_TPB) cnt[i] = 0;
-        __syncthreads();
+        const uint32_t mask = (uint32_t)bins - 1u;
         uint32_t* const mine = cnt + warp * SORT_BINS;
+        if (warp < warps)
+            for (int i = lane; i < bins; i += 32) mine[i] = 0;
+        __syncwarp();
         for (long long b = t0; b < t1; b += 32) {
             const bool on = b + lane < t1;
             const uint32_t active = __ballot_sync(0xFFFFFFFFu, on);
@@ -167,21 +200,23 @@ k_sort_fill(SortArgs a, FillArgs f) {
         if (bad) *bad_flag = 1;
         __syncthreads();
         // bins: prefix over this CTA's warps, the CTA's total
-        if (threadIdx.x < SORT_BINS) {
+        if (threadIdx.x < bins) {
             uint32_t s = 0;
-            for (int w = 0; w < SORT_WARPS; ++w) {
+#pragma unroll 8
+            for (int w = 0; w < warps; ++w) {
                 const uint32_t v = cnt[w * SORT_BINS + threadIdx.x];
                 cnt[w * SORT_BINS + threadIdx.x] = s;
                 s += v;
             }
             tot[threadIdx.x] = s;
         }
-        cluster.sync();
+        sync_all();
         // start of each bin for this CTA: earlier bins of all CTAs, earlier CTAs of this bin
         uint32_t all = 0, before = 0;
-        if (threadIdx.x < SORT_BINS) {
-            for (int c = 0; c < SORT_CLUSTER; ++c) {
-                const uint32_t v = cluster.map_shared_rank(tot, c)[threadIdx.x];
+        if (threadIdx.x < bins) {
+#pragma unroll
+            for (int c = 0; c < CTAS; ++c) {
+                const uint32_t v = CTAS == 1 ? tot[threadIdx.x] : cluster.map_shared_rank(tot, c)[threadIdx.x];
                 all += v;
                 if (c < me) before += v;
             }
@@ -194,10 +229,11 @@ k_sort_fill(SortArgs a, FillArgs f) {
         }
         if (lane == 31) scan[warp] = inc;
         __syncthreads();
-        if (threadIdx.x < SORT_BINS) {
+        if (threadIdx.x < bins) {
             uint32_t base = before + inc - all;
             for (int w = 0; w < warp; ++w) base += scan[w];
-            for (int w = 0; w < SORT_WARPS; ++w) cnt[w * SORT_BINS + threadIdx.x] += base;
+#pragma unroll 8
+            for (int w = 0; w < warps; ++w) cnt[w * SORT_BINS + threadIdx.x] += base;
         }
         __syncthreads();
         for (long long b = t0; b < t1; b += 32) {
@@ -216,11 +252,11 @@ k_sort_fill(SortArgs a, FillArgs f) {
         }
         if (p == 0 && me == 0 && threadIdx.x == 0) {
             int any = 0;
-            for (int c = 0; c < SORT_CLUSTER; ++c) any |= *cluster.map_shared_rank(bad_flag, c);
+            for (int c = 0; c < CTAS; ++c) any |= CTAS == 1 ? *bad_flag : *cluster.map_shared_rank(bad_flag, c);
             if (a.status) *a.status = any ? (int32_t)ISO_ERR_INDEX : (int32_t)ISO_OK;
             *a.n_joins = 0;
         }
-        cluster.sync();   // dst is complete; no CTA still reads another's shared memory
+        sync_all();   // dst is complete; no CTA still reads another's shared memory
     }
 }
 
@@ -230,6 +266,7 @@ struct RowArgs {
     uint32_t rows;          // table rows: the id of padding
     float scale;
     int cols, segs, accumulate;
+    int win;                // sorted tokens per window
     float* part;            // [window][2][cols]: the run that enters the window, the run that leaves it
     long long ld_part;
     uint32_t* joins;        // windows whose last run starts there and goes on
@@ -251,69 +288,112 @@ __device__ __forceinline__ void write_row(O* row, int c, int cols, float (&v)[8]
     store8<VEC>(row, c, cols, v);
 }
 
-template <typename T, typename O, bool VEC>
-__global__ void __launch_bounds__(EM_TPB) k_row_sums(const T* dy, long long ldd, O* grad, long long ldg, RowArgs a) {
-    const int lane = threadIdx.x & 31;
-    const long long wins = (a.n + WIN - 1) / WIN, items = wins * a.segs, warps = (long long)gridDim.x * EM_WPB;
-    for (long long i = (long long)blockIdx.x * EM_WPB + (threadIdx.x >> 5); i < items; i += warps) {
-        const long long w = i / a.segs;
-        const int seg = (int)(i - w * a.segs), c = seg * TRAIN_SEG + lane * 8;
-        const long long p0 = w * WIN;
-        const uint2 it = p0 + lane < a.n ? a.sorted[p0 + lane] : make_uint2(a.rows, 0u);
-        const uint32_t prev = p0 > 0 ? a.sorted[p0 - 1].x : 0xFFFFFFFFu;
-        const uint32_t next = p0 + WIN < a.n ? a.sorted[p0 + WIN].x : 0xFFFFFFFFu;
-        float acc[8] = {};
-        bool enters = __shfl_sync(0xFFFFFFFFu, it.x, 0) == prev;
-        constexpr int UN = 8;
-#pragma unroll 1
-        for (int b = 0; b < WIN; b += UN) {
-            float v[UN][8];
+// eight channels of a row of dY into this lane's place in shared memory,
+// channels past the end as zeros
+template <typename T>
+__device__ __forceinline__ void copy8_async(uint32_t dst, const T* row, int c, int cols) {
+    const int bytes = max(0, min(8, cols - c)) * (int)sizeof(T);
+    const char* src = reinterpret_cast<const char*>(row + (bytes ? c : 0));
 #pragma unroll
-            for (int j = 0; j < UN; ++j) {
-                const uint32_t id = __shfl_sync(0xFFFFFFFFu, it.x, b + j), pos = __shfl_sync(0xFFFFFFFFu, it.y, b + j);
-                if (id < a.rows) load8<VEC>(dy + (long long)pos * ldd, c, a.cols, v[j]);
-            }
-#pragma unroll
-            for (int j = 0; j < UN; ++j) {
-                const uint32_t id = __shfl_sync(0xFFFFFFFFu, it.x, b + j);
-                if (id >= a.rows) break;
-                const uint32_t nx = __shfl_sync(0xFFFFFFFFu, it.x, (b + j + 1) & 31);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) acc[k] += v[j][k];
-                const bool last = b + j == WIN - 1;
-                const bool leaves = last && next == id;
-                if (!last && nx == id) continue;
-                if (!enters && !leaves) {
-                    write_row<O, VEC>(grad + (long long)id * ldg, c, a.cols, acc, a.scale, a.accumulate);
-                } else if (c < a.cols) {
-                    float* part = a.part + (w * 2 + (enters ? 0 : 1)) * a.ld_part;
-                    store8<true>(part, c, (int)a.ld_part, acc);
-                }
-                if (!enters && leaves && seg == 0 && lane == 0) a.joins[atomicAdd(a.n_joins, 1u)] = (uint32_t)w;
-                enters = false;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) acc[k] = 0.0f;
-            }
-        }
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+        const int here = max(0, min(16, bytes - 16 * i));
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                     :: "r"(dst + 16u * i), "l"(src + (here ? 16 * i : 0)), "r"(here) : "memory");
     }
 }
 
-template <typename O, bool VEC>
+// A warp per (window, 256 channels).  Rows of dY that start on 16-byte
+// boundaries stream through a ring of rows in shared memory (every
+// lane reads back what it copied itself), so the loads of later tokens are
+// under way while a run is written; loaded eight tokens at a time into
+// registers instead, the 32768 x 3584 case measured 148 us, this way 80 us.
+template <typename T, typename O, bool VEC>
+__global__ void __launch_bounds__(SUM_TPB) k_row_sums(const T* dy, long long ldd, O* grad, long long ldg, RowArgs a) {
+    constexpr int LANE_BYTES = 8 * (int)sizeof(T), SLOT = 32 * LANE_BYTES, DEPTH = SUM_RING / SLOT;
+    __shared__ __align__(16) unsigned char ring[VEC ? SUM_WPB * SUM_RING : 16];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    unsigned char* const mine = ring + (VEC ? warp * SUM_RING + lane * LANE_BYTES : 0);
+    const uint32_t mine_s = smem_u32(mine);
+    const long long wins = (a.n + a.win - 1) / a.win, items = wins * a.segs;
+    for (long long i = (long long)blockIdx.x * SUM_WPB + warp; i < items; i += (long long)gridDim.x * SUM_WPB) {
+        const long long w = i / a.segs;
+        const int seg = (int)(i - w * a.segs), c = seg * TRAIN_SEG + lane * 8;
+        const long long p0 = w * a.win, end = min(a.n, p0 + a.win);
+        // lane l holds sorted item 32 q + l of the window, for this q and the next
+        auto items_at = [&](long long p) { return p + lane < end ? a.sorted[p + lane] : make_uint2(a.rows, 0u); };
+        uint2 cur = items_at(p0), nxt = items_at(p0 + 32);
+        const uint32_t prev = p0 > 0 ? a.sorted[p0 - 1].x : 0xFFFFFFFFu;
+        const uint32_t after = end < a.n ? a.sorted[end].x : 0xFFFFFFFFu;
+        auto id_at = [&](int k) { return __shfl_sync(0xFFFFFFFFu, k < 32 ? cur.x : nxt.x, k & 31); };
+        auto pos_at = [&](int k) { return __shfl_sync(0xFFFFFFFFu, k < 32 ? cur.y : nxt.y, k & 31); };
+        auto fetch = [&](int k, uint32_t slot) {                     // start the copy of item k (padding: nothing)
+            if (VEC) {
+                const uint32_t id = id_at(k), pos = pos_at(k);
+                if (id < a.rows) copy8_async(mine_s + slot * SLOT, dy + (long long)pos * ldd, c, a.cols);
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            }
+        };
+        float acc[8] = {};
+        uint32_t id = id_at(0);
+        bool enters = id == prev;
+#pragma unroll 1
+        for (int k = 0; k < DEPTH - 1; ++k) fetch(k, (uint32_t)k);
+        uint32_t slot = 0;
+        for (long long q = p0; id < a.rows; q += 32) {               // padding sorts last
+#pragma unroll 1
+            for (int k = 0; k < 32 && id < a.rows; ++k) {
+                const uint32_t next = id_at(k + 1);
+                fetch(k + DEPTH - 1, (slot + DEPTH - 1) % DEPTH);
+                float v[8];
+                if constexpr (VEC) {
+                    asm volatile("cp.async.wait_group %0;" :: "n"(DEPTH - 1) : "memory");
+                    Raw8<T> raw;
+                    raw.load_shared(mine + slot * SLOT);
+                    raw.get(v);
+                } else {
+                    load8<false>(dy + (long long)pos_at(k) * ldd, c, a.cols, v);
+                }
+                slot = (slot + 1) % DEPTH;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j] += v[j];
+                // past the window's end, ids read as padding
+                const bool leaves = q + k + 1 == end && after == id;
+                if (next != id) {
+                    if (!enters && !leaves)
+                        write_row<O, VEC>(grad + (long long)id * ldg, c, a.cols, acc, a.scale, a.accumulate);
+                    else if (c < a.cols)
+                        put8(a.part + (w * 2 + (enters ? 0 : 1)) * a.ld_part + c, acc);
+                    if (!enters && leaves && seg == 0 && lane == 0) a.joins[atomicAdd(a.n_joins, 1u)] = (uint32_t)w;
+                    enters = false;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) acc[j] = 0.0f;
+                }
+                id = next;
+            }
+            cur = nxt;
+            nxt = items_at(q + 64);
+        }
+        if (VEC) asm volatile("cp.async.wait_all;" ::: "memory");
+    }
+}
+
+// A CTA per (run, 128 channels): its warps take the run's partial rows in turn.
+template <typename O>
 __global__ void __launch_bounds__(JOIN_TPB) k_row_join(O* grad, long long ldg, RowArgs a) {
     __shared__ float4 sums[JOIN_TPB / 32][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr int WARPS = JOIN_TPB / 32;
     const int slices = (a.cols + JOIN_COLS - 1) / JOIN_COLS;
-    const long long items = (long long)*a.n_joins * slices, wins = (a.n + WIN - 1) / WIN;
+    const long long items = (long long)*a.n_joins * slices, wins = (a.n + a.win - 1) / a.win;
     for (long long i = blockIdx.x; i < items; i += gridDim.x) {
         const long long e = i / slices, w = a.joins[e];
         const int c = (int)(i - e * slices) * JOIN_COLS + lane * 4;
-        const uint32_t id = a.sorted[w * WIN + WIN - 1].x;
+        const uint32_t id = a.sorted[(w + 1) * a.win].x;
         // windows w + 1 .. w + k whose first token continues the run
         long long k = 0;
         for (;;) {
             const long long q = w + 1 + k + threadIdx.x;
-            const int got = __syncthreads_count(q < wins && a.sorted[q * WIN].x == id);
+            const int got = __syncthreads_count(q < wins && a.sorted[q * a.win].x == id);
             k += got;
             if (got < JOIN_TPB) break;
         }
@@ -357,15 +437,26 @@ Bytes2D ids_bytes(const void* ids, int32_t i64, int64_t n) {
     return {reinterpret_cast<uintptr_t>(ids), n > 0 ? 1u : 0u, (uint64_t)n * (i64 ? 8 : 4), (uint64_t)n * (i64 ? 8 : 4)};
 }
 
+// Sorted tokens per window: short enough for SUM_WARPS_PER_SM warps a SM (one
+// wave of k_row_sums), within WIN_MIN .. WIN_MAX.
+int window_of(int64_t n, int64_t cols) {
+    const long long segs = (cols + TRAIN_SEG - 1) / TRAIN_SEG, warps = (long long)train_sms() * SUM_WARPS_PER_SM;
+    int win = WIN_MIN;
+    while (win < WIN_MAX && n * segs > warps * win) win *= 2;
+    return win;
+}
+
 // workspace: header (join count), the two sort buffers, the join list, the partial rows
 struct GradLayout {
     size_t buf0, buf1, joins, part, end;
     long long ld_part;
+    int win;
 };
 GradLayout grad_layout(int64_t n, int64_t cols) {
     auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
-    const size_t wins = (size_t)((n + WIN - 1) / WIN);
     GradLayout L;
+    L.win = window_of(n, cols);
+    const size_t wins = (size_t)((n + L.win - 1) / L.win);
     L.ld_part = (cols + 7) / 8 * 8;
     L.buf0 = 256;
     L.buf1 = L.buf0 + up((size_t)n * sizeof(uint2));
@@ -373,6 +464,41 @@ GradLayout grad_layout(int64_t n, int64_t cols) {
     L.part = L.joins + up(wins * sizeof(uint32_t));
     L.end = L.part + up(wins * 2 * (size_t)L.ld_part * sizeof(float));
     return L;
+}
+
+// the sort: one cluster
+template <int CTAS>
+int launch_sort(const SortArgs& a, cudaStream_t s) {
+    if (cudaFuncSetAttribute(k_sort<CTAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, SORT_SMEM) != cudaSuccess)
+        return ISO_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(CTAS);
+    cfg.blockDim = dim3(SORT_TPB);
+    cfg.dynamicSmemBytes = SORT_SMEM;
+    cfg.stream = s;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = CTAS;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    TRAIN_LAUNCH(cudaLaunchKernelEx(&cfg, k_sort<CTAS>, a));
+    return ISO_OK;
+}
+// the zeros, allowed to start once the sort has
+int launch_fill(const FillArgs& f, cudaStream_t s) {
+    const long long chunks = f.rows * ((f.width + FILL_CHUNK - 1) / FILL_CHUNK);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)std::min((chunks + FILL_TPB / 32 - 1) / (FILL_TPB / 32), (long long)EXTENT_LIMIT));
+    cfg.blockDim = dim3(FILL_TPB);
+    cfg.stream = s;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    TRAIN_LAUNCH(cudaLaunchKernelEx(&cfg, k_fill, f));
+    return ISO_OK;
 }
 
 template <typename F>
@@ -403,14 +529,14 @@ int32_t iso_embed(const iso_mat* table, const void* ids, int32_t ids_i64, int64_
     if (status && cudaMemsetAsync(status, 0, sizeof(int32_t), s) != cudaSuccess) return ISO_ERR_CUDA;
     if (n == 0 || out->cols == 0) return ISO_OK;
     const Ids id{ids, (long long)n, (long long)pad_id, (long long)table->rows, ids_i64};
-    const int segs = (int)((out->cols + TRAIN_SEG - 1) / TRAIN_SEG);
-    const int grid = (int)std::max(1LL, std::min(((long long)n * segs + EM_WPB - 1) / EM_WPB, (long long)train_sms() * 8));
+    const int runs = (int)((out->cols + EM_SEGS * TRAIN_SEG - 1) / (EM_SEGS * TRAIN_SEG));
+    const unsigned grid = (unsigned)std::min(((long long)n * runs + EM_WPB - 1) / EM_WPB, (long long)EXTENT_LIMIT);
     return dispatch2(table->dtype, out->dtype, rows_aligned(table) && rows_aligned(out), [&](auto* tp, auto* op, auto v) -> int {
         using T = std::remove_pointer_t<decltype(tp)>;
         using O = std::remove_pointer_t<decltype(op)>;
         TRAIN_LAUNCH((k_embed<T, O, decltype(v)::value><<<grid, EM_TPB, 0, s>>>(
             static_cast<const T*>(table->data), table->ld, id, scale, static_cast<O*>(out->data), out->ld,
-            (int)out->cols, segs, status)));
+            (int)out->cols, runs, status)));
         return ISO_OK;
     });
 }
@@ -457,16 +583,9 @@ int32_t iso_embed_grad(const iso_mat* dY, const void* ids, int32_t ids_i64, int6
         fa = {static_cast<char*>(grad->data), flat ? 1 : (long long)grad->rows,
               (long long)grad->cols * es * (flat ? (long long)grad->rows : 1), (long long)grad->ld * es};
     }
-    constexpr int smem = (SORT_WARPS * SORT_BINS + SORT_BINS + 32 + 4) * (int)sizeof(uint32_t);
-    if (cudaFuncSetAttribute(k_sort_fill, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
-        return ISO_ERR_CUDA;
-    int fill_ctas = 0;
-    if (fa.base) {
-        const long long chunks = fa.rows * ((fa.width + FILL_CHUNK - 1) / FILL_CHUNK);
-        fill_ctas = (int)std::min((chunks + SORT_WARPS - 1) / SORT_WARPS, (long long)train_sms());
-        fill_ctas = (fill_ctas + SORT_CLUSTER - 1) / SORT_CLUSTER * SORT_CLUSTER;
-    }
-    TRAIN_LAUNCH((k_sort_fill<<<SORT_CLUSTER + fill_ctas, SORT_TPB, smem, s>>>(sa, fa)));
+    if (n <= SORT_ONE_CTA) ISO_TRY(launch_sort<1>(sa, s));
+    else ISO_TRY(launch_sort<SORT_CLUSTER>(sa, s));
+    if (fa.base) ISO_TRY(launch_fill(fa, s));
     if (n == 0 || grad->rows == 0 || grad->cols == 0) return ISO_OK;
 
     RowArgs ra;
@@ -481,17 +600,18 @@ int32_t iso_embed_grad(const iso_mat* dY, const void* ids, int32_t ids_i64, int6
     ra.ld_part = L.ld_part;
     ra.joins = reinterpret_cast<uint32_t*>(ws + L.joins);
     ra.n_joins = sa.n_joins;
-    const long long wins = (n + WIN - 1) / WIN;
-    const int sums_grid = (int)std::min((wins * ra.segs + EM_WPB - 1) / EM_WPB, (long long)train_sms() * 8);
-    const int join_grid = (int)std::min(wins * ((grad->cols + JOIN_COLS - 1) / JOIN_COLS), (long long)train_sms() * 2);
+    ra.win = L.win;
+    const long long wins = (n + L.win - 1) / L.win;
+    const int sums_grid = (int)std::min((wins * ra.segs + SUM_WPB - 1) / SUM_WPB, (long long)EXTENT_LIMIT);
+    const int join_grid = (int)std::min(wins * ((grad->cols + JOIN_COLS - 1) / JOIN_COLS), (long long)train_sms() * 16);
     return dispatch2(dY->dtype, grad->dtype, rows_aligned(dY) && rows_aligned(grad), [&](auto* tp, auto* op, auto v) -> int {
         using T = std::remove_pointer_t<decltype(tp)>;
         using O = std::remove_pointer_t<decltype(op)>;
         constexpr bool VEC = decltype(v)::value;
-        TRAIN_LAUNCH((k_row_sums<T, O, VEC><<<sums_grid, EM_TPB, 0, s>>>(
+        TRAIN_LAUNCH((k_row_sums<T, O, VEC><<<sums_grid, SUM_TPB, 0, s>>>(
             static_cast<const T*>(dY->data), dY->ld, static_cast<O*>(grad->data), grad->ld, ra)));
         if (wins > 1)
-            TRAIN_LAUNCH((k_row_join<O, VEC><<<join_grid, JOIN_TPB, 0, s>>>(static_cast<O*>(grad->data), grad->ld, ra)));
+            TRAIN_LAUNCH((k_row_join<O><<<join_grid, JOIN_TPB, 0, s>>>(static_cast<O*>(grad->data), grad->ld, ra)));
         return ISO_OK;
     });
 }

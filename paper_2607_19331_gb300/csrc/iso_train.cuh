@@ -181,45 +181,119 @@ __device__ __forceinline__ void store8(float* row, int c, int cols, const float 
 // Exponent byte of a group whose largest magnitude has the binary32 bits
 // `amax`.  With amax = 1.f 2^(E - 127), amax <= 127 2^e = 1.984375 2^(e + 6)
 // holds for e = E - 133 when 1.f <= 1.984375 (mantissa bits <= 0x7E0000) and
-// for e = E - 132 otherwise; the byte is e + 127, at least 1 (e = -126).
+// for e = E - 132 otherwise, where adding 0x1FFFF carries into the exponent;
+// the byte is e + 127, at least 1 (e = -126).
 __device__ __forceinline__ uint32_t act_exp_byte(uint32_t amax) {
-    if (amax >= 0x7F800000u) return 255u;   // a NaN or an infinity in the group
-    const int b = (int)(amax >> 23) - 6 + ((amax & 0x7FFFFFu) > 0x7E0000u ? 1 : 0);
-    return (uint32_t)max(b, 1);
+    const int b = (int)((amax + 0x1FFFFu) >> 23) - 6;
+    return amax >= 0x7F800000u ? 255u : (uint32_t)max(b, 1);   // 255: a NaN or an infinity in the group
 }
 // 2^(b - 127) for b in 1 .. 254, +Inf for 255 (its codes are 0: 0 * Inf = NaN)
 __device__ __forceinline__ float act_scale(uint32_t b) { return __uint_as_float(b << 23); }
 
-// Codes of this lane's eight values; the group's four lanes (a multiple of
-// four lanes on) hold its 32 values.  Every lane of the warp calls it.
-__device__ __forceinline__ uint32_t act_encode(const float (&v)[8], uint2& codes) {
+// largest magnitude of eight values, as binary32 bits; any NaN counts as one
+__device__ __forceinline__ uint32_t abs_max8(const float (&v)[8]) {
     uint32_t a = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    return a;
+}
+// the four lanes of a group; every lane of the warp calls it
+__device__ __forceinline__ uint32_t group_max(uint32_t a) {
     a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
-    a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
-    const uint32_t b = act_exp_byte(a);
-    const float inv = __uint_as_float((254u - min(b, 253u)) << 23);   // 2^(127 - b), b <= 249 unless 255
+    return max(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
+}
+// the low bytes of four words, the first one lowest
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+// Codes of eight values under the exponent byte b.  x 2^(127 - b) is exact, so
+// adding 1.5 2^23 to it rounds it once, to the nearest integer with halves to
+// even, and leaves that integer in the sum's low byte.
+__device__ __forceinline__ uint2 act_codes(const float (&v)[8], uint32_t b) {
+    const float inv = __uint_as_float((254u - b) << 23);
     uint32_t q[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = (uint32_t)__float2int_rn(v[i] * inv) & 0xFFu;
+    for (int i = 0; i < 8; ++i) q[i] = __float_as_uint(__fmaf_rn(v[i], inv, 12582912.0f));
     if (b >= 249u) {   // 64 * 2^122 is no binary32 number; NaN and Inf groups hold zeros
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int c = min(max((int)(int8_t)q[i], -63), 63);
-            q[i] = b == 255u ? 0u : (uint32_t)c & 0xFFu;
-        }
+        for (int i = 0; i < 8; ++i) q[i] = b == 255u ? 0u : (uint32_t)min(max((int)(int8_t)q[i], -63), 63);
     }
-    codes.x = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
-    codes.y = q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24;
+    return make_uint2(low_bytes(q[0], q[1], q[2], q[3]), low_bytes(q[4], q[5], q[6], q[7]));
+}
+// Codes of this lane's eight values, of a group of four lanes; returns the
+// exponent byte.  Every lane of the warp calls it.
+__device__ __forceinline__ uint32_t act_encode(const float (&v)[8], uint2& codes) {
+    const uint32_t b = act_exp_byte(group_max(abs_max8(v)));
+    codes = act_codes(v, b);
     return b;
 }
+// Eight values.  A code's byte with its top bit flipped, under the exponent of
+// 2^23, is 2^23 + 128 + code: taking the offset off and scaling are both exact
+// (b = 255: 0 * Inf = NaN).
 __device__ __forceinline__ void act_decode(uint2 codes, uint32_t b, float (&v)[8]) {
     const float s = act_scale(b);
+    const uint32_t x = codes.x ^ 0x80808080u, y = codes.y ^ 0x80808080u;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        v[i] = (float)(int8_t)(codes.x >> (8 * i)) * s;
-        v[4 + i] = (float)(int8_t)(codes.y >> (8 * i)) * s;
+        v[i] = (__uint_as_float(__byte_perm(x, 0x4B000000u, 0x7440u + i)) - 8388736.0f) * s;
+        v[4 + i] = (__uint_as_float(__byte_perm(y, 0x4B000000u, 0x7440u + i)) - 8388736.0f) * s;
+    }
+}
+
+// eight entries of a row that starts on a 16-byte boundary, as loaded
+template <typename T> struct Raw8;
+template <> struct Raw8<__nv_bfloat16> {
+    uint4 w;
+    __device__ __forceinline__ void load_shared(const void* p) { w = *static_cast<const uint4*>(p); }
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { w = __ldcs(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        bf16x2_to_f32(w.x, v[0], v[1]);
+        bf16x2_to_f32(w.y, v[2], v[3]);
+        bf16x2_to_f32(w.z, v[4], v[5]);
+        bf16x2_to_f32(w.w, v[6], v[7]);
+    }
+    // magnitudes compared two by two: as for binary32, their bits order them, NaN above all
+    __device__ __forceinline__ uint32_t abs_max() const {
+        const uint32_t m = 0x7FFF7FFFu;
+        const uint32_t a = __vmaxu2(__vmaxu2(w.x & m, w.y & m), __vmaxu2(w.z & m, w.w & m));
+        return max(a & 0xFFFF0000u, a << 16);
+    }
+};
+template <> struct Raw8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load_shared(const void* p) {
+        a = static_cast<const float4*>(p)[0];
+        b = static_cast<const float4*>(p)[1];
+    }
+    __device__ __forceinline__ void load(const float* p) {
+        a = __ldcs(reinterpret_cast<const float4*>(p));
+        b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+    __device__ __forceinline__ uint32_t abs_max() const {
+        float v[8];
+        get(v);
+        return abs_max8(v);
+    }
+};
+
+__device__ __forceinline__ void put8(__nv_bfloat16* p, const float (&v)[8]) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(f32_to_bf16x2(v[0], v[1]), f32_to_bf16x2(v[2], v[3]),
+                                              f32_to_bf16x2(v[4], v[5]), f32_to_bf16x2(v[6], v[7]));
+}
+// 32 bytes in one store where they are aligned to that: two 16-byte ones write
+// half sectors
+__device__ __forceinline__ void put8(float* p, const float (&v)[8]) {
+    if ((reinterpret_cast<uintptr_t>(p) & 31u) == 0) {
+        asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                     :: "l"(p), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+                     : "memory");
+    } else {
+        reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
     }
 }
 
