@@ -141,31 +141,86 @@ __global__ void __launch_bounds__(ACT_TPB) k_act_pack(const T* x, long long ld, 
 }
 
 template <typename T, bool VEC>
+__device__ __forceinline__ void unpack_run(const ActView& in, int cols, T* out, long long ld, const Run& r, int lane) {
+    T* dst = out + r.row * ld + r.c;
+    const uint8_t* codes = in.codes + r.row * in.ld_codes + r.c;
+    const uint8_t* exps = in.exps + r.row * in.ld_exps + r.c / ISO_ACT_GROUP;
+    uint2 q[SEGS];
+    uint32_t b[SEGS];
+#pragma unroll
+    for (int k = 0; k < SEGS; ++k)
+        if (VEC && k < r.full) {
+            q[k] = __ldcs(reinterpret_cast<const uint2*>(codes + k * TRAIN_SEG));
+            b[k] = exps[k * (TRAIN_SEG / ISO_ACT_GROUP)];
+        }
+#pragma unroll
+    for (int k = 0; k < SEGS; ++k) {
+        float v[8];
+        if (VEC && k < r.full) {
+            act_decode(q[k], b[k], v);
+            put8(dst + k * TRAIN_SEG, v);
+        } else if (r.c - lane * 8 + k * TRAIN_SEG < cols) {
+            const int c = r.c + k * TRAIN_SEG;
+            act_load(in, r.row, c, cols, q[k], b[k]);
+            act_decode(q[k], b[k], v);
+            store8<VEC>(out + r.row * ld, c, cols, v);
+        }
+    }
+}
+
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(ACT_TPB) k_act_unpack(ActView in, int cols, T* out, long long ld, Items it) {
     ACT_FOR_RUNS {
         const Run r(it, i, lane, cols, VEC);
-        T* dst = out + r.row * ld + r.c;
-        const uint8_t* codes = in.codes + r.row * in.ld_codes + r.c;
-        const uint8_t* exps = in.exps + r.row * in.ld_exps + r.c / ISO_ACT_GROUP;
-        uint2 q[SEGS];
-        uint32_t b[SEGS];
+        unpack_run<T, VEC>(in, cols, out, ld, r, lane);
+    }
+}
+
+// The weight gradient's operands.  The first `unpack_blocks` blocks decode x;
+// the others write dY as bf16 parts with rows on 16-byte boundaries.  Parts of
+// a binary32 value are its leading eight significant bits, cut off (not
+// rounded, so that none overflows), then those of the remainder, twice: 24
+// bits in all.  A NaN or an infinity stays in the first part.
+struct PartsArgs {
+    const void* dy;
+    long long ldd_in;
+    int cols;
+    __nv_bfloat16* out;
+    long long ldd, part_stride, n;     // n: pieces of eight channels, `segs` a row
+    int segs;
+};
+template <typename T>
+__global__ void __launch_bounds__(ACT_TPB) k_wgrad_operands(ActView in, int cols, __nv_bfloat16* x, long long ldx,
+                                                            Items it, unsigned unpack_blocks, PartsArgs p) {
+    const int lane = threadIdx.x & 31;
+    if (blockIdx.x < unpack_blocks) {
+        for (long long i = (long long)blockIdx.x * ACT_WPB + (threadIdx.x >> 5); i < it.n; i += (long long)unpack_blocks * ACT_WPB) {
+            const Run r(it, i, lane, cols, true);
+            unpack_run<__nv_bfloat16, true>(in, cols, x, ldx, r, lane);
+        }
+        return;
+    }
+    const long long threads = (long long)(gridDim.x - unpack_blocks) * ACT_TPB;
+    for (long long i = (long long)(blockIdx.x - unpack_blocks) * ACT_TPB + threadIdx.x; i < p.n; i += threads) {
+        const long long t = i / p.segs;
+        const int c = (int)(i - t * p.segs) * 8;
+        float v[8];
+        load8<false>(static_cast<const T*>(p.dy) + t * p.ldd_in, c, p.cols, v);
+        __nv_bfloat16* o = p.out + t * p.ldd + c;
+        if constexpr (sizeof(T) == 2) {
+            put8(o, v);
+        } else {
 #pragma unroll
-        for (int k = 0; k < SEGS; ++k)
-            if (VEC && k < r.full) {
-                q[k] = __ldcs(reinterpret_cast<const uint2*>(codes + k * TRAIN_SEG));
-                b[k] = exps[k * (TRAIN_SEG / ISO_ACT_GROUP)];
-            }
+            for (int q = 0; q < WGRAD_PARTS; ++q) {
+                float hi[8];
 #pragma unroll
-        for (int k = 0; k < SEGS; ++k) {
-            float v[8];
-            if (VEC && k < r.full) {
-                act_decode(q[k], b[k], v);
-                put8(dst + k * TRAIN_SEG, v);
-            } else if (r.c - lane * 8 + k * TRAIN_SEG < cols) {
-                const int c = r.c + k * TRAIN_SEG;
-                act_load(in, r.row, c, cols, q[k], b[k]);
-                act_decode(q[k], b[k], v);
-                store8<false>(out + r.row * ld, c, cols, v);
+                for (int j = 0; j < 8; ++j) {
+                    uint32_t b = __float_as_uint(v[j]);
+                    if ((b & 0x7FFFFFFFu) > 0x7F800000u) b |= 0x400000u;     // a NaN stays one without its low bits
+                    hi[j] = __uint_as_float(b & 0xFFFF0000u);
+                    v[j] = (b & 0x7F800000u) == 0x7F800000u ? 0.0f : v[j] - hi[j];
+                }
+                put8(o + q * p.part_stride, hi);
             }
         }
     }
@@ -318,6 +373,30 @@ Items items_of(int64_t rows, int64_t cols) {
 unsigned act_grid(const Items& it) {
     return (unsigned)std::min((it.n + ACT_WPB - 1) / ACT_WPB, (long long)EXTENT_LIMIT);
 }
+
+}  // namespace
+
+int launch_wgrad_operands(const iso_act* pack, __nv_bfloat16* x, long long ldx, const iso_mat* dy,
+                          __nv_bfloat16* parts, long long ldd, cudaStream_t s) {
+    const Items it = items_of(pack->rows, pack->cols);
+    const unsigned unpack_blocks = std::min(act_grid(it), 1u << 30);
+    PartsArgs p{};
+    unsigned part_blocks = 0;
+    if (dy) {
+        const int segs = (int)((dy->cols + 7) / 8);
+        p = {dy->data, (long long)dy->ld, (int)dy->cols, parts, ldd, (long long)dy->rows * ldd, (long long)dy->rows * segs, segs};
+        part_blocks = (unsigned)std::min((p.n + ACT_TPB - 1) / ACT_TPB, 1LL << 30);
+    }
+    if (dy && dy->dtype == ISO_F32)
+        TRAIN_LAUNCH((k_wgrad_operands<float><<<unpack_blocks + part_blocks, ACT_TPB, 0, s>>>(
+            view(pack), (int)pack->cols, x, ldx, it, unpack_blocks, p)));
+    else
+        TRAIN_LAUNCH((k_wgrad_operands<__nv_bfloat16><<<unpack_blocks + part_blocks, ACT_TPB, 0, s>>>(
+            view(pack), (int)pack->cols, x, ldx, it, unpack_blocks, p)));
+    return ISO_OK;
+}
+
+namespace {
 
 template <typename F>
 int dispatch_act(int32_t dtype, bool vec, F&& f) {

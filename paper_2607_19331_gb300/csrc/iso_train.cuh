@@ -104,6 +104,13 @@ inline bool rows_aligned(const iso_mat* m) {
 // SMs of the current device (queried once per device)
 int train_sms();
 
+// The weight gradient's bf16 operands, in one kernel (iso_act.cu): x (rows of
+// ldx) <- the values of pack; with dy, parts (WGRAD_PARTS or 1 matrices of
+// rows x ldd) <- dY.  ldx and ldd are multiples of 8.
+constexpr int WGRAD_PARTS = 3;
+int launch_wgrad_operands(const iso_act* pack, __nv_bfloat16* x, long long ldx, const iso_mat* dy,
+                          __nv_bfloat16* parts, long long ldd, cudaStream_t s);
+
 // ---------------------------------------------------------------------------
 // device: rows, eight elements at a time
 // ---------------------------------------------------------------------------

@@ -40,21 +40,41 @@ namespace iso {
 namespace {
 
 constexpr int WG_BM = 256;                 // rows of G (dY channels) per CTA pair
-constexpr int WG_BN = 256;                 // columns of G (X channels) per CTA pair
 constexpr int WG_BK = 128;                 // tokens per stage
-constexpr int WG_STAGES = 3;
 constexpr int WG_BOX = 64;                 // channels of one copy: 128 bytes, the swizzle's row
 constexpr int WG_BOX_BYTES = WG_BOX * WG_BK * 2;
-constexpr int WG_OP_BYTES = 2 * WG_BOX_BYTES;          // 128 channels of an operand: this CTA's half
-constexpr int WG_STAGE_BYTES = 2 * WG_OP_BYTES;
+constexpr int WG_A_BYTES = 2 * WG_BOX_BYTES;           // 128 channels of dY: this CTA's half of a stage
 constexpr int WG_EPI_WARPS = 8;
 constexpr int WG_OUT_BYTES = 32 * 32 * 4;  // an epilogue warp's 32 x 32 block on its way out
-constexpr int WG_SMEM = 1024 + WG_STAGES * WG_STAGE_BYTES + WG_EPI_WARPS * WG_OUT_BYTES + 256;
-static_assert(WG_SMEM <= 232448, "shared memory of one CTA");
+// What depends on BN, the columns of G (X channels) per CTA pair
+template <int BN>
+struct WgTile {
+    static constexpr int B_BOXES = BN / 2 / WG_BOX;        // this CTA's half of X
+    static constexpr int STAGE_BYTES = WG_A_BYTES + B_BOXES * WG_BOX_BYTES;
+    static constexpr int STAGES = BN == 256 ? 3 : 4;
+    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + WG_EPI_WARPS * WG_OUT_BYTES + 256;
+    static constexpr int TMEM_COLS = 2 * BN;               // two accumulators
+    static constexpr int BLOCKS = BN / 64;                 // 32-column blocks of an epilogue warp: half the columns
+    // kind::f16, fp32 accumulator, bf16 A and B, both MN-major, M = 256 over the pair, N = BN
+    static constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) |
+                                      ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(WG_BM >> 4) << 24);
+    static_assert(SMEM <= 232448, "shared memory of one CTA");
+};
 constexpr int WG_THREADS = (WG_EPI_WARPS + 2) * 32;    // epilogue warps, a copy warp, a product warp
-constexpr int WG_MAX_PARTS = 3;
-constexpr int WG_MAX_SPLIT = 8;
+constexpr int WG_MAX_PARTS = WGRAD_PARTS;
+constexpr int WG_MAX_SPLIT = 32;
 constexpr int WG_CHAIN = 8;                // steps accumulated in tensor memory before they are added in registers
+// the plan's estimates, in clocks: a step of either tile width, an item's start
+// and end, a join's launch and its bytes per clock
+constexpr long long WG_STEP_256 = 1250, WG_STEP_128 = 860, WG_ITEM = 4000, WG_JOIN = 4000, WG_JOIN_BYTES = 4100;
+// Up to WG_FEW tokens and WG_FEW_WORK multiply-adds take k_wgrad_few.  Measured,
+// it against k_wgrad with its operands' kernel: 1 token, G 18944 x 3584 f32 40 / 59
+// us, 300 x 200 2.7 / 7.9 us; 16 tokens, 3000 x 1000 9.3 / 13.4 us; 8 tokens,
+// 18944 x 3584 74 / 59 us; 32 tokens, 3000 x 1000 14.9 / 12.6 us.
+constexpr int WG_FEW = 16;
+constexpr long long WG_FEW_WORK = 1LL << 28;
+constexpr int FEW_TPB = 128, FEW_WARPS = FEW_TPB / 32, FEW_ROWS = 8;
+constexpr int WG_SPLIT_STEPS = 4;          // a part of the tokens has this many steps at least
 constexpr int WG_BAND = 8;                 // tile rows that are walked together
 
 struct WgradArgs {
@@ -68,12 +88,12 @@ struct WgradArgs {
     long long ldo;
     int32_t out_dtype;
     int32_t out_vec;       // rows of G start on 16-byte boundaries
-    float* part;           // split > 1: [split][M][ld_part]
-    long long ld_part;
+    int32_t out_copy;      // blocks leave by bulk copies (maps.out): rows so aligned, nothing to add to
     int32_t* status;
 };
 struct WgradMaps {
     CUtensorMap a[WG_MAX_PARTS], b;
+    CUtensorMap out;       // G, or the parts of the contraction: columns, rows, part
 };
 
 // Shared-memory descriptor of an MN-major operand in the 128-byte swizzle:
@@ -84,11 +104,6 @@ struct WgradMaps {
 constexpr uint32_t WG_DESC_LO = (uint32_t)(WG_BOX_BYTES >> 4) << 16;                    // leading offset: 64 channels on
 constexpr uint32_t WG_DESC_HI = (1024u >> 4) | 1u << 14 | 2u << 29;                     // stride offset: eight tokens on
 __device__ __forceinline__ uint32_t mn_desc_lo(uint32_t saddr) { return WG_DESC_LO + (saddr >> 4); }
-
-// kind::f16, fp32 accumulator, bf16 A and B, both MN-major, M = 256 over the
-// pair, N = 256
-constexpr uint32_t WG_IDESC = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) |
-                              ((uint32_t)(WG_BN >> 3) << 17) | ((uint32_t)(WG_BM >> 4) << 24);
 
 __device__ __forceinline__ uint32_t cta_rank() {
     uint32_t r;
@@ -110,11 +125,12 @@ __device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* m
                  " [%0], [%1, {%2, %3}], [%4];"
                  :: "r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar) : "memory");
 }
+template <uint32_t IDESC>
 __device__ __forceinline__ void umma_bf16_pair(uint32_t tmem_d, uint32_t a_lo, uint32_t b_lo, uint32_t accumulate) {
     asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\t"
                  "mov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
                  "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %4, p;\n\t}"
-                 :: "r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(WG_DESC_HI), "r"(WG_IDESC), "r"(accumulate) : "memory");
+                 :: "r"(tmem_d), "r"(a_lo), "r"(b_lo), "r"(WG_DESC_HI), "r"(IDESC), "r"(accumulate) : "memory");
 }
 // arrive on this barrier in both CTAs once the products issued so far are done
 __device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
@@ -140,34 +156,41 @@ __device__ __forceinline__ bool wait_pair(uint32_t bar, uint32_t parity, volatil
     *abort_flag = 1;
     return false;
 }
-// 16 consecutive columns of this thread's accumulator row
-__device__ __forceinline__ void tmem_load16(uint32_t taddr, float (&v)[16]) {
-    uint32_t r[16];
+// 16 consecutive columns of this thread's accumulator row; the values may be
+// used after the wait below, which takes them as operands so that no use is
+// moved before it
+__device__ __forceinline__ void tmem_load(uint32_t taddr, float (&v)[16]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
                  "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-                   "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-                   "=r"(r[14]), "=r"(r[15])
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]),
+                   "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]),
+                   "=f"(v[14]), "=f"(v[15])
                  : "r"(taddr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int j = 0; j < 16; ++j) v[j] = __uint_as_float(r[j]);
+}
+__device__ __forceinline__ void tmem_wait(float (&v)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]),
+                   "+f"(v[7]), "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]),
+                   "+f"(v[14]), "+f"(v[15])
+                 :: "memory");
 }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-// A warp's 32 x 32 block of G: lane l holds row l.  Through shared memory
-// (16-byte words swizzled by row), so that a store covers whole runs of a row:
-// one row by 16-byte words of eight (f32) or four (bf16) lanes where G's rows
-// start on 16-byte boundaries, else a row's 32 columns by the 32 lanes.
-template <typename O>
-__device__ __forceinline__ void store_block(float4* buf, const float (&v)[32], int lane, O* out, long long ldo, int m,
-                                            int n, int M, int N, bool vec, int accumulate) {
-    __syncwarp();
+// A warp's 32 x 32 block of G: lane l holds row l.  Into shared memory, rows of
+// 128 bytes, their 16-byte words swizzled by row (no bank is hit twice, and a
+// bulk copy with the 128-byte swizzle reads it).
+__device__ __forceinline__ void stage_block(float4* buf, const float (&v)[32], int lane) {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
         buf[lane * 8 + (j ^ (lane & 7))] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-    __syncwarp();
+}
+// The staged block to G where bulk copies cannot: a store covers whole runs of
+// a row, 16-byte words of eight (f32) or four (bf16) lanes where G's rows
+// start on 16-byte boundaries, else a row's 32 columns by the 32 lanes.
+template <typename O>
+__device__ __forceinline__ void store_block(const float4* buf, int lane, O* out, long long ldo, int m, int n, int M, int N,
+                                         bool vec, int accumulate) {
     const int rows = min(32, M - m);
     if (vec && n + 32 <= N) {
         if constexpr (sizeof(O) == 4) {
@@ -211,39 +234,53 @@ __device__ __forceinline__ void store_block(float4* buf, const float (&v)[32], i
     }
 }
 
+// The warp's block out of shared memory by a bulk copy, clipped at G's edges
+__device__ __forceinline__ void copy_out(const CUtensorMap* map, uint32_t src, int n, int m, int part) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];"
+                 :: "l"(reinterpret_cast<uint64_t>(map)), "r"(n), "r"(m), "r"(part), "r"(src) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// the buffer of the copies so far may be written again
+__device__ __forceinline__ void copies_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
 // Work item i: a part of the contraction of one tile; tiles in bands of
 // WG_BAND tile rows, column by column inside a band, so that the pairs that
 // run together share their operands' rows in L2.
+template <int BN>
 __device__ __forceinline__ void work_item(const WgradArgs& g, int i, int& m0, int& n0, int& k0, int& k1, int& part) {
     const int tile = i / g.split;
     part = i - tile * g.split;
     const int band = tile / (WG_BAND * g.n_tiles), in = tile - band * WG_BAND * g.n_tiles;
     const int rows = min(WG_BAND, g.m_tiles - band * WG_BAND);
     m0 = (band * WG_BAND + in % rows) * WG_BM;
-    n0 = in / rows * WG_BN;
+    n0 = in / rows * BN;
     k0 = (int)((long long)g.k_tiles * part / g.split);
     k1 = (int)((long long)g.k_tiles * (part + 1) / g.split);
 }
 
+template <int BN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(WG_THREADS, 1)
 k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
+    using Tile = WgTile<BN>;
+    constexpr int STAGES = Tile::STAGES, STAGE_BYTES = Tile::STAGE_BYTES;
     extern __shared__ unsigned char wg_smem_raw[];
     unsigned char* const smem =
         reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(wg_smem_raw) + 1023) & ~(uintptr_t)1023);
     uint64_t* const bars =
-        reinterpret_cast<uint64_t*>(smem + WG_STAGES * WG_STAGE_BYTES + WG_EPI_WARPS * WG_OUT_BYTES);
-    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * WG_STAGES + 4);
+        reinterpret_cast<uint64_t*>(smem + STAGES * STAGE_BYTES + WG_EPI_WARPS * WG_OUT_BYTES);
+    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 4);
     volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cta_rank();
     const uint32_t st = smem_u32(smem), bar = smem_u32(bars);
     auto full = [&](int s) { return bar + 8u * s; };                          // leader: both CTAs' copies landed
-    auto empty = [&](int s) { return bar + 8u * (WG_STAGES + s); };           // products that read the stage are done
-    auto acc_full = [&](int a) { return bar + 8u * (2 * WG_STAGES + a); };    // accumulator complete
-    auto acc_empty = [&](int a) { return bar + 8u * (2 * WG_STAGES + 2 + a); };   // leader: accumulator read by all
+    auto empty = [&](int s) { return bar + 8u * (STAGES + s); };           // products that read the stage are done
+    auto acc_full = [&](int a) { return bar + 8u * (2 * STAGES + a); };    // accumulator complete
+    auto acc_empty = [&](int a) { return bar + 8u * (2 * STAGES + 2 + a); };   // leader: accumulator read by all
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < WG_STAGES; ++s) {
+        for (int s = 0; s < STAGES; ++s) {
             mbar_init(full(s), 1);
             mbar_init(empty(s), 1);
         }
@@ -256,7 +293,7 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
     }
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
-                     :: "r"(smem_u32(tmem_slot)), "r"(512) : "memory");
+                     :: "r"(smem_u32(tmem_slot)), "r"(Tile::TMEM_COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     tc_before();
@@ -264,66 +301,68 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
     cluster_barrier();
     tc_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(tmem_slot);
+    asm volatile("griddepcontrol.wait;" ::: "memory");     // the operands are written by the kernel before
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const int items = g.m_tiles * g.n_tiles * g.split;
 
     if (warp == WG_EPI_WARPS && lane == 0) {
         // copies: this CTA's 128 channels of either operand
-        const uint32_t full0 = in_leader(full(0)), own = rank * 128;
+        const uint32_t full0 = in_leader(full(0));
         uint32_t s = 0, ph = 1, done = 0;            // stage, its parity, copies issued
         bool ok = true;
         for (int i = pair; ok && i < items; i += pairs) {
             int m0, n0, k0, k1, part;
-            work_item(g, i, m0, n0, k0, k1, part);
-            m0 += own;
-            n0 += own;
+            work_item<BN>(g, i, m0, n0, k0, k1, part);
+            m0 += (int)rank * 128;
+            n0 += (int)rank * (BN / 2);
             int p = k0 / g.t_tiles, t = (k0 - p * g.t_tiles) * WG_BK;
             for (int k = k0; k < k1; ++k) {
                 if (!wait_pair(empty(s), ph, abort_flag)) { ok = false; break; }
-                if (rank == 0) mbar_arrive_tx(full(s), 2 * WG_STAGE_BYTES);
+                if (rank == 0) mbar_arrive_tx(full(s), 2 * STAGE_BYTES);
                 const CUtensorMap* am = &maps.a[p];
-                const uint32_t fb = full0 + 8u * s, a = st + s * WG_STAGE_BYTES, b = a + WG_OP_BYTES;
+                const uint32_t fb = full0 + 8u * s, a = st + s * STAGE_BYTES, b = a + WG_A_BYTES;
                 tma_load_pair(a, am, m0, t, fb);
                 tma_load_pair(a + WG_BOX_BYTES, am, m0 + WG_BOX, t, fb);
-                tma_load_pair(b, &maps.b, n0, t, fb);
-                tma_load_pair(b + WG_BOX_BYTES, &maps.b, n0 + WG_BOX, t, fb);
+#pragma unroll
+                for (int q = 0; q < Tile::B_BOXES; ++q)
+                    tma_load_pair(b + q * WG_BOX_BYTES, &maps.b, n0 + q * WG_BOX, t, fb);
                 if ((t += WG_BK) >= g.t_tiles * WG_BK) { t = 0; ++p; }
-                if (++s == WG_STAGES) { s = 0; ph ^= 1u; }
+                if (++s == STAGES) { s = 0; ph ^= 1u; }
                 ++done;
             }
         }
         // every copy into this CTA has been consumed before it may exit: the
         // products that read a stage free it in both CTAs
-        for (uint32_t q = 0; q < min(done, (uint32_t)WG_STAGES); ++q) {
-            if (s == 0) { s = WG_STAGES; ph ^= 1u; }
+        for (uint32_t q = 0; q < min(done, (uint32_t)STAGES); ++q) {
+            if (s == 0) { s = STAGES; ph ^= 1u; }
             --s;
             for (int spin = 0; spin < MBAR_SPIN_LIMIT; ++spin)
                 if (try_wait_cluster(empty(s), ph ^ 1u) || *abort_flag) break;
         }
     } else if (warp == WG_EPI_WARPS + 1 && lane == 0 && rank == 0) {
         // products of the pair, chain by chain
-        const uint32_t a0 = mn_desc_lo(st), b0 = mn_desc_lo(st + WG_OP_BYTES);
+        const uint32_t a0 = mn_desc_lo(st), b0 = mn_desc_lo(st + WG_A_BYTES);
         uint32_t s = 0, ph = 0, acc = 0, acc_ph = 1;
         bool ok = true;
         for (int i = pair; ok && i < items; i += pairs) {
             int m0, n0, k0, k1, part;
-            work_item(g, i, m0, n0, k0, k1, part);
+            work_item<BN>(g, i, m0, n0, k0, k1, part);
             for (int kc = k0; ok && kc < k1; kc += WG_CHAIN) {
                 if (!wait_pair(acc_empty(acc), acc_ph, abort_flag)) { ok = false; break; }
                 tc_after();
-                const uint32_t d = tmem + acc * WG_BN;
+                const uint32_t d = tmem + acc * BN;
                 uint32_t more = 0;
                 for (int k = min(k1 - kc, WG_CHAIN); k > 0; --k) {
                     if (!wait_pair(full(s), ph, abort_flag)) { ok = false; break; }
                     tc_after();
-                    const uint32_t a = a0 + s * (WG_STAGE_BYTES >> 4), b = b0 + s * (WG_STAGE_BYTES >> 4);
+                    const uint32_t a = a0 + s * (STAGE_BYTES >> 4), b = b0 + s * (STAGE_BYTES >> 4);
 #pragma unroll
                     for (uint32_t q = 0; q < WG_BK / 16; ++q) {   // 16 tokens per product: two atoms of eight
-                        umma_bf16_pair(d, a + (2048u >> 4) * q, b + (2048u >> 4) * q, more);
+                        umma_bf16_pair<Tile::IDESC>(d, a + (2048u >> 4) * q, b + (2048u >> 4) * q, more);
                         more = 1;
                     }
                     umma_commit_pair(empty(s));
-                    if (++s == WG_STAGES) { s = 0; ph ^= 1u; }
+                    if (++s == STAGES) { s = 0; ph ^= 1u; }
                 }
                 umma_commit_pair(acc_full(acc));
                 acc ^= 1u;
@@ -331,17 +370,17 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
             }
         }
     } else if (warp < WG_EPI_WARPS) {
-        // epilogue: warp w reads tensor-memory lanes 32 (w mod 4) ..., 128 of the 256 columns
+        // epilogue: warp w reads tensor-memory lanes 32 (w mod 4) ..., half of the columns
         const int quad = warp & 3, half = warp >> 2;
-        float4* const buf = reinterpret_cast<float4*>(smem + WG_STAGES * WG_STAGE_BYTES + warp * WG_OUT_BYTES);
+        float4* const buf = reinterpret_cast<float4*>(smem + STAGES * STAGE_BYTES + warp * WG_OUT_BYTES);
         int n_acc = 0;
         bool ok = true;
         for (int i = pair; ok && i < items; i += pairs) {
             int m0, n0, k0, k1, part;
-            work_item(g, i, m0, n0, k0, k1, part);
-            float sum[4][32];
+            work_item<BN>(g, i, m0, n0, k0, k1, part);
+            float sum[Tile::BLOCKS][32];
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+            for (int c = 0; c < Tile::BLOCKS; ++c)
 #pragma unroll
                 for (int j = 0; j < 32; ++j) sum[c][j] = 0.0f;
             for (int kc = k0; kc < k1; kc += WG_CHAIN, ++n_acc) {
@@ -349,11 +388,14 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
                 if (!wait_pair(acc_full(acc), (uint32_t)(n_acc >> 1) & 1u, abort_flag)) { ok = false; break; }
                 __syncwarp();
                 tc_after();
-                const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * WG_BN + half * 128);
+                const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * BN + half * (BN / 2));
+                // 16 columns at a time: reading a chain's block in one go holds the next chain's
+                // products up (730 us against 590 for 18944 x 3584 over 8192 tokens)
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
+                for (int c = 0; c < 2 * Tile::BLOCKS; ++c) {
                     float v[16];
-                    tmem_load16(at + c * 16, v);
+                    tmem_load(at + c * 16, v);
+                    tmem_wait(v);
 #pragma unroll
                     for (int j = 0; j < 16; ++j) sum[c >> 1][(c & 1) * 16 + j] += v[j];
                 }
@@ -364,21 +406,51 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
             if (!ok) break;
             const int m = m0 + (int)rank * 128 + quad * 32;
             if (m >= g.M) continue;
+            if (g.out_copy) {
+                // 32 rows of 128 bytes, their 16-byte words swizzled by row as the copy expects them
+                const bool narrow = g.split == 1 && g.out_dtype == ISO_BF16;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const int n = n0 + half * 128 + c * 32;
+                for (int c = 0; c < Tile::BLOCKS; ++c) {
+                    const int n = n0 + half * (BN / 2) + c * 32;
+                    if (!narrow || (c & 1) == 0) {
+                        if (lane == 0) copies_read();
+                        __syncwarp();
+                    }
+                    if (narrow) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            reinterpret_cast<uint4*>(buf)[lane * 8 + (((c & 1) * 4 + j) ^ (lane & 7))] =
+                                make_uint4(f32_to_bf16x2(sum[c][8 * j], sum[c][8 * j + 1]),
+                                           f32_to_bf16x2(sum[c][8 * j + 2], sum[c][8 * j + 3]),
+                                           f32_to_bf16x2(sum[c][8 * j + 4], sum[c][8 * j + 5]),
+                                           f32_to_bf16x2(sum[c][8 * j + 6], sum[c][8 * j + 7]));
+                    } else {
+                        stage_block(buf, sum[c], lane);
+                    }
+                    if (!narrow || (c & 1) == 1) {
+                        const int first = narrow ? n - 32 : n;
+                        fence_async_shared();
+                        __syncwarp();
+                        if (lane == 0 && first < g.N) copy_out(&maps.out, smem_u32(buf), first, m, part);
+                    }
+                }
+                continue;
+            }
+#pragma unroll
+            for (int c = 0; c < Tile::BLOCKS; ++c) {
+                const int n = n0 + half * (BN / 2) + c * 32;
+                __syncwarp();
+                stage_block(buf, sum[c], lane);
+                __syncwarp();
                 if (n >= g.N) continue;
-                if (g.part)
-                    store_block(buf, sum[c], lane, g.part + (long long)part * g.M * g.ld_part, g.ld_part, m, n, g.M,
-                                g.N, true, 0);
-                else if (g.out_dtype == ISO_BF16)
-                    store_block(buf, sum[c], lane, static_cast<__nv_bfloat16*>(g.out), g.ldo, m, n, g.M, g.N,
-                                g.out_vec, g.accumulate);
-                else
-                    store_block(buf, sum[c], lane, static_cast<float*>(g.out), g.ldo, m, n, g.M, g.N, g.out_vec,
+                if (g.out_dtype == ISO_BF16)
+                    store_block(buf, lane, static_cast<__nv_bfloat16*>(g.out), g.ldo, m, n, g.M, g.N, g.out_vec,
                                 g.accumulate);
+                else
+                    store_block(buf, lane, static_cast<float*>(g.out), g.ldo, m, n, g.M, g.N, g.out_vec, g.accumulate);
             }
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
     tc_before();
@@ -387,7 +459,65 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
     if (threadIdx.x == 0 && *abort_flag && g.status) atomicCAS(g.status, 0, (int32_t)ISO_ERR_TIMEOUT);
     if (warp == 0) {
         tc_after();
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(512) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(Tile::TMEM_COLS) : "memory");
+    }
+}
+
+// Few tokens: the tensor cores' fixed costs (the operands' kernel, a step of 128
+// tokens, the accumulator's way out) outweigh the products.  Here a warp holds
+// FEW_ROWS x 256 of G in registers and adds token by token, decoding X on the
+// way; dY's values of the block are staged in shared memory.
+template <typename T, typename O, bool VEC>
+__global__ void __launch_bounds__(FEW_TPB) k_wgrad_few(const T* dy, long long ldd, const uint8_t* codes, long long ldc,
+                                                       const uint8_t* exps, long long lde, O* out, long long ldo,
+                                                       int tokens, int M, int N, int m_blocks, int accumulate) {
+    constexpr int ROWS = FEW_WARPS * FEW_ROWS;
+    __shared__ __align__(16) float d[WG_FEW][ROWS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int nb = blockIdx.x / m_blocks, mb = blockIdx.x - nb * m_blocks;
+    const int c = nb * TRAIN_SEG + lane * 8;
+    for (int i = threadIdx.x; i < tokens * ROWS; i += FEW_TPB) {
+        const int t = i / ROWS, m = mb * ROWS + i % ROWS;
+        d[t][i % ROWS] = m < M ? to_f32(dy[t * ldd + m]) : 0.0f;
+    }
+    __syncthreads();
+    float acc[FEW_ROWS][8] = {};
+#pragma unroll 2
+    for (int t = 0; t < tokens; ++t) {
+        uint2 q = make_uint2(0u, 0u);
+        uint32_t b = 1;
+        if (c < N) {   // codes are padded to whole groups of 32 channels
+            q = *reinterpret_cast<const uint2*>(codes + t * ldc + c);
+            b = exps[t * lde + c / ISO_ACT_GROUP];
+        }
+        float x[8];
+        act_decode(q, b, x);
+#pragma unroll
+        for (int r = 0; r < FEW_ROWS; r += 4) {
+            const float4 w = *reinterpret_cast<const float4*>(&d[t][warp * FEW_ROWS + r]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                acc[r][j] = fmaf(w.x, x[j], acc[r][j]);
+                acc[r + 1][j] = fmaf(w.y, x[j], acc[r + 1][j]);
+                acc[r + 2][j] = fmaf(w.z, x[j], acc[r + 2][j]);
+                acc[r + 3][j] = fmaf(w.w, x[j], acc[r + 3][j]);
+            }
+        }
+    }
+    const int m0 = mb * ROWS + warp * FEW_ROWS;
+    if (c >= N) return;
+#pragma unroll
+    for (int r = 0; r < FEW_ROWS; ++r) {
+        if (m0 + r >= M) break;
+        O* row = out + (long long)(m0 + r) * ldo;
+        if (accumulate) {
+            float old[8];
+            load8<VEC>(row, c, N, old);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[r][j] += old[j];
+        }
+        if (VEC && c + 8 <= N) put8(row + c, acc[r]);
+        else store8<false>(row, c, N, acc[r]);
     }
 }
 
@@ -415,40 +545,6 @@ __global__ void __launch_bounds__(256) k_wgrad_join(const float* part, long long
             for (int j = 0; j < 8; ++j) s[j] += old[j];
         }
         store8<VEC>(o, c, N, s);
-    }
-}
-
-// dY as bf16 parts with rows on 16-byte boundaries.  Parts of a binary32
-// value are its leading eight significant bits, cut off (not rounded, so that
-// none overflows), then those of the remainder, twice: 24 bits in all.  A NaN
-// or an infinity stays in the first part.
-template <typename T>
-__global__ void __launch_bounds__(256) k_wgrad_parts(const T* dy, long long ldd, int tokens, int M,
-                                                     __nv_bfloat16* out, long long ldo, long long part_stride) {
-    const int segs = (M + 7) / 8;
-    const long long n = (long long)tokens * segs;
-    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
-        const long long t = i / segs;
-        const int c = (int)(i - t * segs) * 8;
-        float v[8];
-        load8<false>(dy + t * ldd, c, M, v);
-        __nv_bfloat16* o = out + t * ldo;
-        if constexpr (sizeof(T) == 2) {
-            store8<true>(o, c, (int)ldo, v);
-        } else {
-#pragma unroll
-            for (int p = 0; p < WG_MAX_PARTS; ++p) {
-                float hi[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    uint32_t b = __float_as_uint(v[j]);
-                    if ((b & 0x7FFFFFFFu) > 0x7F800000u) b |= 0x400000u;     // a NaN stays one without its low bits
-                    hi[j] = __uint_as_float(b & 0xFFFF0000u);
-                    v[j] = (b & 0x7F800000u) == 0x7F800000u ? 0.0f : v[j] - hi[j];
-                }
-                store8<true>(o + p * part_stride, c, (int)ldo, hi);
-            }
-        }
     }
 }
 
@@ -482,6 +578,22 @@ int bf16_map(CUtensorMap* map, const void* base, long long rows, long long cols,
                : ISO_ERR_CUDA;
 }
 
+// G or its parts: cols, rows, parts; blocks of 32 rows of 128 bytes
+int out_map(CUtensorMap* map, void* base, int32_t dtype, long long rows, long long cols, long long ld, int parts) {
+    EncodeTiled fn = encode_tiled();
+    if (!fn) return ISO_ERR_CUDA;
+    const long long es = elem_size(dtype);
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)parts};
+    const cuuint64_t strides[2] = {(cuuint64_t)(ld * es), (cuuint64_t)(rows * ld * es)};
+    const cuuint32_t box[3] = {(cuuint32_t)(128 / es), 32, 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, dtype == ISO_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, base, dims,
+              strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? ISO_OK
+               : ISO_ERR_CUDA;
+}
+
 int check_wgrad(const iso_mat* dY, const iso_act* pack, const iso_mat* out) {
     ISO_TRY(check_mat(dY));
     ISO_TRY(check_act(pack));
@@ -491,16 +603,18 @@ int check_wgrad(const iso_mat* dY, const iso_act* pack, const iso_mat* out) {
 }
 
 // the pairs of CTAs that run at once on the current device
+template <int BN>
 int resident_pairs() {
     static int pairs[64] = {};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
     if (!pairs[dev]) {
-        if (cudaFuncSetAttribute(k_wgrad, cudaFuncAttributeMaxDynamicSharedMemorySize, WG_SMEM) != cudaSuccess) return 0;
+        if (cudaFuncSetAttribute(k_wgrad<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, WgTile<BN>::SMEM) != cudaSuccess)
+            return 0;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)(train_sms() / 2 * 2));
         cfg.blockDim = dim3(WG_THREADS);
-        cfg.dynamicSmemBytes = WG_SMEM;
+        cfg.dynamicSmemBytes = WgTile<BN>::SMEM;
         cudaLaunchAttribute at;
         at.id = cudaLaunchAttributeClusterDimension;
         at.val.clusterDim.x = 2;
@@ -508,32 +622,73 @@ int resident_pairs() {
         cfg.attrs = &at;
         cfg.numAttrs = 1;
         int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, k_wgrad, &cfg) != cudaSuccess || n <= 0) return 0;
+        if (cudaOccupancyMaxActiveClusters(&n, k_wgrad<BN>, &cfg) != cudaSuccess || n <= 0) return 0;
         pairs[dev] = n;
     }
     return pairs[dev];
 }
 
+// The product; it may be set up while the operands' kernel ends, and waits for it.
+template <int BN>
+int launch_wgrad(const WgradMaps& maps, const WgradArgs& g, int items, cudaStream_t s) {
+    const int pairs = resident_pairs<BN>();
+    if (pairs <= 0) return ISO_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(2 * std::min(items, pairs)));
+    cfg.blockDim = dim3(WG_THREADS);
+    cfg.dynamicSmemBytes = WgTile<BN>::SMEM;
+    cfg.stream = s;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    TRAIN_LAUNCH(cudaLaunchKernelEx(&cfg, k_wgrad<BN>, maps, g));
+    return ISO_OK;
+}
+
+bool few_tokens(long long T, long long M, long long N) {
+    return T <= WG_FEW && (long double)T * M * N <= (long double)WG_FEW_WORK;
+}
+
 struct WgradPlan {
     size_t x_bf16, dy_parts, parts, end;
     long long ldx, ldd, ld_part;
-    int m_tiles, n_tiles, k_tiles, split, n_parts;
+    int bn, m_tiles, n_tiles, k_tiles, split, n_parts;
     bool dy_direct;
 };
 // Host only, the same for the sizing call and the launch (the pair count of a
 // GB300 stands in where there is no device).
 WgradPlan plan_wgrad(const iso_mat* dY, const iso_act* pack, const iso_mat* out) {
     auto up = [](size_t b) { return (b + 255) & ~(size_t)255; };
-    WgradPlan p;
+    WgradPlan p{};
     const long long T = dY->rows, M = out->rows, N = out->cols;
+    if (few_tokens(T, M, N)) {
+        p.end = 256;
+        return p;
+    }
     p.n_parts = dY->dtype == ISO_F32 ? 3 : 1;
     p.dy_direct = dY->dtype == ISO_BF16 && (reinterpret_cast<uintptr_t>(dY->data) & 15u) == 0 && dY->ld % 8 == 0;
     p.m_tiles = (int)((M + WG_BM - 1) / WG_BM);
-    p.n_tiles = (int)((N + WG_BN - 1) / WG_BN);
     p.k_tiles = (int)((T + WG_BK - 1) / WG_BK) * p.n_parts;
-    const long long tiles = (long long)p.m_tiles * p.n_tiles, pairs = std::max(1, train_sms() / 2);
-    // cut the tokens where the tiles leave half the pairs idle, four steps a part at least
-    p.split = (int)std::max(1LL, std::min({pairs / std::max(1LL, tiles), (long long)p.k_tiles / 4, (long long)WG_MAX_SPLIT}));
+    // Tile width and token split by the estimated time of the longest-running
+    // pair, in clocks
+    const long long pairs = std::max(1, train_sms() / 2);
+    long long best = -1;
+    for (int bn : {256, 128}) {
+        const long long n_tiles = (N + bn - 1) / bn, tiles = p.m_tiles * n_tiles;
+        for (int split = 1; split <= WG_MAX_SPLIT && (split == 1 || p.k_tiles / split >= WG_SPLIT_STEPS); ++split) {
+            const long long rounds = (tiles * split + pairs - 1) / pairs, steps = (p.k_tiles + split - 1) / split;
+            const long long cost = rounds * (steps * (bn == 256 ? WG_STEP_256 : WG_STEP_128) + WG_ITEM) +
+                                   (split > 1 ? WG_JOIN + M * N * (split + 1) * 4 / WG_JOIN_BYTES : 0);
+            if (best < 0 || cost < best) {
+                best = cost;
+                p.bn = bn;
+                p.n_tiles = (int)n_tiles;
+                p.split = split;
+            }
+        }
+    }
     p.ldx = (N + 7) / 8 * 8;
     p.ldd = (M + 7) / 8 * 8;
     p.ld_part = (N + 7) / 8 * 8;
@@ -583,28 +738,36 @@ int32_t iso_act_wgrad(const iso_mat* dY, const iso_act* pack, const iso_mat* out
         const size_t es = elem_size(out->dtype);
         return cudaMemset2DAsync(out->data, out->ld * es, 0, N * es, M, s) == cudaSuccess ? ISO_OK : ISO_ERR_CUDA;
     }
-    const int pairs = resident_pairs();
-    if (pairs <= 0) return ISO_ERR_CUDA;
+    if (few_tokens(T, M, N)) {
+        const long long m_blocks = (M + FEW_WARPS * FEW_ROWS - 1) / (FEW_WARPS * FEW_ROWS), n_blocks = (N + TRAIN_SEG - 1) / TRAIN_SEG;
+        if (m_blocks * n_blocks > EXTENT_LIMIT) return ISO_ERR_UNSUPPORTED;
+        return by_dtype(dY->dtype, [&](auto* tp) -> int {
+            return by_dtype(out->dtype, [&](auto* op) -> int {
+                using E = std::remove_pointer_t<decltype(tp)>;
+                using O = std::remove_pointer_t<decltype(op)>;
+                auto go = [&](auto v) -> int {
+                    TRAIN_LAUNCH((k_wgrad_few<E, O, decltype(v)::value><<<(unsigned)(m_blocks * n_blocks), FEW_TPB, 0, s>>>(
+                        static_cast<const E*>(dY->data), dY->ld, static_cast<const uint8_t*>(pack->codes), pack->ld_codes,
+                        static_cast<const uint8_t*>(pack->exps), pack->ld_exps, static_cast<O*>(out->data), out->ld,
+                        (int)T, (int)M, (int)N, (int)m_blocks, accumulate)));
+                    return ISO_OK;
+                };
+                return rows_aligned(out) ? go(std::true_type{}) : go(std::false_type{});
+            });
+        });
+    }
 
-    const iso_mat xb{ws + p.x_bf16, T, N, p.ldx, ISO_BF16, 0};
-    ISO_TRY(iso_act_unpack(pack, &xb, stream));
-    const int flat_grid = train_sms() * 8;
-    if (!p.dy_direct)
-        ISO_TRY(by_dtype(dY->dtype, [&](auto* tp) -> int {
-            using E = std::remove_pointer_t<decltype(tp)>;
-            TRAIN_LAUNCH((k_wgrad_parts<E><<<flat_grid, 256, 0, s>>>(
-                static_cast<const E*>(dY->data), dY->ld, (int)T, (int)M,
-                reinterpret_cast<__nv_bfloat16*>(ws + p.dy_parts), p.ldd, T * p.ldd)));
-            return ISO_OK;
-        }));
+    __nv_bfloat16* const xb = reinterpret_cast<__nv_bfloat16*>(ws + p.x_bf16);
+    __nv_bfloat16* const dy_parts = reinterpret_cast<__nv_bfloat16*>(ws + p.dy_parts);
+    ISO_TRY(launch_wgrad_operands(pack, xb, p.ldx, p.dy_direct ? nullptr : dY, dy_parts, p.ldd, s));
     WgradMaps maps;
-    ISO_TRY(bf16_map(&maps.b, xb.data, T, N, p.ldx));
-    for (int q = 0; q < WG_MAX_PARTS; ++q) {
-        const int part = std::max(0, p.n_parts - 1 - q);     // the last part first: small sums before large ones
+    ISO_TRY(bf16_map(&maps.b, xb, T, N, p.ldx));
+    for (int q = 0; q < p.n_parts; ++q) {
+        const int part = p.n_parts - 1 - q;      // the last part first: small sums before large ones
         if (p.dy_direct)
-            ISO_TRY(bf16_map(&maps.a[q], dY->data, T, M, dY->rows == 1 ? (M + 7) / 8 * 8 : dY->ld));
+            ISO_TRY(bf16_map(&maps.a[q], dY->data, T, M, dY->ld));
         else
-            ISO_TRY(bf16_map(&maps.a[q], ws + p.dy_parts + (size_t)part * T * p.ldd * 2, T, M, p.ldd));
+            ISO_TRY(bf16_map(&maps.a[q], dy_parts + (size_t)part * T * p.ldd, T, M, p.ldd));
     }
     WgradArgs g{};
     g.M = (int)M;
@@ -619,20 +782,25 @@ int32_t iso_act_wgrad(const iso_mat* dY, const iso_act* pack, const iso_mat* out
     g.ldo = out->ld;
     g.out_dtype = out->dtype;
     g.out_vec = rows_aligned(out);
-    g.part = p.split > 1 ? reinterpret_cast<float*>(ws + p.parts) : nullptr;
-    g.ld_part = p.ld_part;
+    // a bulk copy's rows are 16 bytes apart at least and start on such boundaries
+    g.out_copy = p.split > 1 || (!accumulate && g.out_vec && (out->ld * elem_size(out->dtype)) % 16 == 0);
+    float* const parts = reinterpret_cast<float*>(ws + p.parts);
+    if (p.split > 1)
+        ISO_TRY(out_map(&maps.out, parts, ISO_F32, M, N, p.ld_part, p.split));
+    else if (g.out_copy)
+        ISO_TRY(out_map(&maps.out, out->data, out->dtype, M, N, out->ld, 1));
     g.status = status;
     const int items = p.m_tiles * p.n_tiles * p.split;
-    TRAIN_LAUNCH((k_wgrad<<<2 * std::min(items, pairs), WG_THREADS, WG_SMEM, s>>>(maps, g)));
+    ISO_TRY(p.bn == 256 ? launch_wgrad<256>(maps, g, items, s) : launch_wgrad<128>(maps, g, items, s));
     if (p.split == 1) return ISO_OK;
     return by_dtype(out->dtype, [&](auto* op) -> int {
         using O = std::remove_pointer_t<decltype(op)>;
-        const int grid = (int)std::min((M * ((N + 7) / 8) + 255) / 256, (long long)flat_grid);
+        const int grid = (int)std::min((M * ((N + 7) / 8) + 255) / 256, (long long)EXTENT_LIMIT);
         if (g.out_vec)
-            TRAIN_LAUNCH((k_wgrad_join<O, true><<<grid, 256, 0, s>>>(g.part, g.ld_part, g.split, g.M, g.N,
+            TRAIN_LAUNCH((k_wgrad_join<O, true><<<grid, 256, 0, s>>>(parts, p.ld_part, g.split, g.M, g.N,
                                                                     static_cast<O*>(out->data), out->ld, accumulate)));
         else
-            TRAIN_LAUNCH((k_wgrad_join<O, false><<<grid, 256, 0, s>>>(g.part, g.ld_part, g.split, g.M, g.N,
+            TRAIN_LAUNCH((k_wgrad_join<O, false><<<grid, 256, 0, s>>>(parts, p.ld_part, g.split, g.M, g.N,
                                                                      static_cast<O*>(out->data), out->ld, accumulate)));
         return ISO_OK;
     });
