@@ -26,6 +26,7 @@
 #include "iso_internal.cuh"
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cooperative_groups.h>
 
@@ -47,6 +48,9 @@ constexpr long long SORT_ONE_CTA = 4096;                // up to this many token
 constexpr int SORT_SMEM = (SORT_WARPS * SORT_BINS + SORT_BINS + 32 + 4) * (int)sizeof(uint32_t);
 constexpr int FILL_TPB = 256;
 constexpr int FILL_CHUNK = 8192;                        // bytes of zeros a warp writes
+// Up to this many chunks the zeros ride along with the sort of one CTA: one launch
+// less (about 3 us of host time); 32 MB take about 5 us there.
+constexpr long long FILL_WITH_SORT = (32 << 20) / FILL_CHUNK;
 constexpr int SUM_TPB = 256;
 constexpr int SUM_WPB = SUM_TPB / 32;
 constexpr int SUM_RING = 4096;                          // bytes of dY rows in flight per warp
@@ -135,13 +139,16 @@ __device__ __forceinline__ void warp_zero(char* p, long long len, int lane) {
 
 // zeros in short blocks, in the order of addresses (a persistent grid reaches
 // 6.4 - 6.6 TB/s of writes here, short blocks 7.7)
-__global__ void __launch_bounds__(FILL_TPB) k_fill(FillArgs f) {
-    const int lane = threadIdx.x & 31;
-    const long long per_row = (f.width + FILL_CHUNK - 1) / FILL_CHUNK, warps = (long long)gridDim.x * (FILL_TPB / 32);
-    for (long long i = (long long)blockIdx.x * (FILL_TPB / 32) + (threadIdx.x >> 5); i < f.rows * per_row; i += warps) {
+__device__ __forceinline__ void fill_zeros(const FillArgs& f, long long warp, long long warps, int lane) {
+    const long long per_row = (f.width + FILL_CHUNK - 1) / FILL_CHUNK;
+    for (long long i = warp; i < f.rows * per_row; i += warps) {
         const long long r = i / per_row, off = (i - r * per_row) * FILL_CHUNK;
         warp_zero(f.base + r * f.stride + off, min((long long)FILL_CHUNK, f.width - off), lane);
     }
+}
+__global__ void __launch_bounds__(FILL_TPB) k_fill(FillArgs f) {
+    fill_zeros(f, (long long)blockIdx.x * (FILL_TPB / 32) + (threadIdx.x >> 5), (long long)gridDim.x * (FILL_TPB / 32),
+               threadIdx.x & 31);
     // this grid is not done before the sort that it started beside
     if (blockIdx.x == gridDim.x - 1) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
@@ -162,11 +169,16 @@ __device__ __forceinline__ uint2 sort_item(const SortArgs& a, const uint2* src, 
     return make_uint2(!pad && in ? (uint32_t)id : (uint32_t)a.ids.rows, (uint32_t)t);
 }
 
-// CTAS: the CTAs of the one cluster that is launched
+// CTAS: the CTAs of the one cluster that sorts.  With CTAS = 1 further CTAs of
+// the grid may write the zeros f.
 template <int CTAS>
-__global__ void __launch_bounds__(SORT_TPB, 1) k_sort(SortArgs a) {
+__global__ void __launch_bounds__(SORT_TPB, 1) k_sort(SortArgs a, FillArgs f) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the fill may start
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (CTAS == 1 && blockIdx.x > 0) {
+        fill_zeros(f, (long long)(blockIdx.x - 1) * SORT_WARPS + warp, (long long)(gridDim.x - 1) * SORT_WARPS, lane);
+        return;
+    }
     extern __shared__ uint32_t sort_smem[];
     uint32_t* const cnt = sort_smem;                                  // [warp][bin]
     uint32_t* const tot = cnt + SORT_WARPS * SORT_BINS;               // [bin]: this CTA's items
@@ -525,13 +537,21 @@ GradLayout grad_layout(int64_t n, int64_t cols) {
     return L;
 }
 
-// the sort: one cluster
+long long fill_chunks(const FillArgs& f) { return f.base ? f.rows * ((f.width + FILL_CHUNK - 1) / FILL_CHUNK) : 0; }
+
+// the sort: one cluster, and with CTAS = 1 the CTAs that write f's zeros
 template <int CTAS>
-int launch_sort(const SortArgs& a, cudaStream_t s) {
-    if (cudaFuncSetAttribute(k_sort<CTAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, SORT_SMEM) != cudaSuccess)
-        return ISO_ERR_CUDA;
+int launch_sort(const SortArgs& a, const FillArgs& f, cudaStream_t s) {
+    static std::atomic<uint64_t> ready{0};      // devices whose limit is raised, one bit each
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return ISO_ERR_CUDA;
+    if (dev >= 64 || !(ready.load(std::memory_order_relaxed) >> dev & 1)) {
+        if (cudaFuncSetAttribute(k_sort<CTAS>, cudaFuncAttributeMaxDynamicSharedMemorySize, SORT_SMEM) != cudaSuccess)
+            return ISO_ERR_CUDA;
+        if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+    }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(CTAS);
+    cfg.gridDim = dim3((unsigned)(CTAS + std::min((fill_chunks(f) + SORT_WARPS - 1) / SORT_WARPS, (long long)train_sms())));
     cfg.blockDim = dim3(SORT_TPB);
     cfg.dynamicSmemBytes = SORT_SMEM;
     cfg.stream = s;
@@ -541,12 +561,12 @@ int launch_sort(const SortArgs& a, cudaStream_t s) {
     at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
-    TRAIN_LAUNCH(cudaLaunchKernelEx(&cfg, k_sort<CTAS>, a));
+    TRAIN_LAUNCH(cudaLaunchKernelEx(&cfg, k_sort<CTAS>, a, f));
     return ISO_OK;
 }
 // the zeros, allowed to start once the sort has
 int launch_fill(const FillArgs& f, cudaStream_t s) {
-    const long long chunks = f.rows * ((f.width + FILL_CHUNK - 1) / FILL_CHUNK);
+    const long long chunks = fill_chunks(f);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)std::min((chunks + FILL_TPB / 32 - 1) / (FILL_TPB / 32), (long long)EXTENT_LIMIT));
     cfg.blockDim = dim3(FILL_TPB);
@@ -661,9 +681,12 @@ int32_t iso_embed_grad(const iso_mat* dY, const void* ids, int32_t ids_i64, int6
         fa = {static_cast<char*>(grad->data), flat ? 1 : (long long)grad->rows,
               (long long)grad->cols * es * (flat ? (long long)grad->rows : 1), (long long)grad->ld * es};
     }
-    if (n <= SORT_ONE_CTA) ISO_TRY(launch_sort<1>(sa, s));
-    else ISO_TRY(launch_sort<SORT_CLUSTER>(sa, s));
-    if (fa.base) ISO_TRY(launch_fill(fa, s));
+    if (n <= SORT_ONE_CTA && fill_chunks(fa) <= FILL_WITH_SORT) {
+        ISO_TRY(launch_sort<1>(sa, fa, s));
+    } else {
+        ISO_TRY(n <= SORT_ONE_CTA ? launch_sort<1>(sa, FillArgs{}, s) : launch_sort<SORT_CLUSTER>(sa, FillArgs{}, s));
+        if (fa.base) ISO_TRY(launch_fill(fa, s));
+    }
 
     RowArgs ra;
     ra.sorted = sa.buf[0];

@@ -62,7 +62,6 @@ struct WgTile {
 };
 constexpr int WG_THREADS = (WG_EPI_WARPS + 2) * 32;    // epilogue warps, a copy warp, a product warp
 constexpr int WG_MAX_PARTS = WGRAD_PARTS;
-constexpr int WG_MAX_SPLIT = 32;
 constexpr int WG_CHAIN = 8;                // steps accumulated in tensor memory before they are added in registers
 // the plan's estimates, in clocks: a step of either tile width, an item's start
 // and end, a join's launch and its bytes per clock
@@ -677,7 +676,8 @@ WgradPlan plan_wgrad(const iso_mat* dY, const iso_act* pack, const iso_mat* out)
     long long best = -1;
     for (int bn : {256, 128}) {
         const long long n_tiles = (N + bn - 1) / bn, tiles = p.m_tiles * n_tiles;
-        for (int split = 1; split <= WG_MAX_SPLIT && (split == 1 || p.k_tiles / split >= WG_SPLIT_STEPS); ++split) {
+        for (int split : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+            if (split > 1 && p.k_tiles / split < WG_SPLIT_STEPS) break;
             const long long rounds = (tiles * split + pairs - 1) / pairs, steps = (p.k_tiles + split - 1) / split;
             const long long cost = rounds * (steps * (bn == 256 ? WG_STEP_256 : WG_STEP_128) + WG_ITEM) +
                                    (split > 1 ? WG_JOIN + M * N * (split + 1) * 4 / WG_JOIN_BYTES : 0);

@@ -57,54 +57,29 @@ def _new(rows: int, cols: int, dtype, device):
     return t, IsoMat(t.data_ptr(), rows, cols, cols, code, 0)
 
 
-class _On:
-    """The stream and device of a call, from its first tensor: ``s`` is the raw
-    stream.  Entered, an explicit stream is the current one, so that tensors
-    allocated meanwhile belong to it and their memory is not reused before its
-    work.  The tensors' device must be the current one."""
-
-    __slots__ = ("s", "index", "device", "ctx")
-
-    def __init__(self, first: torch.Tensor, stream):
-        self.device = first.device
-        self.index = first.get_device()
-        if torch.cuda.current_device() != self.index:
-            raise ValueError(f"tensors are on {self.device}, the current device is cuda:{torch.cuda.current_device()}")
-        if stream is None:
-            self.ctx = None
-            self.s = _raw_stream(self.index)
-        else:
-            self.ctx = torch.cuda.stream(stream)
-            self.s = stream.cuda_stream
-
-    def __enter__(self):
-        if self.ctx is not None:
-            self.ctx.__enter__()
-        return self
-
-    def __exit__(self, *exc):
-        if self.ctx is not None:
-            self.ctx.__exit__(*exc)
-        return False
-
-    def has(self, *tensors: Optional[torch.Tensor]):
-        for t in tensors:
-            if t is not None and t.get_device() != self.index:
-                raise ValueError(f"tensors on different devices: {self.device} and {t.device}")
+def _here(first: torch.Tensor, *rest: Optional[torch.Tensor]) -> int:
+    """The current stream's handle; the tensors must be on the current device."""
+    index = first.get_device()
+    if torch.cuda.current_device() != index:
+        raise ValueError(f"tensors are on {first.device}, the current device is cuda:{torch.cuda.current_device()}")
+    for t in rest:
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"tensors on different devices: {first.device} and {t.device}")
+    return _raw_stream(index)
 
 
 _workspaces = {}
 
 
-def _scratch(ws: Optional[Workspace], on: _On, nbytes: int):
+def _scratch(ws: Optional[Workspace], device: torch.device, s: int) -> Workspace:
     """The caller's workspace, or a default one of the call's own stream (calls
     on different streams may overlap and must not share scratch)."""
     if ws is None:
-        key = (on.index, on.s)
+        key = (device.index, s)
         ws = _workspaces.get(key)
         if ws is None:
-            ws = _workspaces[key] = Workspace(on.device)
-    return ws.get(nbytes)
+            ws = _workspaces[key] = Workspace(device)
+    return ws
 
 
 def _status(want: bool, device):
@@ -190,30 +165,40 @@ class ActPack:
         return f"ActPack(shape={self.shape}, dtype={self.dtype}, device={self._buf.device})"
 
 
+# Every entry point, given a stream, runs with it as the current one: tensors
+# that the call allocates then belong to it, and their memory is not reused
+# before its work.
 def act_pack(x: torch.Tensor, out: Optional[ActPack] = None, stream=None) -> ActPack:
     """The 8-bit checkpoint of x (iso_act_pack)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return act_pack(x, out)
     dx = _mat(x, "x")
-    with _On(x, stream) as on:
-        if out is None:
-            out = ActPack.empty(dx.rows, dx.cols, x.dtype, on.device)
-        else:
-            on.has(out._buf)
-        check(lib().iso_act_pack(_byref(dx), _byref(out._abi), on.s), "iso_act_pack")
+    if out is None:
+        s = _here(x)
+        out = ActPack.empty(dx.rows, dx.cols, x.dtype, x.device)
+    else:
+        s = _here(x, out._buf)
+    check(lib().iso_act_pack(_byref(dx), _byref(out._abi), s), "iso_act_pack")
     return out
 
 
 def act_unpack(pack: ActPack, dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
                stream=None) -> torch.Tensor:
     """The values a checkpoint stands for (iso_act_unpack), exact in either type."""
-    with _On(pack._buf, stream) as on:
-        if out is None:
-            out, do = _new(pack._abi.rows, pack.cols, dtype or pack.dtype, on.device)
-        else:
-            if dtype is not None and out.dtype != dtype:
-                raise TypeError(f"out is {out.dtype}, dtype asks for {dtype}")
-            do = _mat(out, "out")
-            on.has(out)
-        check(lib().iso_act_unpack(_byref(pack._abi), _byref(do), on.s), "iso_act_unpack")
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return act_unpack(pack, dtype, out)
+    buf = pack._buf
+    if out is None:
+        s = _here(buf)
+        out, do = _new(pack._abi.rows, pack.cols, dtype or pack.dtype, buf.device)
+    else:
+        if dtype is not None and out.dtype != dtype:
+            raise TypeError(f"out is {out.dtype}, dtype asks for {dtype}")
+        do = _mat(out, "out")
+        s = _here(buf, out)
+    check(lib().iso_act_unpack(_byref(pack._abi), _byref(do), s), "iso_act_unpack")
     return out
 
 
@@ -230,24 +215,29 @@ def act_wgrad(dy: torch.Tensor, pack: ActPack, out: Optional[torch.Tensor] = Non
     (iso_act_wgrad), out_features x in_features, as opt_step takes it, in
     ``dtype`` (float32) or into ``out``; added to ``out`` with accumulate.
     Returns it (and the device status with status=True)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return act_wgrad(dy, pack, out, dtype, accumulate, workspace, status)
     dd = _mat(dy, "dy")
-    with _On(dy, stream) as on:
-        on.has(pack._buf)
-        if out is None:
-            if accumulate:
-                raise ValueError("accumulate needs an out to add to")
-            out, do = _new(dd.cols, pack.cols, dtype or torch.float32, on.device)
-        else:
-            if dtype is not None and out.dtype != dtype:
-                raise TypeError(f"out is {out.dtype}, dtype asks for {dtype}")
-            do = _mat(out, "out")
-            on.has(out)
+    s = _here(dy, pack._buf, out)
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs an out to add to")
+        out, do = _new(dd.cols, pack.cols, dtype or torch.float32, dy.device)
+    else:
+        if dtype is not None and out.dtype != dtype:
+            raise TypeError(f"out is {out.dtype}, dtype asks for {dtype}")
+        do = _mat(out, "out")
+    ws = _scratch(workspace, dy.device, s)
+    st = _status(status, dy.device)
+    L, args = lib(), (_byref(dd), _byref(pack._abi), _byref(do))
+    acc = 1 if accumulate else 0
+    rc = L.iso_act_wgrad(*args, acc, *ws.get(0), _ptr(st), s)
+    if rc == _abi.ISO_ERR_WORKSPACE:          # nothing was enqueued: grow the scratch to what the call needs
         nb = ctypes.c_size_t(0)
-        check(lib().iso_act_wgrad_workspace_size(_byref(dd), _byref(pack._abi), _byref(do), _byref(nb)), "iso_act_wgrad")
-        wptr, wlen = _scratch(workspace, on, nb.value)
-        st = _status(status, on.device)
-        check(lib().iso_act_wgrad(_byref(dd), _byref(pack._abi), _byref(do), int(bool(accumulate)), wptr, wlen,
-                                  _ptr(st), on.s), "iso_act_wgrad")
+        check(L.iso_act_wgrad_workspace_size(*args, _byref(nb)), "iso_act_wgrad")
+        rc = L.iso_act_wgrad(*args, acc, *ws.get(nb.value), _ptr(st), s)
+    check(rc, "iso_act_wgrad")
     return (out, st) if status else out
 
 
@@ -259,43 +249,54 @@ def swiglu_pack(gate: torch.Tensor, up: torch.Tensor, out: Optional[torch.Tensor
     """(h, gate_pack, up_pack): h = silu(gate) up and the checkpoints of both
     inputs in one pass (iso_swiglu_pack).  gate and up may be the halves of
     one buffer."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return swiglu_pack(gate, up, out, packs)
     dg, du = _mat(gate, "gate"), _mat(up, "up")
-    with _On(gate, stream) as on:
-        on.has(up)
-        if out is None:
-            out, do = _new(dg.rows, dg.cols, gate.dtype, on.device)
-        else:
-            do = _mat(out, "out")
-            on.has(out)
-        if packs is None:
-            packs = (ActPack.empty(dg.rows, dg.cols, gate.dtype, on.device),
-                     ActPack.empty(dg.rows, dg.cols, gate.dtype, on.device))
-        else:
-            on.has(packs[0]._buf, packs[1]._buf)
-        check(lib().iso_swiglu_pack(_byref(dg), _byref(du), _byref(do), _byref(packs[0]._abi), _byref(packs[1]._abi),
-                                    on.s), "iso_swiglu_pack")
-    return out, packs[0], packs[1]
+    s = _here(gate, up, out)
+    if out is None:
+        out, do = _new(dg.rows, dg.cols, gate.dtype, gate.device)
+    else:
+        do = _mat(out, "out")
+    if packs is None:
+        a = ActPack.empty(dg.rows, dg.cols, gate.dtype, gate.device)
+        b = ActPack.empty(dg.rows, dg.cols, gate.dtype, gate.device)
+    else:
+        a, b = packs
+        _here(gate, a._buf, b._buf)
+    check(lib().iso_swiglu_pack(_byref(dg), _byref(du), _byref(do), _byref(a._abi), _byref(b._abi), s),
+          "iso_swiglu_pack")
+    return out, a, b
 
 
 def swiglu_grad(dh: torch.Tensor, gate_pack: ActPack, up_pack: ActPack, out=None, need_h=True, stream=None):
     """(d_gate, d_up, h) from the gradient of h and the checkpoints of its
     inputs (iso_swiglu_grad); h is None without need_h.  ``out`` gives the
     tensors to write, d_gate and d_up possibly the halves of one buffer."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return swiglu_grad(dh, gate_pack, up_pack, out, need_h)
     dd = _mat(dh, "dh")
-    n = 3 if need_h else 2
-    with _On(dh, stream) as on:
-        on.has(gate_pack._buf, up_pack._buf)
-        if out is None:
-            got = [_new(dd.rows, dd.cols, dh.dtype, on.device) for _ in range(n)]
-            out, descs = [g[0] for g in got], [g[1] for g in got]
-        else:
-            if len(out) < n:
-                raise ValueError(f"out needs {n} tensors")
-            descs = [_mat(t, w) for t, w in zip(out[:n], ("d_gate", "d_up", "h"))]
-            on.has(*out[:n])
-        check(lib().iso_swiglu_grad(_byref(dd), _byref(gate_pack._abi), _byref(up_pack._abi), _byref(descs[0]),
-                                    _byref(descs[1]), _byref(descs[2]) if need_h else None, on.s), "iso_swiglu_grad")
-    return out[0], out[1], out[2] if need_h else None
+    s = _here(dh, gate_pack._buf, up_pack._buf)
+    h = dhh = None
+    if out is None:
+        rows, cols, dtype, device = dd.rows, dd.cols, dh.dtype, dh.device
+        d_gate, dg = _new(rows, cols, dtype, device)
+        d_up, du = _new(rows, cols, dtype, device)
+        if need_h:
+            h, dhh = _new(rows, cols, dtype, device)
+    else:
+        if len(out) < (3 if need_h else 2):
+            raise ValueError("out needs d_gate, d_up and, with need_h, h")
+        d_gate, d_up = out[0], out[1]
+        dg, du = _mat(d_gate, "d_gate"), _mat(d_up, "d_up")
+        if need_h:
+            h = out[2]
+            dhh = _mat(h, "h")
+        _here(dh, d_gate, d_up, h)
+    check(lib().iso_swiglu_grad(_byref(dd), _byref(gate_pack._abi), _byref(up_pack._abi), _byref(dg), _byref(du),
+                                None if dhh is None else _byref(dhh), s), "iso_swiglu_grad")
+    return d_gate, d_up, h
 
 
 # ---------------------------------------------------------------------------
@@ -322,20 +323,21 @@ def embed(table: torch.Tensor, ids: torch.Tensor, scale=1.0, pad_id: Optional[in
     table's type unless ``dtype`` or ``out`` says otherwise; zero rows where
     the id is pad_id.  Other ids outside the table give zero rows and
     ISO_ERR_INDEX in the device status (returned with status=True)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return embed(table, ids, scale, pad_id, out, dtype, status)
     dt = _mat(table, "table")
     ptr, i64, n = _ids(ids)
-    with _On(table, stream) as on:
-        on.has(ids)
-        if out is None:
-            out, do = _new(n, dt.cols, dtype or table.dtype, on.device)
-        else:
-            if dtype is not None and out.dtype != dtype:
-                raise TypeError(f"out is {out.dtype}, dtype asks for {dtype}")
-            do = _mat(out, "out")
-            on.has(out)
-        st = _status(status, on.device)
-        check(lib().iso_embed(_byref(dt), ptr, i64, n, -1 if pad_id is None else int(pad_id), _scale(scale),
-                              _byref(do), _ptr(st), on.s), "iso_embed")
+    s = _here(table, ids, out)
+    if out is None:
+        out, do = _new(n, dt.cols, dtype or table.dtype, table.device)
+    else:
+        if dtype is not None and out.dtype != dtype:
+            raise TypeError(f"out is {out.dtype}, dtype asks for {dtype}")
+        do = _mat(out, "out")
+    st = _status(status, table.device)
+    check(lib().iso_embed(_byref(dt), ptr, i64, n, -1 if pad_id is None else int(pad_id), _scale(scale), _byref(do),
+                          _ptr(st), s), "iso_embed")
     return (out, st) if status else out
 
 
@@ -353,27 +355,28 @@ def embed_grad(dy: torch.Tensor, ids: torch.Tensor, rows: Optional[int] = None, 
     (float32) or into ``out``, zero where no token has the row's id; added to
     ``out`` with accumulate.  The same inputs give the same bits.  Returns it
     (and the device status with status=True)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return embed_grad(dy, ids, rows, scale, pad_id, out, dtype, accumulate, workspace, status)
     dd = _mat(dy, "dy")
     ptr, i64, n = _ids(ids)
     if n != dd.rows:
         raise ValueError(f"{n} ids for {dd.rows} rows of dy")
-    with _On(dy, stream) as on:
-        on.has(ids)
-        if out is None:
-            if accumulate:
-                raise ValueError("accumulate needs an out to add to")
-            if rows is None:
-                raise ValueError("embed_grad needs rows (the table's) or out")
-            out, do = _new(int(rows), dd.cols, dtype or torch.float32, on.device)
-        else:
-            if rows is not None and out.shape[0] != rows:
-                raise ValueError(f"out has {out.shape[0]} rows, rows is {rows}")
-            if dtype is not None and out.dtype != dtype:
-                raise TypeError(f"out is {out.dtype}, dtype asks for {dtype}")
-            do = _mat(out, "out")
-            on.has(out)
-        wptr, wlen = _scratch(workspace, on, embed_grad_workspace_size(n, dd.cols))
-        st = _status(status, on.device)
-        check(lib().iso_embed_grad(_byref(dd), ptr, i64, -1 if pad_id is None else int(pad_id), _scale(scale),
-                                   _byref(do), int(bool(accumulate)), wptr, wlen, _ptr(st), on.s), "iso_embed_grad")
+    s = _here(dy, ids, out)
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs an out to add to")
+        if rows is None:
+            raise ValueError("embed_grad needs rows (the table's) or out")
+        out, do = _new(int(rows), dd.cols, dtype or torch.float32, dy.device)
+    else:
+        if rows is not None and out.shape[0] != rows:
+            raise ValueError(f"out has {out.shape[0]} rows, rows is {rows}")
+        if dtype is not None and out.dtype != dtype:
+            raise TypeError(f"out is {out.dtype}, dtype asks for {dtype}")
+        do = _mat(out, "out")
+    wptr, wlen = _scratch(workspace, dy.device, s).get(embed_grad_workspace_size(n, dd.cols))
+    st = _status(status, dy.device)
+    check(lib().iso_embed_grad(_byref(dd), ptr, i64, -1 if pad_id is None else int(pad_id), _scale(scale),
+                               _byref(do), 1 if accumulate else 0, wptr, wlen, _ptr(st), s), "iso_embed_grad")
     return (out, st) if status else out
