@@ -445,7 +445,7 @@ int32_t iso_gemm_tf32(const float* A, int64_t lda, const float* B, int64_t ldb, 
  * Matrices are row-major with a row stride (rows are tokens unless said
  * otherwise).  Any element-aligned address and stride is accepted; rows that
  * start on 16-byte boundaries (address and row stride multiples of 16 bytes)
- * take vector loads and stores.  rows and cols are below 2^31.  Two matrices
+ * take vector loads and stores.  rows and cols are at most 2^31 - 2^16.  Two matrices
  * "overlap" when they share a byte: the halves of one wider buffer (same row
  * stride, disjoint column ranges) do not.  An empty matrix may have data =
  * NULL. */
@@ -530,7 +530,7 @@ int32_t iso_embed(const iso_mat* table, const void* ids, int32_t ids_i64, int64_
  * without tokens unchanged.  dY n x cols; grad table rows x cols, BF16 or
  * F32.  Tokens are sorted by id and each row's sum is binary32 in an order
  * that depends on the ids alone, so equal inputs give equal bits; one rounding
- * to grad's type.  n < 2^31.  grad overlaps neither dY nor ids.  An empty grad:
+ * to grad's type.  grad overlaps neither dY nor ids.  An empty grad:
  * nothing is read, and no id is reported. */
 int32_t iso_embed_grad_workspace_size(int64_t n, int64_t cols, size_t* bytes);
 int32_t iso_embed_grad(const iso_mat* dY, const void* ids, int32_t ids_i64, int64_t pad_id, float scale,

@@ -10,19 +10,20 @@
 #include "iso_train.cuh"
 
 #include <algorithm>
+#include <atomic>
 
 namespace iso {
 
 int train_sms() {
-    static int sms[64] = {};
+    static std::atomic<int> sms[64];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 152;
-    if (!sms[dev]) {
-        int n = 0;
+    int n = sms[dev].load(std::memory_order_relaxed);
+    if (!n) {
         if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 152;
-        sms[dev] = n;
+        sms[dev].store(n, std::memory_order_relaxed);
     }
-    return sms[dev];
+    return n;
 }
 
 namespace {

@@ -26,13 +26,16 @@ inline int64_t act_exps_padded(int64_t cols) {
     return ((cols + ISO_ACT_GROUP - 1) / ISO_ACT_GROUP + 7) / 8 * 8;
 }
 
-constexpr int64_t EXTENT_LIMIT = 0x7FFFFFFFLL;
+constexpr int64_t EXTENT_LIMIT = 0x7FFF0000LL;    // below 2^31 with room for a kernel's last step
 constexpr int64_t STRIDE_LIMIT = 1LL << 36;
+constexpr int64_t SPAN_LIMIT = 1LL << 52;         // rows x stride
+inline bool span_too_large(int64_t rows, int64_t ld) { return rows > 1 && ld > SPAN_LIMIT / rows; }
 
 inline int check_mat(const iso_mat* m) {
     if (!m || m->reserved != 0) return ISO_ERR_ARG;
     if (m->rows < 0 || m->cols < 0 || m->ld < m->cols) return ISO_ERR_SHAPE;
-    if (m->rows > EXTENT_LIMIT || m->cols > EXTENT_LIMIT || m->ld > STRIDE_LIMIT) return ISO_ERR_UNSUPPORTED;
+    if (m->rows > EXTENT_LIMIT || m->cols > EXTENT_LIMIT || m->ld > STRIDE_LIMIT || span_too_large(m->rows, m->ld))
+        return ISO_ERR_UNSUPPORTED;
     if (m->dtype != ISO_BF16 && m->dtype != ISO_F32) return ISO_ERR_DTYPE;
     if (m->rows == 0 || m->cols == 0) return ISO_OK;
     if (!m->data) return ISO_ERR_ARG;
@@ -43,8 +46,8 @@ inline int check_mat(const iso_mat* m) {
 inline int check_act(const iso_act* a) {
     if (!a) return ISO_ERR_ARG;
     if (a->rows < 0 || a->cols < 0) return ISO_ERR_SHAPE;
-    if (a->rows > EXTENT_LIMIT || a->cols > EXTENT_LIMIT - ISO_ACT_GROUP || a->ld_codes > STRIDE_LIMIT ||
-        a->ld_exps > STRIDE_LIMIT)
+    if (a->rows > EXTENT_LIMIT || a->cols > EXTENT_LIMIT || a->ld_codes > STRIDE_LIMIT || a->ld_exps > STRIDE_LIMIT ||
+        span_too_large(a->rows, a->ld_codes) || span_too_large(a->rows, a->ld_exps))
         return ISO_ERR_UNSUPPORTED;
     if (a->ld_codes < act_cols_padded(a->cols) || a->ld_exps < act_exps_padded(a->cols)) return ISO_ERR_SHAPE;
     if (a->ld_codes % ISO_ACT_GROUP || a->ld_exps % 8) return ISO_ERR_ALIGN;
