@@ -696,6 +696,8 @@ int run_group(const Call& c, int t0, int t1, char* ws, cudaStream_t s, const iso
                 else if (K == 2) ISO_TRY(gram(std::integral_constant<int, 2>{}));
                 else if (K <= 4) ISO_TRY(gram(std::integral_constant<int, 4>{}));
                 else ISO_TRY(gram(std::integral_constant<int, 8>{}));
+            } else if (gram_mode == GRAM_ACCUM) {
+                ISO_TRY(launch(KD_GRAM, s, [&] { k_block_gram<<<T, 256, 0, s>>>(P); }));
             }
             ISO_TRY(launch(KD_SOLVE, s, [&] { k_solve<<<(T + 127) / 128, 128, 0, s>>>(P, gram_mode); }));
         }

@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(BLOCK_TPB, BLOCK_CTAS_PER_SM) k_block_select(P
             U.state = ST_DONE;
             if (want_gamma) {
                 const double ft = (double)__uint_as_float(tk);
-                atomicAdd(&P.gram[t], g + (double)need * ft * ft);
+                U.gamma = g + (double)need * ft * ft;
             }
             stats(tk, k, tot_above, tot_ties, need);
         }
@@ -355,11 +355,30 @@ __global__ void __launch_bounds__(BLOCK_TPB, BLOCK_CTAS_PER_SM) k_block_select(P
         U.state = ST_DONE;
         if (want_gamma) {
             const double ft = (double)__uint_as_float(tk);
-            atomicAdd(&P.gram[t], g + (double)need * ft * ft);
+            U.gamma = g + (double)need * ft * ft;
         }
         stats(tk, k, tot_above, tot_ties, need);
     }
     if (P.fuse_block) apply_block(tk, cut, false);
+}
+
+// K = 1 retention: the tensor's Gram from its units' sums, one block per tensor,
+// in an order fixed by the unit's place (threads take every 256th unit, then
+// their sums in thread order by the block's tree), so equal inputs give equal
+// bits; added up by atomics, the last bits depended on the units' timing.
+__global__ void __launch_bounds__(256) k_block_gram(Plan P) {
+    __shared__ double s[256];
+    const TensorDesc& d = P.tens[blockIdx.x];
+    double g = 0.0;
+    if (d.flags & TF_TRIM)
+        for (int b = threadIdx.x; b < d.nblocks; b += 256) g += P.units[d.unit + b].gamma;
+    s[threadIdx.x] = g;
+    __syncthreads();
+    for (int o = 128; o > 0; o >>= 1) {
+        if (threadIdx.x < o) s[threadIdx.x] += s[threadIdx.x + o];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) P.gram[blockIdx.x] = s[0];
 }
 
 #define ISO_BLOCK_INST(XT, BT, CK) template __global__ void k_block_select<XT, BT, CK>(Plan);
