@@ -51,7 +51,7 @@ constexpr int FILL_CHUNK = 8192;                        // bytes of zeros a warp
 // Up to this many chunks the zeros ride along with the sort of one CTA: one launch
 // less (about 3 us of host time); 32 MB take about 5 us there.
 constexpr long long FILL_WITH_SORT = (32 << 20) / FILL_CHUNK;
-constexpr int SUM_TPB = 256;
+constexpr int SUM_TPB = 128;
 constexpr int SUM_WPB = SUM_TPB / 32;
 constexpr int SUM_RING = 4096;                          // bytes of dY rows in flight per warp
 constexpr int SUM_WARPS_PER_SM = 24;                    // windows are as long as leaves this many warps a SM
@@ -307,7 +307,8 @@ __device__ __forceinline__ void write_row(O* row, int c, int cols, float (&v)[8]
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] *= scale;
     }
-    store8<VEC>(row, c, cols, v);
+    if (VEC && c + 8 <= cols) put8(row + c, v);
+    else store8<false>(row, c, cols, v);
 }
 
 // eight channels of a row of dY into this lane's place in shared memory,
@@ -328,7 +329,7 @@ __device__ __forceinline__ void copy8_async(uint32_t dst, const T* row, int c, i
 // boundaries stream through a ring of rows in shared memory (every
 // lane reads back what it copied itself), so the loads of later tokens are
 // under way while a run is written; loaded eight tokens at a time into
-// registers instead, the 32768 x 3584 case measured 148 us, this way 80 us.
+// registers instead, the 32768 x 3584 case measured 148 us, this way 75 us (84 us with blocks of 256 threads).
 template <typename T, typename O, bool VEC>
 __global__ void __launch_bounds__(SUM_TPB) k_row_sums(const T* dy, long long ldd, O* grad, long long ldg, RowArgs a) {
     constexpr int LANE_BYTES = 8 * (int)sizeof(T), SLOT = 32 * LANE_BYTES, DEPTH = SUM_RING / SLOT;
