@@ -329,7 +329,8 @@ __device__ __forceinline__ void copy8_async(uint32_t dst, const T* row, int c, i
 // boundaries stream through a ring of rows in shared memory (every
 // lane reads back what it copied itself), so the loads of later tokens are
 // under way while a run is written; loaded eight tokens at a time into
-// registers instead, the 32768 x 3584 case measured 148 us, this way 75 us (84 us with blocks of 256 threads).
+// registers instead, the 32768 x 3584 case measured 148 us, this way 75 us (84
+// us with blocks of 256 threads).
 template <typename T, typename O, bool VEC>
 __global__ void __launch_bounds__(SUM_TPB) k_row_sums(const T* dy, long long ldd, O* grad, long long ldg, RowArgs a) {
     constexpr int LANE_BYTES = 8 * (int)sizeof(T), SLOT = 32 * LANE_BYTES, DEPTH = SUM_RING / SLOT;

@@ -18,16 +18,17 @@
 //              the waits and commits of a stage costing the same), persistent
 //              over the tiles.  The tensor cores' accumulation cuts low bits
 //              off at every product: the relative error of a binary32 G grows
-//              in proportion to the chain of products (1.1e-6, 4.4e-7 and 2.0e-7 at chains of 4096, 2048 and 1024
-//              tokens of 8192 random ones; a plain binary32 product has
-//              3.1e-7).  So a chain is 1024 tokens; the epilogue warps add the
+//              in proportion to the chain of products (1.1e-6, 4.4e-7 and
+//              2.0e-7 at chains of 4096, 2048 and 1024 tokens of 8192 random
+//              ones; a plain binary32 product has 3.1e-7).  So a chain is 1024 tokens; the epilogue warps add the
 //              chains up in registers, 128 sums a thread, rounding to nearest,
 //              while the next chain runs in the other of two accumulators in
 //              tensor memory (chains of 2048 measured 1 % faster).
-//   measured   18944 x 3584 over 8192 tokens (1.11 PFLOP): 579 us alone, 1922
-//              TFLOP/s, with 16 us before it for the decoding; a bf16 library
+//   measured   18944 x 3584 over 8192 tokens (1.11 PFLOP): 571 us, 1.95
+//              PFLOP/s, and 11 us before it for the decoding; a bf16 library
 //              product of the same operands 559 - 580 us.  The products
-//              themselves bound it, then the copies (about 470 us alone).
+//              themselves bound it (tensor pipe 85 % active), then the copies
+//              (472 us without products).
 //   split      a G of few tiles under many tokens is cut along the tokens as
 //              well; the parts are binary32 in the workspace and k_wgrad_join
 //              adds them in order.
