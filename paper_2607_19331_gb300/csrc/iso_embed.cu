@@ -44,7 +44,10 @@ constexpr int SORT_TPB = 1024;
 constexpr int SORT_WARPS = SORT_TPB / 32;
 constexpr int SORT_BITS = 9;
 constexpr int SORT_BINS = 1 << SORT_BITS;
-constexpr long long SORT_ONE_CTA = 4096;                // up to this many tokens one CTA sorts alone
+// Up to this many tokens one CTA sorts alone.  Measured, the accumulating gradient
+// of 152064 x 64 whole, one CTA against a cluster of eight: 2000 tokens 23.1 / 23.2
+// us, 4096 tokens 29.5 / 24.1 us.
+constexpr long long SORT_ONE_CTA = 2048;
 constexpr int SORT_SMEM = (SORT_WARPS * SORT_BINS + SORT_BINS + 32 + 4) * (int)sizeof(uint32_t);
 constexpr int FILL_TPB = 256;
 constexpr int FILL_CHUNK = 8192;                        // bytes of zeros a warp writes
