@@ -1,7 +1,8 @@
-"""Build the CUDA library ``libiso_gb300.so`` in-tree for sm_103a.
+"""Build the CUDA library ``libiso_gb300.so`` in-tree for sm_103a, and the host
+module ``_iso_train`` that marshals torch tensors for the training-step calls.
 
-Each translation unit is compiled by nvcc in parallel, then linked into a
-shared library next to this file under ``_build/``.  Nothing is installed.
+Each translation unit is compiled in parallel, then linked into a shared
+library next to this file under ``_build/``.  Nothing is installed.
 """
 from __future__ import annotations
 
@@ -9,12 +10,14 @@ import concurrent.futures as cf
 import os
 import shutil
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(BUILD, "libiso_gb300.so")
+BINDING = os.path.join(BUILD, "_iso_train.so")
 SOURCES = ["iso_api.cu", "iso_select.cu", "iso_apply.cu", "iso_merge.cu", "iso_block.cu", "iso_fused.cu",
            "iso_gemm.cu", "iso_frame.cu", "iso_range.cu", "iso_act.cu", "iso_wgrad.cu", "iso_embed.cu"]
 HEADERS = ["iso_internal.cuh", "iso_kernels.cuh", "iso_gemm.cuh", "iso_train.cuh"]
@@ -28,6 +31,24 @@ def nvcc() -> str:
     if not os.path.exists(exe):
         raise RuntimeError("nvcc not found: the CUDA toolkit is required to build libiso_gb300")
     return exe
+
+
+def binding_commands(obj: str):
+    """(compile, link) commands of the host module."""
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc())))
+    cxx = shutil.which("g++") or "g++"
+    inc = [os.path.join(ROOT, "include"), os.path.join(root, "include"),
+           os.path.join(root, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include"),
+           "/usr/local/cuda/include", sysconfig.get_paths()["include"]]
+    compile_ = [cxx, "-O2", "-std=c++17", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                *[x for i in inc if os.path.isdir(i) for x in ("-I", i)], "-c", os.path.join(CSRC, "train_binding.cpp"),
+                "-o", obj]
+    lib = os.path.join(root, "lib")
+    link = [cxx, "-shared", obj, "-L", lib, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", "-L", BUILD,
+            "-l:libiso_gb300.so", "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{lib}"]
+    return compile_, link
 
 
 def _stale(target: str, deps) -> bool:
@@ -49,20 +70,31 @@ def build(force: bool = False, verbose: bool = False, extra=None) -> str:
             cmd = [nvcc(), *ARCH, *FLAGS, *(extra or []), "-c", s, "-o", o]
             jobs.append(cmd)
 
+    bobj = os.path.join(BUILD, "train_binding.o")
+    bcompile, blink = binding_commands(bobj)
+    bnew = force or _stale(bobj, [os.path.join(CSRC, "train_binding.cpp"), os.path.join(ROOT, "include", "iso.h")])
+    cu_jobs = len(jobs)
+    if bnew:
+        jobs.append(bcompile)
+
     def run(cmd):
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
-            raise RuntimeError(f"nvcc failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+            raise RuntimeError(f"compilation failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
         return r.stderr
 
-    with cf.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
         for err in ex.map(run, jobs):
             if verbose and err:
                 print(err)
-    if force or jobs or _stale(LIB, objs):
+    if force or cu_jobs or _stale(LIB, objs):
         tmp = LIB + f".tmp{os.getpid()}"
         subprocess.check_call([nvcc(), *ARCH, "-shared", "-o", tmp, *objs, "-lcudart"])
         os.replace(tmp, LIB)
+    if bnew or _stale(BINDING, [bobj]):
+        tmp = BINDING + f".tmp{os.getpid()}"
+        subprocess.check_call([*blink, "-o", tmp])
+        os.replace(tmp, BINDING)
     return LIB
 
 

@@ -3,7 +3,9 @@
 and the token embedding with its gradient.
 
 Argument marshalling only, as in ``api``; every step of the computation runs in
-libiso_gb300.so.  Matrices are 2-D CUDA tensors (tokens in rows), bfloat16 or
+libiso_gb300.so.  The common form of a call (outputs allocated by it, on the
+current stream) is marshalled by the host module ``_iso_train``
+(csrc/train_binding.cpp), any other form here.  Matrices are 2-D CUDA tensors (tokens in rows), bfloat16 or
 float32, with unit stride along a row and any row stride.  Work is enqueued on
 ``stream`` (default: the current stream), where tensors that a call allocates
 belong too; nothing waits for the device.
@@ -12,7 +14,9 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import importlib.util
 import math
+import os
 from typing import Optional, Tuple
 
 import torch
@@ -24,6 +28,23 @@ from .api import Workspace
 GROUP = _abi.ISO_ACT_GROUP
 _CODES = {torch.bfloat16: _abi.ISO_BF16, torch.float32: _abi.ISO_F32}
 _byref = ctypes.byref
+_native = None
+
+
+def _load_native():
+    """The host module beside the loaded library; raises if it has not been built."""
+    global _native
+    if _native is None:
+        lib()
+        path = os.path.join(os.path.dirname(_abi.LIB_PATH), "_iso_train.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"_iso_train not found at {path}: build it first "
+                               "(python -c 'import __graft_entry__ as g; g.build()')")
+        spec = importlib.util.spec_from_file_location("_iso_train", path)
+        mod = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(mod)
+        _native = mod
+    return _native
 # the current stream's handle without a Stream object, where this torch has it
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
@@ -82,6 +103,13 @@ def _scratch(ws: Optional[Workspace], device: torch.device, s: int) -> Workspace
     return ws
 
 
+def _done(result, where: str):
+    """The native call's result, or the error its status code stands for."""
+    if type(result) is int:
+        check(result, where)
+    return result
+
+
 def _status(want: bool, device):
     return torch.zeros(1, dtype=torch.int32, device=device) if want else None
 
@@ -100,7 +128,8 @@ class ActPack:
     default of act_unpack.  ``rows(a, b)`` is the checkpoint of a range of
     rows, sharing storage."""
 
-    __slots__ = ("cols", "dtype", "_abi", "_parts", "_buf")
+    # _t: storage, addresses of codes and exponents, rows, cols, row strides of both
+    __slots__ = ("dtype", "_t", "_parts")
 
     def __init__(self, codes: torch.Tensor, exps: torch.Tensor, cols: int, dtype=torch.bfloat16):
         if codes.dtype != torch.int8 or exps.dtype != torch.uint8 or codes.dim() != 2 or exps.dim() != 2:
@@ -114,10 +143,16 @@ class ActPack:
             raise ValueError("a checkpoint's codes and exponents do not fit its shape")
         if cols and (codes.stride(1) != 1 or exps.stride(1) != 1):
             raise ValueError("a checkpoint's codes and exponents must have unit stride along their rows")
-        rows, one = codes.shape[0], codes.shape[0] <= 1
-        self.cols, self.dtype, self._buf, self._parts = cols, dtype, codes, (codes, exps)
-        self._abi = IsoAct(codes.data_ptr(), exps.data_ptr(), rows, cols, codes.shape[1] if one else codes.stride(0),
-                           exps.shape[1] if one else exps.stride(0))
+        one = codes.shape[0] <= 1
+        self.dtype, self._parts = dtype, (codes, exps)
+        self._t = (codes, codes.data_ptr(), exps.data_ptr(), int(codes.shape[0]), int(cols),
+                   int(codes.shape[1]) if one else codes.stride(0), int(exps.shape[1]) if one else exps.stride(0))
+
+    @staticmethod
+    def _of(t: tuple, dtype) -> "ActPack":
+        self = object.__new__(ActPack)
+        self.dtype, self._t, self._parts = dtype, t, None
+        return self
 
     @staticmethod
     def empty(rows: int, cols: int, dtype=torch.bfloat16, device="cuda") -> "ActPack":
@@ -127,20 +162,28 @@ class ActPack:
             raise TypeError(f"a checkpoint's dtype must be bfloat16 or float32, got {dtype}")
         groups = -(-cols // GROUP)
         ldc, lde = groups * GROUP, -(-groups // 8) * 8
-        self = object.__new__(ActPack)
-        self.cols, self.dtype, self._parts = cols, dtype, None
-        self._buf = buf = torch.empty(rows * (ldc + lde), dtype=torch.uint8, device=device)
+        buf = torch.empty(rows * (ldc + lde), dtype=torch.uint8, device=device)
         at = buf.data_ptr()
-        self._abi = IsoAct(at, at + rows * ldc, rows, cols, ldc, lde)
-        return self
+        return ActPack._of((buf, at, at + rows * ldc, rows, cols, ldc, lde), dtype)
 
     def _views(self):
         if self._parts is None:
-            a = self._abi
-            n = a.rows * a.ld_codes
-            self._parts = (self._buf[:n].view(torch.int8).view(a.rows, a.ld_codes),
-                           self._buf[n:].view(a.rows, a.ld_exps))
+            buf, _, _, rows, _, ldc, lde = self._t
+            n = rows * ldc
+            self._parts = buf[:n].view(torch.int8).view(rows, ldc), buf[n:].view(rows, lde)
         return self._parts
+
+    @property
+    def _buf(self) -> torch.Tensor:
+        return self._t[0]
+
+    @property
+    def _abi(self) -> IsoAct:
+        return IsoAct(*self._t[1:])
+
+    @property
+    def cols(self) -> int:
+        return self._t[4]
 
     @property
     def codes(self) -> torch.Tensor:
@@ -152,7 +195,7 @@ class ActPack:
 
     @property
     def shape(self) -> Tuple[int, int]:
-        return self._abi.rows, self.cols
+        return self._t[3], self._t[4]
 
     @property
     def nbytes(self) -> int:
@@ -170,6 +213,8 @@ class ActPack:
 # before its work.
 def act_pack(x: torch.Tensor, out: Optional[ActPack] = None, stream=None) -> ActPack:
     """The 8-bit checkpoint of x (iso_act_pack)."""
+    if out is None and stream is None:
+        return ActPack._of(_done((_native or _load_native()).act_pack(x), "iso_act_pack"), x.dtype)
     if stream is not None:
         with torch.cuda.stream(stream):
             return act_pack(x, out)
@@ -186,13 +231,15 @@ def act_pack(x: torch.Tensor, out: Optional[ActPack] = None, stream=None) -> Act
 def act_unpack(pack: ActPack, dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
                stream=None) -> torch.Tensor:
     """The values a checkpoint stands for (iso_act_unpack), exact in either type."""
+    if out is None and stream is None:
+        return _done((_native or _load_native()).act_unpack(pack._t, dtype or pack.dtype), "iso_act_unpack")
     if stream is not None:
         with torch.cuda.stream(stream):
             return act_unpack(pack, dtype, out)
     buf = pack._buf
     if out is None:
         s = _here(buf)
-        out, do = _new(pack._abi.rows, pack.cols, dtype or pack.dtype, buf.device)
+        out, do = _new(pack.shape[0], pack.cols, dtype or pack.dtype, buf.device)
     else:
         if dtype is not None and out.dtype != dtype:
             raise TypeError(f"out is {out.dtype}, dtype asks for {dtype}")
@@ -215,6 +262,8 @@ def act_wgrad(dy: torch.Tensor, pack: ActPack, out: Optional[torch.Tensor] = Non
     (iso_act_wgrad), out_features x in_features, as opt_step takes it, in
     ``dtype`` (float32) or into ``out``; added to ``out`` with accumulate.
     Returns it (and the device status with status=True)."""
+    if out is None and stream is None and workspace is None and not status and not accumulate:
+        return _done((_native or _load_native()).act_wgrad(dy, pack._t, dtype), "iso_act_wgrad")
     if stream is not None:
         with torch.cuda.stream(stream):
             return act_wgrad(dy, pack, out, dtype, accumulate, workspace, status)
@@ -249,6 +298,9 @@ def swiglu_pack(gate: torch.Tensor, up: torch.Tensor, out: Optional[torch.Tensor
     """(h, gate_pack, up_pack): h = silu(gate) up and the checkpoints of both
     inputs in one pass (iso_swiglu_pack).  gate and up may be the halves of
     one buffer."""
+    if out is None and packs is None and stream is None:
+        h, a, b = _done((_native or _load_native()).swiglu_pack(gate, up), "iso_swiglu_pack")
+        return h, ActPack._of(a, gate.dtype), ActPack._of(b, gate.dtype)
     if stream is not None:
         with torch.cuda.stream(stream):
             return swiglu_pack(gate, up, out, packs)
@@ -273,6 +325,9 @@ def swiglu_grad(dh: torch.Tensor, gate_pack: ActPack, up_pack: ActPack, out=None
     """(d_gate, d_up, h) from the gradient of h and the checkpoints of its
     inputs (iso_swiglu_grad); h is None without need_h.  ``out`` gives the
     tensors to write, d_gate and d_up possibly the halves of one buffer."""
+    if out is None and stream is None:
+        return _done((_native or _load_native()).swiglu_grad(dh, gate_pack._t, up_pack._t, bool(need_h)),
+                     "iso_swiglu_grad")
     if stream is not None:
         with torch.cuda.stream(stream):
             return swiglu_grad(dh, gate_pack, up_pack, out, need_h)
@@ -323,6 +378,9 @@ def embed(table: torch.Tensor, ids: torch.Tensor, scale=1.0, pad_id: Optional[in
     table's type unless ``dtype`` or ``out`` says otherwise; zero rows where
     the id is pad_id.  Other ids outside the table give zero rows and
     ISO_ERR_INDEX in the device status (returned with status=True)."""
+    if out is None and stream is None and not status:
+        return _done((_native or _load_native()).embed(table, ids, _scale(scale), -1 if pad_id is None else int(pad_id),
+                                                       dtype), "iso_embed")
     if stream is not None:
         with torch.cuda.stream(stream):
             return embed(table, ids, scale, pad_id, out, dtype, status)
@@ -355,6 +413,10 @@ def embed_grad(dy: torch.Tensor, ids: torch.Tensor, rows: Optional[int] = None, 
     (float32) or into ``out``, zero where no token has the row's id; added to
     ``out`` with accumulate.  The same inputs give the same bits.  Returns it
     (and the device status with status=True)."""
+    if out is None and rows is not None and stream is None and workspace is None and not status and not accumulate:
+        return _done((_native or _load_native()).embed_grad(dy, ids, int(rows), _scale(scale),
+                                                            -1 if pad_id is None else int(pad_id), dtype),
+                     "iso_embed_grad")
     if stream is not None:
         with torch.cuda.stream(stream):
             return embed_grad(dy, ids, rows, scale, pad_id, out, dtype, accumulate, workspace, status)
