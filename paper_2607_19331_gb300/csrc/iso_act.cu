@@ -195,6 +195,8 @@ struct PartsArgs {
 template <typename T>
 __global__ void __launch_bounds__(ACT_TPB) k_wgrad_operands(ActView in, int cols, __nv_bfloat16* x, long long ldx,
                                                             Items it, unsigned unpack_blocks, PartsArgs p) {
+    start_next();
+    wait_before();
     const int lane = threadIdx.x & 31;
     if (blockIdx.x < unpack_blocks) {
         for (long long i = (long long)blockIdx.x * ACT_WPB + (threadIdx.x >> 5); i < it.n; i += (long long)unpack_blocks * ACT_WPB) {
@@ -391,11 +393,11 @@ int launch_wgrad_operands(const iso_act* pack, __nv_bfloat16* x, long long ldx, 
         part_blocks = (unsigned)std::min((p.n + ACT_TPB - 1) / ACT_TPB, 1LL << 30);
     }
     if (dy && dy->dtype == ISO_F32)
-        TRAIN_LAUNCH((k_wgrad_operands<float><<<unpack_blocks + part_blocks, ACT_TPB, 0, s>>>(
-            view(pack), (int)pack->cols, x, ldx, it, unpack_blocks, p)));
+        TRAIN_LAUNCH(launch_early(k_wgrad_operands<float>, unpack_blocks + part_blocks, ACT_TPB, 0, s, view(pack),
+                                  (int)pack->cols, x, ldx, it, unpack_blocks, p));
     else
-        TRAIN_LAUNCH((k_wgrad_operands<__nv_bfloat16><<<unpack_blocks + part_blocks, ACT_TPB, 0, s>>>(
-            view(pack), (int)pack->cols, x, ldx, it, unpack_blocks, p)));
+        TRAIN_LAUNCH(launch_early(k_wgrad_operands<__nv_bfloat16>, unpack_blocks + part_blocks, ACT_TPB, 0, s, view(pack),
+                                  (int)pack->cols, x, ldx, it, unpack_blocks, p));
     return ISO_OK;
 }
 

@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(FILL_TPB) k_fill(FillArgs f) {
     fill_zeros(f, (long long)blockIdx.x * (FILL_TPB / 32) + (threadIdx.x >> 5), (long long)gridDim.x * (FILL_TPB / 32),
                threadIdx.x & 31);
     // this grid is not done before the sort that it started beside
-    if (blockIdx.x == gridDim.x - 1) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (blockIdx.x == gridDim.x - 1) wait_before();
 }
 
 struct SortArgs {
@@ -176,7 +176,7 @@ __device__ __forceinline__ uint2 sort_item(const SortArgs& a, const uint2* src, 
 // the grid may write the zeros f.
 template <int CTAS>
 __global__ void __launch_bounds__(SORT_TPB, 1) k_sort(SortArgs a, FillArgs f) {
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the fill may start
+    start_next();                                                     // the fill, or the row sums, may start
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (CTAS == 1 && blockIdx.x > 0) {
         fill_zeros(f, (long long)(blockIdx.x - 1) * SORT_WARPS + warp, (long long)(gridDim.x - 1) * SORT_WARPS, lane);
@@ -336,6 +336,8 @@ __device__ __forceinline__ void copy8_async(uint32_t dst, const T* row, int c, i
 // us with blocks of 256 threads).
 template <typename T, typename O, bool VEC>
 __global__ void __launch_bounds__(SUM_TPB) k_row_sums(const T* dy, long long ldd, O* grad, long long ldg, RowArgs a) {
+    start_next();
+    wait_before();
     constexpr int LANE_BYTES = 8 * (int)sizeof(T), SLOT = 32 * LANE_BYTES, DEPTH = SUM_RING / SLOT;
     __shared__ __align__(16) unsigned char ring[VEC ? SUM_WPB * SUM_RING : 16];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -408,6 +410,7 @@ __global__ void __launch_bounds__(SUM_TPB) k_row_sums(const T* dy, long long ldd
 template <typename O>
 __global__ void __launch_bounds__(JOIN_TPB) k_row_join(O* grad, long long ldg, RowArgs a) {
     __shared__ float4 sums[JOIN_TPB / 32][32];
+    wait_before();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr int WARPS = JOIN_TPB / 32;
     const int slices = (a.cols + JOIN_COLS - 1) / JOIN_COLS;
@@ -572,16 +575,8 @@ int launch_sort(const SortArgs& a, const FillArgs& f, cudaStream_t s) {
 // the zeros, allowed to start once the sort has
 int launch_fill(const FillArgs& f, cudaStream_t s) {
     const long long chunks = fill_chunks(f);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)std::min((chunks + FILL_TPB / 32 - 1) / (FILL_TPB / 32), (long long)EXTENT_LIMIT));
-    cfg.blockDim = dim3(FILL_TPB);
-    cfg.stream = s;
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    TRAIN_LAUNCH(cudaLaunchKernelEx(&cfg, k_fill, f));
+    TRAIN_LAUNCH(launch_early(k_fill, (unsigned)std::min((chunks + FILL_TPB / 32 - 1) / (FILL_TPB / 32), (long long)EXTENT_LIMIT),
+                              FILL_TPB, 0, s, f));
     return ISO_OK;
 }
 
@@ -713,10 +708,11 @@ int32_t iso_embed_grad(const iso_mat* dY, const void* ids, int32_t ids_i64, int6
         using T = std::remove_pointer_t<decltype(tp)>;
         using O = std::remove_pointer_t<decltype(op)>;
         constexpr bool VEC = decltype(v)::value;
-        TRAIN_LAUNCH((k_row_sums<T, O, VEC><<<sums_grid, SUM_TPB, 0, s>>>(
-            static_cast<const T*>(dY->data), dY->ld, static_cast<O*>(grad->data), grad->ld, ra)));
+        TRAIN_LAUNCH(launch_early(k_row_sums<T, O, VEC>, (unsigned)sums_grid, SUM_TPB, 0, s, static_cast<const T*>(dY->data),
+                                  dY->ld, static_cast<O*>(grad->data), grad->ld, ra));
         if (wins > 1)
-            TRAIN_LAUNCH((k_row_join<O><<<join_grid, JOIN_TPB, 0, s>>>(static_cast<O*>(grad->data), grad->ld, ra)));
+            TRAIN_LAUNCH(launch_early(k_row_join<O>, (unsigned)join_grid, JOIN_TPB, 0, s, static_cast<O*>(grad->data),
+                                      grad->ld, ra));
         return ISO_OK;
     });
 }

@@ -107,6 +107,27 @@ inline bool rows_aligned(const iso_mat* m) {
 // SMs of the current device (queried once per device)
 int train_sms();
 
+// A kernel that may be launched while the one before it on the stream still
+// runs; it calls wait_before (below) ahead of its first access to memory.  The
+// one before lets it start early by calling start_next, which says nothing
+// about its own work being done.
+template <typename... P, typename... A>
+cudaError_t launch_early(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, cudaStream_t s, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+__device__ __forceinline__ void wait_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void start_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // The weight gradient's bf16 operands, in one kernel (iso_act.cu): x (rows of
 // ldx) <- the values of pack; with dy, parts (WGRAD_PARTS or 1 matrices of
 // rows x ldd) <- dY.  ldx and ldd are multiples of 8.

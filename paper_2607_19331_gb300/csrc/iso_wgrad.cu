@@ -325,7 +325,8 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
     cluster_barrier();
     tc_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(tmem_slot);
-    asm volatile("griddepcontrol.wait;" ::: "memory");     // the operands are written by the kernel before
+    start_next();
+    wait_before();           // the operands are written by the kernel before
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const int items = g.m_tiles * g.n_tiles * g.split;
 
@@ -549,6 +550,7 @@ __global__ void __launch_bounds__(FEW_TPB) k_wgrad_few(const T* dy, long long ld
 template <typename O, bool VEC>
 __global__ void __launch_bounds__(256) k_wgrad_join(const float* part, long long ld_part, int split, int M, int N,
                                                     O* out, long long ldo, int accumulate) {
+    wait_before();
     const int segs = (N + 7) / 8;
     const long long n = (long long)M * segs;
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
@@ -657,17 +659,7 @@ template <int BN>
 int launch_wgrad(const WgradMaps& maps, const WgradArgs& g, int items, cudaStream_t s) {
     const int pairs = resident_pairs<BN>();
     if (pairs <= 0) return ISO_ERR_CUDA;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(2 * std::min(items, pairs)));
-    cfg.blockDim = dim3(WG_THREADS);
-    cfg.dynamicSmemBytes = WgTile<BN>::SMEM;
-    cfg.stream = s;
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    TRAIN_LAUNCH(cudaLaunchKernelEx(&cfg, k_wgrad<BN>, maps, g));
+    TRAIN_LAUNCH(launch_early(k_wgrad<BN>, (unsigned)(2 * std::min(items, pairs)), WG_THREADS, WgTile<BN>::SMEM, s, maps, g));
     return ISO_OK;
 }
 
@@ -821,12 +813,8 @@ int32_t iso_act_wgrad(const iso_mat* dY, const iso_act* pack, const iso_mat* out
     return by_dtype(out->dtype, [&](auto* op) -> int {
         using O = std::remove_pointer_t<decltype(op)>;
         const int grid = (int)std::min((M * ((N + 7) / 8) + 255) / 256, (long long)EXTENT_LIMIT);
-        if (g.out_vec)
-            TRAIN_LAUNCH((k_wgrad_join<O, true><<<grid, 256, 0, s>>>(parts, p.ld_part, g.split, g.M, g.N,
-                                                                    static_cast<O*>(out->data), out->ld, accumulate)));
-        else
-            TRAIN_LAUNCH((k_wgrad_join<O, false><<<grid, 256, 0, s>>>(parts, p.ld_part, g.split, g.M, g.N,
-                                                                     static_cast<O*>(out->data), out->ld, accumulate)));
+        TRAIN_LAUNCH(launch_early(g.out_vec ? k_wgrad_join<O, true> : k_wgrad_join<O, false>, (unsigned)grid, 256u, 0, s,
+                                  parts, p.ld_part, g.split, g.M, g.N, static_cast<O*>(out->data), out->ld, accumulate));
         return ISO_OK;
     });
 }
