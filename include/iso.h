@@ -529,8 +529,8 @@ int32_t iso_embed(const iso_mat* table, const void* ids, int32_t ids_i64, int64_
  * rows without tokens; with accumulate = 1 that sum is added to grad, rows
  * without tokens unchanged.  dY n x cols; grad table rows x cols, BF16 or
  * F32.  Tokens are sorted by id and each row's sum is binary32 in an order
- * that depends on the ids alone, so equal inputs give equal bits; one rounding
- * to grad's type.  grad overlaps neither dY nor ids.  An empty grad:
+ * that depends on the ids and the sizes alone, so equal inputs give equal bits;
+ * one rounding to grad's type.  grad overlaps neither dY nor ids.  An empty grad:
  * nothing is read, and no id is reported. */
 int32_t iso_embed_grad_workspace_size(int64_t n, int64_t cols, size_t* bytes);
 int32_t iso_embed_grad(const iso_mat* dY, const void* ids, int32_t ids_i64, int64_t pad_id, float scale,
