@@ -424,6 +424,26 @@ def test_another_stream_and_capture():
     assert torch.equal(out, iso.act_wgrad(dy, iso.act_pack(x)))
 
 
+def test_both_forms_of_a_call_agree():
+    """A call that allocates its outputs and one that is given them."""
+    def new(*shape, dtype=BF):
+        return torch.empty(*shape, dtype=dtype, device=DEV)
+    x, y, dy = _act(75, 40, 136, BF), _act(76, 40, 136, BF), _act(77, 40, 56, BF)
+    ids, table = _ids(78, 40, 90, False, 89), _act(79, 90, 136, BF)
+    p, q = iso.act_pack(x), iso.act_pack(x, out=iso.ActPack.empty(40, 136))
+    assert torch.equal(p.codes, q.codes) and torch.equal(p.exps[:, :5], q.exps[:, :5]) and p.shape == q.shape == (40, 136)
+    assert torch.equal(iso.act_unpack(p), iso.act_unpack(q, out=new(40, 136)))
+    assert torch.equal(iso.act_wgrad(dy, p, dtype=BF), iso.act_wgrad(dy, q, out=new(56, 136)))
+    h, a, b = iso.swiglu_pack(x, y)
+    h2, a2, b2 = iso.swiglu_pack(x, y, out=new(40, 136), packs=(iso.ActPack.empty(40, 136), iso.ActPack.empty(40, 136)))
+    assert torch.equal(h, h2) and torch.equal(a.codes, a2.codes) and torch.equal(b.codes, b2.codes)
+    for u, v in zip(iso.swiglu_grad(x, a, b), iso.swiglu_grad(x, a2, b2, out=[new(40, 136) for _ in range(3)])):
+        assert torch.equal(u, v)
+    assert torch.equal(iso.embed(table, ids, 2.0, 89), iso.embed(table, ids, 2.0, 89, out=new(40, 136)))
+    assert torch.equal(iso.embed_grad(x, ids, 90, 2.0, 89),
+                       iso.embed_grad(x, ids, scale=2.0, pad_id=89, out=new(90, 136, dtype=F32)))
+
+
 def test_refusals():
     x, dy = _act(81, 8, 64, BF), _act(82, 8, 32, BF)
     p = iso.act_pack(x)
