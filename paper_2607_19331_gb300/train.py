@@ -89,18 +89,12 @@ def _here(first: torch.Tensor, *rest: Optional[torch.Tensor]) -> int:
     return _raw_stream(index)
 
 
-_workspaces = {}
-
-
-def _scratch(ws: Optional[Workspace], device: torch.device, s: int) -> Workspace:
-    """The caller's workspace, or a default one of the call's own stream (calls
-    on different streams may overlap and must not share scratch)."""
-    if ws is None:
-        key = (device.index, s)
-        ws = _workspaces.get(key)
-        if ws is None:
-            ws = _workspaces[key] = Workspace(device)
-    return ws
+def _scratch(ws: Optional[Workspace], device: torch.device) -> Workspace:
+    """The caller's workspace, or one for this call alone, from torch's allocator
+    on the current stream: calls of several threads on one stream may interleave
+    their launches, and a captured call's scratch belongs to its graph.  To be
+    held until the call is enqueued."""
+    return Workspace(device) if ws is None else ws
 
 
 def _done(result, where: str):
@@ -277,16 +271,11 @@ def act_wgrad(dy: torch.Tensor, pack: ActPack, out: Optional[torch.Tensor] = Non
         if dtype is not None and out.dtype != dtype:
             raise TypeError(f"out is {out.dtype}, dtype asks for {dtype}")
         do = _mat(out, "out")
-    ws = _scratch(workspace, dy.device, s)
+    ws = _scratch(workspace, dy.device)
     st = _status(status, dy.device)
-    L, args = lib(), (_byref(dd), _byref(pack._abi), _byref(do))
-    acc = 1 if accumulate else 0
-    rc = L.iso_act_wgrad(*args, acc, *ws.get(0), _ptr(st), s)
-    if rc == _abi.ISO_ERR_WORKSPACE:          # nothing was enqueued: grow the scratch to what the call needs
-        nb = ctypes.c_size_t(0)
-        check(L.iso_act_wgrad_workspace_size(*args, _byref(nb)), "iso_act_wgrad")
-        rc = L.iso_act_wgrad(*args, acc, *ws.get(nb.value), _ptr(st), s)
-    check(rc, "iso_act_wgrad")
+    L, args, nb = lib(), (_byref(dd), _byref(pack._abi), _byref(do)), ctypes.c_size_t(0)
+    check(L.iso_act_wgrad_workspace_size(*args, _byref(nb)), "iso_act_wgrad")
+    check(L.iso_act_wgrad(*args, 1 if accumulate else 0, *ws.get(nb.value), _ptr(st), s), "iso_act_wgrad")
     return (out, st) if status else out
 
 
@@ -437,7 +426,8 @@ def embed_grad(dy: torch.Tensor, ids: torch.Tensor, rows: Optional[int] = None, 
         if dtype is not None and out.dtype != dtype:
             raise TypeError(f"out is {out.dtype}, dtype asks for {dtype}")
         do = _mat(out, "out")
-    wptr, wlen = _scratch(workspace, dy.device, s).get(embed_grad_workspace_size(n, dd.cols))
+    ws = _scratch(workspace, dy.device)
+    wptr, wlen = ws.get(embed_grad_workspace_size(n, dd.cols))
     st = _status(status, dy.device)
     check(lib().iso_embed_grad(_byref(dd), ptr, i64, -1 if pad_id is None else int(pad_id), _scale(scale),
                                _byref(do), 1 if accumulate else 0, wptr, wlen, _ptr(st), s), "iso_embed_grad")

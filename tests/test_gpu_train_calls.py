@@ -1,0 +1,96 @@
+"""How the training-step calls live with a program around them, on the GPU:
+captured in graphs and made by several threads, without a workspace of the
+caller's."""
+import threading
+
+import pytest
+import torch
+
+import paper_2607_19331_gb300 as iso
+from paper_2607_19331_gb300 import _abi
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _cuda():
+    assert torch.cuda.is_available(), "GPU tests need CUDA"
+    torch.cuda.set_device(0)
+    _abi.lib()
+
+
+def _rand(seed, *shape, dtype=BF):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed)).to(DEV, dtype)
+
+
+def test_capture_without_a_workspace():
+    """A replay after a larger call on the captured stream: right results, and
+    nothing written outside the graph's own memory."""
+    x, dy = _rand(1, 700, 256), _rand(2, 700, 384)
+    ids = torch.randint(0, 5000, (700,), generator=torch.Generator().manual_seed(3)).to(DEV)
+    p = iso.act_pack(x)
+    want = iso.act_wgrad(dy, p), iso.embed_grad(dy, ids, 5000)
+    out, grad = torch.empty_like(want[0]), torch.empty_like(want[1])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+
+    def calls():
+        iso.act_wgrad(dy, p, out=out)
+        iso.embed_grad(dy, ids, out=grad)
+    with torch.cuda.stream(s):
+        calls()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            calls()
+        # larger calls on the same stream, then tensors in whatever memory is free now
+        big = _rand(4, 6000, 512)
+        iso.act_wgrad(_rand(5, 6000, 640, dtype=F32), iso.act_pack(big), out=torch.empty(640, 512, device=DEV))
+        iso.embed_grad(big, torch.zeros(6000, dtype=torch.int64, device=DEV), out=torch.empty(10, 512, device=DEV))
+        others = [torch.full((n,), 7, dtype=torch.uint8, device=DEV) for n in [1 << 20] * 64 + [4 << 20] * 16]
+        out.zero_()
+        grad.fill_(9.0)
+        g.replay()
+        g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want[0]) and torch.equal(grad, want[1])
+    assert all(bool((t == 7).all()) for t in others)
+
+
+def test_threads_accumulating_on_one_stream():
+    """Four threads, each with inputs and gradients of its own, all on the
+    default stream."""
+    n = 4
+    x = [_rand(10 + i, 400, 320) for i in range(n)]
+    dy = [_rand(20 + i, 400, 192, dtype=F32) for i in range(n)]
+    ids = [torch.randint(0, 300, (400,), generator=torch.Generator().manual_seed(30 + i)).to(DEV) for i in range(n)]
+    packs = [iso.act_pack(t) for t in x]
+    want = []
+    for i in range(n):
+        G, E = torch.zeros(192, 320, device=DEV), torch.zeros(300, 192, device=DEV)
+        for _ in range(20):
+            iso.act_wgrad(dy[i], packs[i], out=G, accumulate=True)
+            iso.embed_grad(dy[i], ids[i], out=E, accumulate=True)
+        want.append((G, E))
+    got = [(torch.zeros(192, 320, device=DEV), torch.zeros(300, 192, device=DEV)) for _ in range(n)]
+    torch.cuda.synchronize()
+    start, failed = threading.Barrier(n, timeout=60), []
+
+    def work(i):
+        try:
+            torch.cuda.set_device(0)
+            start.wait()
+            for _ in range(20):
+                iso.act_wgrad(dy[i], packs[i], out=got[i][0], accumulate=True)
+                iso.embed_grad(dy[i], ids[i], out=got[i][1], accumulate=True)
+        except BaseException as e:        # noqa: BLE001
+            failed.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(n)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    torch.cuda.synchronize()
+    assert not failed
+    for (G, E), (wG, wE) in zip(got, want):
+        assert torch.equal(G, wG) and torch.equal(E, wE)

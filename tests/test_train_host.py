@@ -1,0 +1,96 @@
+"""Host side of the training-step binding, without a GPU: what a call does
+around the library, against a fake of the library's entry points."""
+import threading
+
+import pytest
+import torch
+
+import paper_2607_19331_gb300 as iso
+from paper_2607_19331_gb300 import _abi, train
+from paper_2607_19331_gb300._abi import IsoMat
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture
+def on_host(monkeypatch):
+    """CPU tensors pass as the binding's matrices and ids; returns the function
+    that puts a fake in the library's place."""
+    def mat(t, name):
+        return IsoMat(t.data_ptr(), t.shape[0], t.shape[1], t.stride(0), train._CODES[t.dtype], 0)
+    monkeypatch.setattr(train, "_mat", mat)
+    monkeypatch.setattr(train, "_here", lambda *t: 7)
+    monkeypatch.setattr(train, "_ids", lambda ids: (ids.data_ptr(), 1, ids.numel()))
+    monkeypatch.setattr(train, "embed_grad_workspace_size", lambda n, cols: 4096)
+    return lambda fake: monkeypatch.setattr(train, "lib", lambda: fake)
+
+
+class FakeLibrary:
+    """Records the scratch that each call is given; with ``calls`` of two, the
+    first call waits inside the library until the second one is inside too."""
+
+    def __init__(self, calls=1):
+        self.scratch, self.both = [], threading.Barrier(calls, timeout=20)
+
+    def iso_act_wgrad_workspace_size(self, dy, pack, out, nb):
+        nb._obj.value = 4096
+        return _abi.ISO_OK
+
+    def _inside(self, ptr, size):
+        if size < 4096:
+            return _abi.ISO_ERR_WORKSPACE
+        self.scratch.append((ptr.value, ptr.value + 4096))
+        self.both.wait()
+        return _abi.ISO_OK
+
+    def iso_act_wgrad(self, dy, pack, out, acc, ptr, size, status, stream):
+        return self._inside(ptr, size)
+
+    def iso_embed_grad(self, dy, ids, i64, pad, scale, grad, acc, ptr, size, status, stream):
+        return self._inside(ptr, size)
+
+
+@pytest.mark.parametrize("name", ["act_wgrad", "embed_grad"])
+def test_calls_of_two_threads_on_one_stream_do_not_share_scratch(on_host, name):
+    dy, out, ids = torch.zeros(40, 8), torch.zeros(8, 64), torch.zeros(40, dtype=torch.int64)
+    buf = torch.zeros(40 * 72, dtype=torch.uint8)
+    pack = iso.ActPack._of((buf, buf.data_ptr(), buf.data_ptr() + 40 * 64, 40, 64, 64, 8), BF)
+    grad, failed = torch.zeros(9, 8), []
+
+    def call():
+        try:
+            if name == "act_wgrad":
+                iso.act_wgrad(dy, pack, out=out, accumulate=True)
+            else:
+                iso.embed_grad(dy, ids, out=grad, accumulate=True)
+        except BaseException as e:        # noqa: BLE001
+            failed.append(e)
+    on_host(FakeLibrary())
+    call()                                # what a first call keeps, if it keeps anything
+    fake = FakeLibrary(calls=2)
+    on_host(fake)
+    threads = [threading.Thread(target=call) for _ in range(2)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    assert not failed
+    (a0, a1), (b0, b1) = fake.scratch
+    assert a1 <= b0 or b1 <= a0
+
+
+def test_a_call_leaves_no_scratch_behind(on_host, monkeypatch):
+    """Scratch that outlives its call would be written by the replay of a graph
+    that captured the call, whoever has the memory by then."""
+    import weakref
+    made, real = [], train.Workspace
+
+    class Recorded(real):
+        def __init__(self, device=None):
+            super().__init__(device)
+            made.append(weakref.ref(self))
+    monkeypatch.setattr(train, "Workspace", Recorded)
+    on_host(FakeLibrary())
+    iso.embed_grad(torch.zeros(40, 8), torch.zeros(40, dtype=torch.int64), out=torch.zeros(9, 8))
+    assert len(made) == 1 and made[0]() is None
+    mine = Recorded("cpu")                # the caller's own is used as it is
+    iso.embed_grad(torch.zeros(40, 8), torch.zeros(40, dtype=torch.int64), out=torch.zeros(9, 8), workspace=mine)
+    assert len(made) == 2 and mine.buf.numel() >= 4096
