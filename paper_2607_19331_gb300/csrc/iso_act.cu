@@ -231,17 +231,11 @@ __global__ void __launch_bounds__(ACT_TPB) k_wgrad_operands(ActView in, int cols
     }
 }
 
-// x / (1 + exp(-x)).  bfloat16 outputs take the fast exponential and
-// reciprocal (a few binary32 ulps, 1.2 more for every unit of |x|; a bfloat16
-// ulp is 2^16 of them), binary32 outputs CUDA's expf and an IEEE division.
-template <typename T>
-__device__ __forceinline__ float silu(float x) {
-    if (sizeof(T) == 2) return __fdividef(x, 1.0f + __expf(-x));
-    const float e = expf(-fabsf(x)), r = __fdiv_rn(1.0f, 1.0f + e);
-    return x * (x < 0.0f ? e * r : r);
-}
 // s = 1 / (1 + exp(-x)) and 1 - s, both without cancellation and down to the
-// subnormals: with e = exp(-|x|) they are 1 / (1 + e) and e / (1 + e).
+// subnormals: with e = exp(-|x|) they are 1 / (1 + e) and e / (1 + e), the
+// divisor in [1, 2].  bfloat16 outputs take the fast exponential and reciprocal
+// (a few binary32 ulps, 1.2 more for every unit of |x|; a bfloat16 ulp is 2^16
+// of them), binary32 outputs CUDA's expf and an IEEE division.
 template <typename T>
 __device__ __forceinline__ void sigmoid(float x, float& s, float& rest) {
     const float e = sizeof(T) == 2 ? __expf(-fabsf(x)) : expf(-fabsf(x));
@@ -249,6 +243,14 @@ __device__ __forceinline__ void sigmoid(float x, float& s, float& rest) {
     const float er = e * r;
     s = x < 0.0f ? er : r;
     rest = x < 0.0f ? r : er;
+}
+// x s.  (As x / (1 + exp(-x)) in one fast division it was 0 below x = -87.3,
+// where the divisor passes 2^126 and x s is still a normal number.)
+template <typename T>
+__device__ __forceinline__ float silu(float x) {
+    float s, rest;
+    sigmoid<T>(x, s, rest);
+    return x * s;
 }
 
 template <typename T, bool VEC>
