@@ -104,6 +104,21 @@ inline bool rows_aligned(const iso_mat* m) {
            ((reinterpret_cast<uintptr_t>(m->data) & 15u) == 0 && (m->rows == 1 || (m->ld * elem_size(m->dtype)) % 16 == 0));
 }
 
+// The clock of a bounded wait: look() at the time now (ns) says whether the wait
+// has lasted longer than its limit.  The GPU's timer runs on while another
+// process has the GPU, so the time between two looks counts WAIT_GAP_NS at most:
+// a kernel that was away does not give up when it comes back.  (Looks are
+// microseconds apart; 2 s take a hundred of the longest gaps.)
+constexpr uint64_t WAIT_GAP_NS = 20000000;
+struct WaitClock {
+    uint64_t last = 0, waited = 0;
+    __host__ __device__ __forceinline__ bool look(uint64_t now, uint64_t limit_ns) {
+        if (last) waited += now - last < WAIT_GAP_NS ? now - last : WAIT_GAP_NS;
+        last = now;
+        return waited > limit_ns;
+    }
+};
+
 // SMs of the current device (queried once per device)
 int train_sms();
 

@@ -156,15 +156,12 @@ __device__ __forceinline__ uint64_t now_ns() {
 // Bounded wait: false after limit_ns, or MBAR_SPIN_LIMIT probes.  The probe
 // without a time hint measured 2 % faster on the whole product than with one;
 // it may suspend the thread for a time of the hardware's choosing, so the
-// bound is on the clock as well.
+// bound is on the clock as well (WaitClock).
 __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, uint64_t limit_ns, volatile int* abort_flag) {
-    uint64_t t0 = 0;
+    WaitClock clock;
     for (int spin = 0; spin < MBAR_SPIN_LIMIT; ++spin) {
         if (try_wait_cluster(bar, parity)) return true;
-        if ((spin & 31) == 31) {
-            if (t0 == 0) t0 = now_ns();
-            if ((abort_flag && *abort_flag) || now_ns() - t0 > limit_ns) return false;
-        }
+        if ((spin & 31) == 31 && (clock.look(now_ns(), limit_ns) || (abort_flag && *abort_flag))) return false;
     }
     return false;
 }

@@ -1,5 +1,6 @@
 """Host side of the training-step binding, without a GPU: what a call does
 around the library, against a fake of the library's entry points."""
+import subprocess
 import threading
 
 import pytest
@@ -94,3 +95,40 @@ def test_a_call_leaves_no_scratch_behind(on_host, monkeypatch):
     mine = Recorded("cpu")                # the caller's own is used as it is
     iso.embed_grad(torch.zeros(40, 8), torch.zeros(40, dtype=torch.int64), out=torch.zeros(9, 8), workspace=mine)
     assert len(made) == 2 and mine.buf.numel() >= 4096
+
+
+CLOCK = r"""
+#include <cstdio>
+#include "iso_train.cuh"
+int main() {
+    const uint64_t MS = 1000000, LIMIT = 2000 * MS;
+    int bad = 0;
+    {   // a minute away between two looks, and again
+        iso::WaitClock c;
+        bad |= c.look(5, LIMIT);
+        for (int i = 1; i <= 50; ++i) bad |= c.look(5 + i * 60000 * MS, LIMIT);
+    }
+    {   // looks a millisecond apart: the limit is reached after 2 s and not before
+        iso::WaitClock c;
+        for (int i = 0; i <= 2000; ++i) bad |= c.look(7 + i * MS, LIMIT);
+        bad |= !c.look(7 + 2001 * MS, LIMIT) << 1;
+    }
+    {   // always away: the wait still ends
+        iso::WaitClock c;
+        int looks = 0;
+        while (looks < 1000 && !c.look(1 + (uint64_t)looks * 1000 * MS, LIMIT)) ++looks;
+        bad |= (looks >= 1000) << 2;
+    }
+    std::printf("%d\n", bad);
+    return bad;
+}
+"""
+
+
+def test_a_wait_does_not_count_the_time_another_process_had_the_gpu(tmp_path):
+    from paper_2607_19331_gb300 import build
+    (tmp_path / "clock.cu").write_text(CLOCK)
+    exe = str(tmp_path / "clock")
+    subprocess.run([build.nvcc(), *build.ARCH, *build.FLAGS, "-o", exe, str(tmp_path / "clock.cu")], check=True)
+    run = subprocess.run([exe], capture_output=True, text=True)
+    assert run.returncode == 0, run.stdout
