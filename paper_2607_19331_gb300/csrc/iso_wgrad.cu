@@ -77,6 +77,8 @@ constexpr long long WG_FEW_WORK = 1LL << 28;
 constexpr int FEW_TPB = 128, FEW_WARPS = FEW_TPB / 32, FEW_ROWS = 8;
 constexpr int WG_SPLIT_STEPS = 4;          // a part of the tokens has this many steps at least
 constexpr int WG_BAND = 8;                 // tile rows that are walked together
+constexpr uint64_t WG_WAIT_NS = 2000000000;    // a wait gives up after this long
+constexpr uint64_t WG_LAND_NS = 1000000;       // time given to copies in flight after a give-up
 
 struct WgradArgs {
     int32_t M, N;
@@ -138,6 +140,10 @@ __device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                  :: "r"(bar), "h"((uint16_t)3) : "memory");
 }
+// the same, on a barrier of this CTA alone
+__device__ __forceinline__ void umma_commit_here(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
 __device__ __forceinline__ void arrive_cluster(uint32_t cluster_bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(cluster_bar) : "memory");
 }
@@ -168,7 +174,7 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, uint64_t
 // false once the limit is reached or another thread of the CTA gave up, which
 // then holds for the whole CTA
 __device__ __forceinline__ bool wait_pair(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-    if (wait_for(bar, parity, 2000000000ull, abort_flag)) return true;
+    if (wait_for(bar, parity, WG_WAIT_NS, abort_flag)) return true;
     *abort_flag = 1;
     return false;
 }
@@ -290,7 +296,7 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
         reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(wg_smem_raw) + 1023) & ~(uintptr_t)1023);
     uint64_t* const bars =
         reinterpret_cast<uint64_t*>(smem + STAGES * STAGE_BYTES + WG_EPI_WARPS * WG_OUT_BYTES);
-    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 4);
+    uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 5);
     volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cta_rank();
@@ -299,6 +305,7 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
     auto empty = [&](int s) { return bar + 8u * (STAGES + s); };           // products that read the stage are done
     auto acc_full = [&](int a) { return bar + 8u * (2 * STAGES + a); };    // accumulator complete
     auto acc_empty = [&](int a) { return bar + 8u * (2 * STAGES + 2 + a); };   // leader: accumulator read by all
+    const uint32_t all_done = bar + 8u * (2 * STAGES + 4);                     // leader: every product issued is done
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
@@ -309,6 +316,7 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
             mbar_init(acc_full(a), 1);
             mbar_init(acc_empty(a), 2 * WG_EPI_WARPS);
         }
+        mbar_init(all_done, 1);
         *abort_flag = 0;
         mbar_fence_init();
     }
@@ -355,11 +363,12 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
         }
         // every copy into this CTA has been consumed before it may exit: the
         // products that read a stage free it in both CTAs.  After a give-up the
-        // products may not come; the waits then only let the copies land.
+        // products may not come; the waits then let the copies land, which takes
+        // microseconds.
         for (uint32_t q = 0; q < min(done, (uint32_t)STAGES); ++q) {
             if (s == 0) { s = STAGES; ph ^= 1u; }
             --s;
-            wait_for(empty(s), ph ^ 1u, *abort_flag ? 1000000ull : 2000000000ull, nullptr);
+            if (!wait_for(empty(s), ph ^ 1u, WG_WAIT_NS, abort_flag)) wait_for(empty(s), ph ^ 1u, WG_LAND_NS, nullptr);
         }
     } else if (warp == WG_EPI_WARPS + 1 && lane == 0 && rank == 0) {
         // products of the pair, chain by chain
@@ -391,6 +400,9 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
                 if (acc == 0) acc_ph ^= 1u;
             }
         }
+        // no product runs on when the tensor memory is freed, after a give-up either
+        umma_commit_here(all_done);
+        wait_for(all_done, 0, WG_WAIT_NS, nullptr);
     } else if (warp < WG_EPI_WARPS) {
         // epilogue: warp w reads tensor-memory lanes 32 (w mod 4) ..., half of the columns
         const int quad = warp & 3, half = warp >> 2;
@@ -407,8 +419,9 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
                 for (int j = 0; j < 32; ++j) sum[c][j] = 0.0f;
             for (int kc = k0; kc < k1; kc += WG_CHAIN, ++n_acc) {
                 const int acc = n_acc & 1;
-                if (!wait_pair(acc_full(acc), (uint32_t)(n_acc >> 1) & 1u, abort_flag)) { ok = false; break; }
-                __syncwarp();
+                // one answer for the warp: loads of tensor memory take all of its lanes
+                ok = __all_sync(0xFFFFFFFFu, wait_pair(acc_full(acc), (uint32_t)(n_acc >> 1) & 1u, abort_flag));
+                if (!ok) break;
                 tc_after();
                 const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * BN + half * (BN / 2));
                 // 16 columns at a time: reading a chain's block in one go holds the next chain's
