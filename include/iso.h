@@ -81,7 +81,8 @@ typedef enum {
                                   a tensor with 2^32 or more entries, GLOBAL scope larger
                                   than the workspace allows */
     ISO_ERR_TIMEOUT = -9,      /* (device) a kernel's wait for its own bulk copies gave up
-                                  after its iteration limit; the outputs are unspecified */
+                                  after its limit; the outputs are unspecified unless the
+                                  call says otherwise */
     ISO_ERR_INDEX = -10        /* (device) a token id outside the embedding table that is not
                                   the padding id; that token counts as padding */
 } iso_status;
@@ -492,10 +493,17 @@ int32_t iso_act_unpack(const iso_act* pack, const iso_mat* out, void* stream);
  * when accumulating.  out may overlap neither input.  The products are exact
  * and sums are binary32.  The workspace is scratch of the size
  * iso_act_wgrad_workspace_size returns for the same arguments, 256-byte
- * aligned.  status (device, may be NULL): ISO_OK or ISO_ERR_TIMEOUT. */
+ * aligned.  status (device, may be NULL): ISO_OK or ISO_ERR_TIMEOUT; entries
+ * whose sums a give-up left unfinished are NaN, whether or not there is a
+ * status. */
 int32_t iso_act_wgrad_workspace_size(const iso_mat* dY, const iso_act* pack, const iso_mat* out, size_t* bytes);
 int32_t iso_act_wgrad(const iso_mat* dY, const iso_act* pack, const iso_mat* out, int32_t accumulate,
                       void* workspace, size_t ws_bytes, int32_t* status, void* stream);
+
+/* Diagnostics: the time after which a wait of iso_act_wgrad's kernel gives up,
+ * for the calls that follow (2 s; the time that another process has the GPU
+ * counts little).  ns < 0 changes nothing.  Returns the limit before the call. */
+int64_t iso_act_wgrad_wait_ns(int64_t ns);
 
 /* h = silu(gate) * up in binary32 from the inputs themselves, rounded once,
  * with both inputs kept as checkpoints, in one pass.  gate, up and h share

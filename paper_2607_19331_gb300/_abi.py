@@ -118,6 +118,7 @@ PROTOTYPES = [
     ("iso_act_unpack", I32, [PA, PM, P]),
     ("iso_act_wgrad_workspace_size", I32, [PM, PA, PM, ctypes.POINTER(SZ)]),
     ("iso_act_wgrad", I32, [PM, PA, PM, I32, P, SZ, P, P]),
+    ("iso_act_wgrad_wait_ns", I64, [I64]),
     ("iso_swiglu_pack", I32, [PM, PM, PM, PA, PA, P]),
     ("iso_swiglu_grad", I32, [PM, PA, PA, PM, PM, PM, P]),
     ("iso_embed", I32, [PM, P, I32, I64, I64, ctypes.c_float, PM, P, P]),

@@ -77,7 +77,8 @@ constexpr long long WG_FEW_WORK = 1LL << 28;
 constexpr int FEW_TPB = 128, FEW_WARPS = FEW_TPB / 32, FEW_ROWS = 8;
 constexpr int WG_SPLIT_STEPS = 4;          // a part of the tokens has this many steps at least
 constexpr int WG_BAND = 8;                 // tile rows that are walked together
-constexpr uint64_t WG_WAIT_NS = 2000000000;    // a wait gives up after this long
+constexpr uint64_t WG_WAIT_NS = 2000000000;    // a wait gives up after this long, unless told otherwise
+std::atomic<uint64_t> g_wait_ns{WG_WAIT_NS};
 constexpr uint64_t WG_LAND_NS = 1000000;       // time given to copies in flight after a give-up
 
 struct WgradArgs {
@@ -93,6 +94,7 @@ struct WgradArgs {
     int32_t out_vec;       // rows of G start on 16-byte boundaries
     int32_t out_copy;      // blocks leave by bulk copies (maps.out): rows so aligned, nothing to add to
     int32_t* status;
+    uint64_t wait_ns;      // limit of a wait for copies, products or accumulators
 };
 struct WgradMaps {
     CUtensorMap a[WG_MAX_PARTS], b;
@@ -173,8 +175,8 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, uint64_t
 }
 // false once the limit is reached or another thread of the CTA gave up, which
 // then holds for the whole CTA
-__device__ __forceinline__ bool wait_pair(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-    if (wait_for(bar, parity, WG_WAIT_NS, abort_flag)) return true;
+__device__ __forceinline__ bool wait_pair(uint32_t bar, uint32_t parity, uint64_t limit_ns, volatile int* abort_flag) {
+    if (wait_for(bar, parity, limit_ns, abort_flag)) return true;
     *abort_flag = 1;
     return false;
 }
@@ -347,7 +349,7 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
             n0 += (int)rank * (BN / 2);
             int p = k0 / g.t_tiles, t = (k0 - p * g.t_tiles) * WG_BK;
             for (int k = k0; k < k1; ++k) {
-                if (!wait_pair(empty(s), ph, abort_flag)) { ok = false; break; }
+                if (!wait_pair(empty(s), ph, g.wait_ns, abort_flag)) { ok = false; break; }
                 if (rank == 0) mbar_arrive_tx(full(s), 2 * STAGE_BYTES);
                 const CUtensorMap* am = &maps.a[p];
                 const uint32_t fb = full0 + 8u * s, a = st + s * STAGE_BYTES, b = a + WG_A_BYTES;
@@ -379,12 +381,12 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
             int m0, n0, k0, k1, part;
             work_item<BN>(g, i, m0, n0, k0, k1, part);
             for (int kc = k0; ok && kc < k1; kc += WG_CHAIN) {
-                if (!wait_pair(acc_empty(acc), acc_ph, abort_flag)) { ok = false; break; }
+                if (!wait_pair(acc_empty(acc), acc_ph, g.wait_ns, abort_flag)) { ok = false; break; }
                 tc_after();
                 const uint32_t d = tmem + acc * BN;
                 uint32_t more = 0;
                 for (int k = min(k1 - kc, WG_CHAIN); k > 0; --k) {
-                    if (!wait_pair(full(s), ph, abort_flag)) { ok = false; break; }
+                    if (!wait_pair(full(s), ph, g.wait_ns, abort_flag)) { ok = false; break; }
                     tc_after();
                     const uint32_t a = a0 + s * (STAGE_BYTES >> 4), b = b0 + s * (STAGE_BYTES >> 4);
 #pragma unroll
@@ -395,6 +397,7 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
                     umma_commit_pair(empty(s));
                     if (++s == STAGES) { s = 0; ph ^= 1u; }
                 }
+                if (!ok) break;                       // the accumulator is not complete
                 umma_commit_pair(acc_full(acc));
                 acc ^= 1u;
                 if (acc == 0) acc_ph ^= 1u;
@@ -409,7 +412,7 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
         float4* const buf = reinterpret_cast<float4*>(smem + STAGES * STAGE_BYTES + warp * WG_OUT_BYTES);
         int n_acc = 0;
         bool ok = true;
-        for (int i = pair; ok && i < items; i += pairs) {
+        for (int i = pair; i < items; i += pairs) {
             int m0, n0, k0, k1, part;
             work_item<BN>(g, i, m0, n0, k0, k1, part);
             float sum[Tile::BLOCKS][32];
@@ -417,10 +420,10 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
             for (int c = 0; c < Tile::BLOCKS; ++c)
 #pragma unroll
                 for (int j = 0; j < 32; ++j) sum[c][j] = 0.0f;
-            for (int kc = k0; kc < k1; kc += WG_CHAIN, ++n_acc) {
+            for (int kc = k0; ok && kc < k1; kc += WG_CHAIN, ++n_acc) {
                 const int acc = n_acc & 1;
                 // one answer for the warp: loads of tensor memory take all of its lanes
-                ok = __all_sync(0xFFFFFFFFu, wait_pair(acc_full(acc), (uint32_t)(n_acc >> 1) & 1u, abort_flag));
+                ok = __all_sync(0xFFFFFFFFu, wait_pair(acc_full(acc), (uint32_t)(n_acc >> 1) & 1u, g.wait_ns, abort_flag));
                 if (!ok) break;
                 tc_after();
                 const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * BN + half * (BN / 2));
@@ -438,7 +441,12 @@ k_wgrad(const __grid_constant__ WgradMaps maps, WgradArgs g) {
                 __syncwarp();
                 if (lane == 0) arrive_cluster(in_leader(acc_empty(acc)));
             }
-            if (!ok) break;
+            if (!ok) {       // blocks that a give-up left without their sums are NaN
+#pragma unroll
+                for (int c = 0; c < Tile::BLOCKS; ++c)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) sum[c][j] = __int_as_float(0x7FFFFFFF);
+            }
             const int m = m0 + (int)rank * 128 + quad * 32;
             if (m >= g.M) continue;
             if (g.out_copy) {
@@ -738,6 +746,11 @@ using namespace iso;
 
 extern "C" {
 
+int64_t iso_act_wgrad_wait_ns(int64_t ns) {
+    return (int64_t)(ns < 0 ? g_wait_ns.load(std::memory_order_relaxed)
+                            : g_wait_ns.exchange((uint64_t)ns, std::memory_order_relaxed));
+}
+
 int32_t iso_act_wgrad_workspace_size(const iso_mat* dY, const iso_act* pack, const iso_mat* out, size_t* bytes) {
     if (!bytes) return ISO_ERR_ARG;
     ISO_TRY(check_wgrad(dY, pack, out));
@@ -817,6 +830,7 @@ int32_t iso_act_wgrad(const iso_mat* dY, const iso_act* pack, const iso_mat* out
     else if (g.out_copy)
         ISO_TRY(out_map(&maps.out, out->data, out->dtype, M, N, out->ld, 1));
     g.status = status;
+    g.wait_ns = g_wait_ns.load(std::memory_order_relaxed);
     const int items = p.m_tiles * p.n_tiles * p.split;
     ISO_TRY(p.bn == 256 ? launch_wgrad<256>(maps, g, items, s) : launch_wgrad<128>(maps, g, items, s));
     if (p.split == 1) return ISO_OK;

@@ -94,3 +94,48 @@ def test_threads_accumulating_on_one_stream():
     assert not failed
     for (G, E), (wG, wE) in zip(got, want):
         assert torch.equal(G, wG) and torch.equal(E, wE)
+
+
+@pytest.fixture
+def no_patience():
+    """Waits of the weight gradient's kernel that give up at once: what the
+    hardware has not delivered by a wait's second look at the clock counts as
+    not coming."""
+    L = _abi.lib()
+    limit = L.iso_act_wgrad_wait_ns(0)
+    assert limit == 2_000_000_000 and L.iso_act_wgrad_wait_ns(-1) == 0
+    yield
+    torch.cuda.synchronize()
+    L.iso_act_wgrad_wait_ns(limit)
+
+
+GIVE_UPS = [
+    # tokens, M, N, dY, G: many tiles a CTA pair with several chains each, parts of the tokens, binary32 parts of dY
+    (2100, 5000, 4104, BF, F32), (2100, 5000, 4104, BF, BF), (8192, 256, 128, BF, F32), (8192, 1536, 1536, BF, BF),
+    (1500, 2000, 1000, F32, F32),
+]
+
+
+@pytest.mark.parametrize("T,M,N,dtype,out", GIVE_UPS)
+def test_a_give_up_leaves_sums_or_nan(no_patience, T, M, N, dtype, out):
+    x, dy = _rand(41, T, N), _rand(42, T, M, dtype=dtype)
+    p = iso.act_pack(x)
+    base = _rand(43, M, N, dtype=out)
+    _abi.lib().iso_act_wgrad_wait_ns(2_000_000_000)
+    want = iso.act_wgrad(dy, p, dtype=out), iso.act_wgrad(dy, p, out=base.clone(), accumulate=True)
+    assert not any(bool(w.isnan().any()) for w in want)
+    torch.cuda.synchronize()
+    _abi.lib().iso_act_wgrad_wait_ns(0)
+    gave_up = 0
+    for _ in range(5):
+        g, st = iso.act_wgrad(dy, p, dtype=out, status=True)
+        h = iso.act_wgrad(dy, p, out=base.clone(), accumulate=True)
+        silent = iso.act_wgrad(dy, p, dtype=out)          # no status: the gradient itself says it
+        for got, ref in ((g, want[0]), (h, want[1]), (silent, want[0])):
+            assert bool(((got == ref) | got.isnan()).all())
+        assert int(st) == (_abi.ISO_ERR_TIMEOUT if bool(g.isnan().any()) else _abi.ISO_OK)
+        gave_up += int(st) != 0
+    # whether a short call runs out is up to its copies' timing; a kernel of 100 us does
+    assert gave_up or T * M * N < 4e10
+    _abi.lib().iso_act_wgrad_wait_ns(2_000_000_000)
+    assert torch.equal(iso.act_wgrad(dy, p, dtype=out), want[0])
