@@ -62,7 +62,9 @@ constexpr long long FILL_WITH_SORT = (32 << 20) / FILL_CHUNK;
 constexpr int SUM_TPB = 128;
 constexpr int SUM_WPB = SUM_TPB / 32;
 constexpr int SUM_RING = 4096;                          // bytes of dY rows in flight per warp
-constexpr int SUM_WARPS_PER_SM = 24;                    // windows are as long as leaves this many warps a SM
+// Windows are as long as leaves this many warps: 24 for each of a GB300's 152
+// SMs.  A constant, whatever GPU runs: the order of the sums is the windows'.
+constexpr long long SUM_WARPS = 152 * 24;
 constexpr int WIN_MIN = 8, WIN_MAX = 256;
 // Up to this many tokens take k_grad_few.  Measured, it against the sort and
 // the rest: 1 token, 18992 x 192 f32 4.5 / 8.3 us, 151936 x 1536 bf16 63 / 67 us;
@@ -553,12 +555,12 @@ Bytes2D ids_bytes(const void* ids, int32_t i64, int64_t n) {
     return {reinterpret_cast<uintptr_t>(ids), n > 0 ? 1u : 0u, (uint64_t)n * (i64 ? 8 : 4), (uint64_t)n * (i64 ? 8 : 4)};
 }
 
-// Sorted tokens per window: short enough for SUM_WARPS_PER_SM warps a SM (one
-// wave of k_row_sums), within WIN_MIN .. WIN_MAX.
+// Sorted tokens per window: short enough for SUM_WARPS warps (one wave of
+// k_row_sums), within WIN_MIN .. WIN_MAX.
 int window_of(int64_t n, int64_t cols) {
-    const long long segs = (cols + TRAIN_SEG - 1) / TRAIN_SEG, warps = (long long)train_sms() * SUM_WARPS_PER_SM;
+    const long long segs = (cols + TRAIN_SEG - 1) / TRAIN_SEG;
     int win = WIN_MIN;
-    while (win < WIN_MAX && n * segs > warps * win) win *= 2;
+    while (win < WIN_MAX && n * segs > SUM_WARPS * win) win *= 2;
     return win;
 }
 

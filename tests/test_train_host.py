@@ -1,6 +1,8 @@
 """Host side of the training-step binding, without a GPU: what a call does
 around the library, against a fake of the library's entry points."""
+import os
 import subprocess
+import sys
 import threading
 
 import pytest
@@ -132,3 +134,34 @@ def test_a_wait_does_not_count_the_time_another_process_had_the_gpu(tmp_path):
     subprocess.run([build.nvcc(), *build.ARCH, *build.FLAGS, "-o", exe, str(tmp_path / "clock.cu")], check=True)
     run = subprocess.run([exe], capture_output=True, text=True)
     assert run.returncode == 0, run.stdout
+
+
+SMALL_GPU = r"""
+extern "C" int cudaGetDevice(int* d) { *d = 0; return 0; }
+extern "C" int cudaDeviceGetAttribute(int* v, int, int) { *v = 20; return 0; }
+"""
+SIZES = """
+import ctypes, sys
+L = ctypes.CDLL(sys.argv[1])
+nb = ctypes.c_size_t()
+for n, cols in ((33, 64), (4097, 72), (32768, 3584), (300000, 1536)):
+    assert L.iso_embed_grad_workspace_size(ctypes.c_int64(n), ctypes.c_int64(cols), ctypes.byref(nb)) == 0
+    print(nb.value)
+"""
+
+
+def test_the_embedding_gradients_windows_depend_on_the_sizes_alone(tmp_path):
+    """The order of its sums is that of its windows, and its workspace holds two
+    rows a window: the same on a device that reports 20 SMs."""
+    from paper_2607_19331_gb300 import build
+    lib = build.build()
+    (tmp_path / "gpu.cpp").write_text(SMALL_GPU)
+    shim = str(tmp_path / "gpu.so")
+    subprocess.run(["g++", "-shared", "-fPIC", "-o", shim, str(tmp_path / "gpu.cpp")], check=True)
+
+    def sizes(**env):
+        run = subprocess.run([sys.executable, "-c", SIZES, lib], capture_output=True, text=True,
+                             env={**os.environ, **env}, check=True)
+        return run.stdout.split()
+    here = sizes()
+    assert len(here) == 4 and sizes(LD_PRELOAD=shim) == here
