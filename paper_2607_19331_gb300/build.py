@@ -2,7 +2,9 @@
 module ``_iso_train`` that marshals torch tensors for the training-step calls.
 
 Each translation unit is compiled in parallel, then linked into a shared
-library next to this file under ``_build/``.  Nothing is installed.
+library next to this file under ``_build/``.  Nothing is installed.  The library
+takes nvcc alone; the host module takes g++ and torch, and is left out where
+there is no torch (the C ABI needs neither).
 """
 from __future__ import annotations
 
@@ -18,6 +20,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(BUILD, "libiso_gb300.so")
 BINDING = os.path.join(BUILD, "_iso_train.so")
+STAMP = os.path.join(BUILD, "_iso_train.txt")    # the torch that BINDING was built for, and its commands
 SOURCES = ["iso_api.cu", "iso_select.cu", "iso_apply.cu", "iso_merge.cu", "iso_block.cu", "iso_fused.cu",
            "iso_gemm.cu", "iso_frame.cu", "iso_range.cu", "iso_act.cu", "iso_wgrad.cu", "iso_embed.cu"]
 HEADERS = ["iso_internal.cuh", "iso_kernels.cuh", "iso_gemm.cuh", "iso_train.cuh"]
@@ -58,6 +61,27 @@ def _stale(target: str, deps) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def stamped_torch():
+    """The torch version that the host module was built for, or None."""
+    if not (os.path.exists(BINDING) and os.path.exists(STAMP)):
+        return None
+    with open(STAMP) as f:
+        return f.readline().strip()
+
+
+def _run(cmd) -> str:
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"compilation failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+    return r.stderr
+
+
+def _link(cmd, target: str) -> None:
+    tmp = target + f".tmp{os.getpid()}"
+    subprocess.check_call([*cmd, "-o", tmp])
+    os.replace(tmp, target)
+
+
 def build(force: bool = False, verbose: bool = False, extra=None) -> str:
     os.makedirs(BUILD, exist_ok=True)
     hdrs = [os.path.join(CSRC, h) for h in HEADERS] + [os.path.join(ROOT, "include", "iso.h")]
@@ -70,31 +94,34 @@ def build(force: bool = False, verbose: bool = False, extra=None) -> str:
             cmd = [nvcc(), *ARCH, *FLAGS, *(extra or []), "-c", s, "-o", o]
             jobs.append(cmd)
 
+    # the host module, again too where the torch or the commands are not those it was built with
     bobj = os.path.join(BUILD, "train_binding.o")
-    bcompile, blink = binding_commands(bobj)
-    bnew = force or _stale(bobj, [os.path.join(CSRC, "train_binding.cpp"), os.path.join(ROOT, "include", "iso.h")])
-    cu_jobs = len(jobs)
-    if bnew:
-        jobs.append(bcompile)
-
-    def run(cmd):
-        r = subprocess.run(cmd, capture_output=True, text=True)
-        if r.returncode != 0:
-            raise RuntimeError(f"compilation failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
-        return r.stderr
+    try:
+        import torch
+        bcompile, blink = binding_commands(bobj)
+        stamp = "\n".join([torch.__version__, " ".join(bcompile), " ".join(blink)]) + "\n"
+    except ImportError:
+        stamp = None
+    if stamp is not None:
+        bnew = force or _stale(bobj, [os.path.join(CSRC, "train_binding.cpp"), os.path.join(ROOT, "include", "iso.h")])
+        if not bnew:
+            bnew = not os.path.exists(STAMP) or open(STAMP).read() != stamp
 
     with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
-        for err in ex.map(run, jobs):
-            if verbose and err:
+        binding = ex.submit(_run, bcompile) if stamp is not None and bnew else None
+        errs = list(ex.map(_run, jobs))
+        if force or jobs or _stale(LIB, objs):
+            _link([nvcc(), *ARCH, "-shared", *objs, "-lcudart"], LIB)
+        if binding is not None:       # its failure comes after the library, which does not need it
+            errs.append(binding.result())
+    if verbose:
+        for err in errs:
+            if err:
                 print(err)
-    if force or cu_jobs or _stale(LIB, objs):
-        tmp = LIB + f".tmp{os.getpid()}"
-        subprocess.check_call([nvcc(), *ARCH, "-shared", "-o", tmp, *objs, "-lcudart"])
-        os.replace(tmp, LIB)
-    if bnew or _stale(BINDING, [bobj]):
-        tmp = BINDING + f".tmp{os.getpid()}"
-        subprocess.check_call([*blink, "-o", tmp])
-        os.replace(tmp, BINDING)
+    if stamp is not None and (bnew or _stale(BINDING, [bobj])):
+        _link(blink, BINDING)
+        with open(STAMP, "w") as f:
+            f.write(stamp)
     return LIB
 
 

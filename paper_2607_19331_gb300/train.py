@@ -16,12 +16,11 @@ import ctypes
 import functools
 import importlib.util
 import math
-import os
 from typing import Optional, Tuple
 
 import torch
 
-from . import _abi
+from . import _abi, build
 from ._abi import IsoAct, IsoMat, check, lib
 from .api import Workspace
 
@@ -32,14 +31,16 @@ _native = None
 
 
 def _load_native():
-    """The host module beside the loaded library; raises if it has not been built."""
+    """The host module beside the loaded library; raises if it has not been built,
+    or was built for another torch."""
     global _native
     if _native is None:
         lib()
-        path = os.path.join(os.path.dirname(_abi.LIB_PATH), "_iso_train.so")
-        if not os.path.exists(path):
-            raise RuntimeError(f"_iso_train not found at {path}: build it first "
-                               "(python -c 'import __graft_entry__ as g; g.build()')")
+        path, made_for = build.BINDING, build.stamped_torch()
+        if made_for != torch.__version__:
+            raise RuntimeError((f"_iso_train not found at {path}" if made_for is None else
+                                f"{path} was built for torch {made_for}, this is torch {torch.__version__}") +
+                               ": build it first (python -c 'import __graft_entry__ as g; g.build()')")
         spec = importlib.util.spec_from_file_location("_iso_train", path)
         mod = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(mod)

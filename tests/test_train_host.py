@@ -165,3 +165,65 @@ def test_the_embedding_gradients_windows_depend_on_the_sizes_alone(tmp_path):
         return run.stdout.split()
     here = sizes()
     assert len(here) == 4 and sizes(LD_PRELOAD=shim) == here
+
+
+@pytest.fixture
+def fake_build(monkeypatch, tmp_path):
+    """build.build() with a recorder in the compilers' place; a command whose
+    text holds ``fails`` fails."""
+    from paper_2607_19331_gb300 import build
+    ran, state = [], {"fails": None}
+
+    def run(cmd, **kw):
+        ran.append(cmd)
+        if state["fails"] and any(state["fails"] in c for c in cmd):
+            return subprocess.CompletedProcess(cmd, 1, "", "no")
+        out = cmd[cmd.index("-o") + 1]
+        with open(out, "w"):
+            pass
+        return subprocess.CompletedProcess(cmd, 0, "", "")
+    monkeypatch.setattr(build.subprocess, "run", run)
+    monkeypatch.setattr(build.subprocess, "check_call", lambda cmd: run(cmd))
+    for name in ("LIB", "BINDING", "STAMP"):
+        if hasattr(build, name):
+            monkeypatch.setattr(build, name, str(tmp_path / os.path.basename(getattr(build, name))))
+    monkeypatch.setattr(build, "BUILD", str(tmp_path))
+    return build, ran, state
+
+
+def test_the_library_builds_without_torch(fake_build, monkeypatch):
+    build, ran, _ = fake_build
+    monkeypatch.setitem(sys.modules, "torch", None)
+    assert os.path.exists(build.build())
+    assert all("nvcc" in cmd[0] for cmd in ran) and not os.path.exists(build.BINDING)
+
+
+def test_the_library_is_there_when_the_host_module_fails(fake_build):
+    build, ran, state = fake_build
+    state["fails"] = "train_binding.cpp"
+    with pytest.raises(RuntimeError, match="compilation failed"):
+        build.build()
+    assert os.path.exists(build.LIB) and not os.path.exists(build.BINDING)
+
+
+def test_the_host_module_follows_the_torch(fake_build, monkeypatch):
+    build, ran, _ = fake_build
+    build.build()
+    n = len(ran)
+    build.build()
+    assert len(ran) == n                                  # nothing to do
+    monkeypatch.setattr(torch, "__version__", "9.9.9")
+    build.build()
+    assert len(ran) == n + 2                              # its compilation and link, nothing else
+    build.build()
+    assert len(ran) == n + 2
+
+
+def test_a_host_module_of_another_torch_is_not_loaded(monkeypatch):
+    from paper_2607_19331_gb300 import build
+    build.build()
+    monkeypatch.setattr(train, "_native", None)
+    monkeypatch.setattr(torch, "__version__", "9.9.9")
+    with pytest.raises(RuntimeError, match="9.9.9"):
+        train._load_native()
+    assert train._native is None
