@@ -52,7 +52,9 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
 
 
 def _mat(t: torch.Tensor, name: str) -> IsoMat:
-    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a tensor")
+    if t.dim() != 2:
         raise ValueError(f"{name} must be a 2-D tensor")
     code = _CODES.get(t.dtype)
     if code is None:
@@ -362,6 +364,19 @@ def _scale(scale) -> float:
     return scale
 
 
+def _pad(pad_id: Optional[int]) -> int:
+    pad_id = -1 if pad_id is None else int(pad_id)
+    if not -1 << 63 <= pad_id < 1 << 63:
+        raise ValueError("pad_id must fit 64 bits")
+    return pad_id
+
+
+def _rows(rows) -> int:
+    if int(rows) < 0:
+        raise ValueError("rows must not be negative")
+    return int(rows)
+
+
 def embed(table: torch.Tensor, ids: torch.Tensor, scale=1.0, pad_id: Optional[int] = None,
           out: Optional[torch.Tensor] = None, dtype: Optional[torch.dtype] = None, status=False, stream=None):
     """scale * table[ids] (iso_embed), one row per id in ids' flat order, in the
@@ -369,7 +384,7 @@ def embed(table: torch.Tensor, ids: torch.Tensor, scale=1.0, pad_id: Optional[in
     the id is pad_id.  Other ids outside the table give zero rows and
     ISO_ERR_INDEX in the device status (returned with status=True)."""
     if out is None and stream is None and not status:
-        return _done((_native or _load_native()).embed(table, ids, _scale(scale), -1 if pad_id is None else int(pad_id),
+        return _done((_native or _load_native()).embed(table, ids, _scale(scale), _pad(pad_id),
                                                        dtype), "iso_embed")
     if stream is not None:
         with torch.cuda.stream(stream):
@@ -384,7 +399,7 @@ def embed(table: torch.Tensor, ids: torch.Tensor, scale=1.0, pad_id: Optional[in
             raise TypeError(f"out is {out.dtype}, dtype asks for {dtype}")
         do = _mat(out, "out")
     st = _status(status, table.device)
-    check(lib().iso_embed(_byref(dt), ptr, i64, n, -1 if pad_id is None else int(pad_id), _scale(scale), _byref(do),
+    check(lib().iso_embed(_byref(dt), ptr, i64, n, _pad(pad_id), _scale(scale), _byref(do),
                           _ptr(st), s), "iso_embed")
     return (out, st) if status else out
 
@@ -404,8 +419,8 @@ def embed_grad(dy: torch.Tensor, ids: torch.Tensor, rows: Optional[int] = None, 
     ``out`` with accumulate.  The same inputs give the same bits.  Returns it
     (and the device status with status=True)."""
     if out is None and rows is not None and stream is None and workspace is None and not status and not accumulate:
-        return _done((_native or _load_native()).embed_grad(dy, ids, int(rows), _scale(scale),
-                                                            -1 if pad_id is None else int(pad_id), dtype),
+        return _done((_native or _load_native()).embed_grad(dy, ids, _rows(rows), _scale(scale),
+                                                            _pad(pad_id), dtype),
                      "iso_embed_grad")
     if stream is not None:
         with torch.cuda.stream(stream):
@@ -420,7 +435,7 @@ def embed_grad(dy: torch.Tensor, ids: torch.Tensor, rows: Optional[int] = None, 
             raise ValueError("accumulate needs an out to add to")
         if rows is None:
             raise ValueError("embed_grad needs rows (the table's) or out")
-        out, do = _new(int(rows), dd.cols, dtype or torch.float32, dy.device)
+        out, do = _new(_rows(rows), dd.cols, dtype or torch.float32, dy.device)
     else:
         if rows is not None and out.shape[0] != rows:
             raise ValueError(f"out has {out.shape[0]} rows, rows is {rows}")
@@ -430,6 +445,6 @@ def embed_grad(dy: torch.Tensor, ids: torch.Tensor, rows: Optional[int] = None, 
     ws = _scratch(workspace, dy.device)
     wptr, wlen = ws.get(embed_grad_workspace_size(n, dd.cols))
     st = _status(status, dy.device)
-    check(lib().iso_embed_grad(_byref(dd), ptr, i64, -1 if pad_id is None else int(pad_id), _scale(scale),
+    check(lib().iso_embed_grad(_byref(dd), ptr, i64, _pad(pad_id), _scale(scale),
                                _byref(do), 1 if accumulate else 0, wptr, wlen, _ptr(st), s), "iso_embed_grad")
     return (out, st) if status else out

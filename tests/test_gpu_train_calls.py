@@ -139,3 +139,51 @@ def test_a_give_up_leaves_sums_or_nan(no_patience, T, M, N, dtype, out):
     assert gave_up or T * M * N < 4e10
     _abi.lib().iso_act_wgrad_wait_ns(2_000_000_000)
     assert torch.equal(iso.act_wgrad(dy, p, dtype=out), want[0])
+
+
+def _refusal(f):
+    try:
+        f()
+    except Exception as e:
+        return type(e), getattr(e, "code", None)
+    return None
+
+
+def test_both_forms_of_a_call_refuse_alike():
+    """The form that allocates its outputs and the one that is given them (or a
+    status, or a stream that is not the current one)."""
+    x, i8 = _rand(51, 8, 64), torch.zeros(8, dtype=torch.int64, device=DEV)
+    p, s = iso.act_pack(x), torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    out, f32 = torch.empty(8, 64, dtype=BF, device=DEV), torch.empty(64, 64, device=DEV)
+    packs = iso.ActPack.empty(8, 64), iso.ActPack.empty(8, 64)
+    bad = [None, [1.0], x.cpu(), x.half(), x[0], x.t(), x[:1].expand(8, 64)]
+    ids = [None, [1], i8.float(), i8.cpu(), torch.zeros(8, 2, dtype=torch.int64, device=DEV)[:, 0]]
+    pairs = []
+    for b in bad:
+        pairs += [(lambda b=b: iso.act_pack(b), lambda b=b: iso.act_pack(b, out=packs[0])),
+                  (lambda b=b: iso.act_wgrad(b, p), lambda b=b: iso.act_wgrad(b, p, out=f32)),
+                  (lambda b=b: iso.swiglu_pack(b, x), lambda b=b: iso.swiglu_pack(b, x, out=out)),
+                  (lambda b=b: iso.swiglu_pack(x, b), lambda b=b: iso.swiglu_pack(x, b, packs=packs)),
+                  (lambda b=b: iso.swiglu_grad(b, p, p), lambda b=b: iso.swiglu_grad(b, p, p, out=(out, out.clone(), out.clone()))),
+                  (lambda b=b: iso.embed(b, i8), lambda b=b: iso.embed(b, i8, status=True)),
+                  (lambda b=b: iso.embed_grad(b, i8, 9), lambda b=b: iso.embed_grad(b, i8, 9, status=True))]
+    for b in ids:
+        pairs += [(lambda b=b: iso.embed(x, b), lambda b=b: iso.embed(x, b, status=True)),
+                  (lambda b=b: iso.embed_grad(x, b, 9), lambda b=b: iso.embed_grad(x, b, 9, status=True))]
+    for b in [torch.float16, 5]:
+        pairs += [(lambda b=b: iso.embed(x, i8, dtype=b), lambda b=b: iso.embed(x, i8, dtype=b, status=True)),
+                  (lambda b=b: iso.act_wgrad(x, p, dtype=b), lambda b=b: iso.act_wgrad(x, p, dtype=b, status=True)),
+                  (lambda b=b: iso.embed_grad(x, i8, 9, dtype=b), lambda b=b: iso.embed_grad(x, i8, 9, dtype=b, status=True))]
+    for kw in [dict(pad_id=1 << 63), dict(pad_id="a"), dict(scale=float("inf")), dict(scale=1e39), dict(scale=None)]:
+        pairs += [(lambda kw=kw: iso.embed(x, i8, **kw), lambda kw=kw: iso.embed(x, i8, status=True, **kw)),
+                  (lambda kw=kw: iso.embed_grad(x, i8, 9, **kw), lambda kw=kw: iso.embed_grad(x, i8, 9, status=True, **kw))]
+    pairs += [(lambda: iso.embed_grad(x, i8, -1), lambda: iso.embed_grad(x, i8, -1, status=True)),
+              (lambda: iso.embed_grad(x, i8[:5], 9), lambda: iso.embed_grad(x, i8[:5], 9, status=True)),
+              (lambda: iso.act_wgrad(x[:7], p), lambda: iso.act_wgrad(x[:7], p, status=True)),
+              (lambda: iso.act_wgrad(x, x), lambda: iso.act_wgrad(x, x, status=True)),
+              (lambda: iso.swiglu_pack(x, x.float()), lambda: iso.swiglu_pack(x, x.float(), out=out)),
+              (lambda: iso.swiglu_grad(x[:, :32], p, p), lambda: iso.swiglu_grad(x[:, :32], p, p, out=(out[:, :32], out[:, 32:]), need_h=False))]
+    for n, (common, other) in enumerate(pairs):
+        a, b = _refusal(common), _refusal(other)
+        assert a is not None and a == b, (n, a, b)
