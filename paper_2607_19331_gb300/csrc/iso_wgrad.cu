@@ -9,18 +9,23 @@
 //              scales powers of two) into the workspace.  A bf16 dY is read in
 //              place when its rows start on 16-byte boundaries, else copied.
 //              A binary32 dY is split into three bf16 parts of eight
-//              significant bits each, hi + mid + lo = dY, and G is the sum of
-//              the three products; so every product is exact and sums are
-//              binary32.
+//              significant bits each, hi + mid + lo = dY (from 2^-110 up; a
+//              part's own last bit is 2^-133), and G is the sum of the three
+//              products; so every product is exact.
 //   k_wgrad    a pair of CTAs per 256 x 256 tile of G, 128 tokens per stage
 //              (32 KB of each operand per CTA, three stages; six stages of 64
 //              tokens have the same bytes in flight and measured 4 % slower,
 //              the waits and commits of a stage costing the same), persistent
-//              over the tiles.  The tensor cores' accumulation cuts low bits
-//              off at every product: the relative error of a binary32 G grows
-//              in proportion to the chain of products (1.1e-6, 4.4e-7 and
-//              2.0e-7 at chains of 4096, 2048 and 1024 tokens of 8192 random
-//              ones; a plain binary32 product has 3.1e-7).  So a chain is 1024 tokens; the epilogue warps add the
+//              over the tiles.  The tensor cores add sixteen products at a time
+//              and cut low bits off: measured, a product of 2^-25 beside a
+//              term of 1 counts, one of 2^-26 does not.  So the error of a
+//              binary32 G grows in proportion to the chain of products (1.1e-6,
+//              4.4e-7 and 2.0e-7 at chains of 4096, 2048 and 1024 tokens of
+//              8192 random ones; a plain binary32 product has 3.1e-7), and is
+//              largest where one large product comes before many small ones of
+//              one sign (1024 of 2^-27 after a 1: 7.6e-6, as a chain of
+//              binary32 additions has).  So a chain is 1024 tokens; the epilogue
+//              warps add the
 //              chains up in registers, 128 sums a thread, rounding to nearest,
 //              while the next chain runs in the other of two accumulators in
 //              tensor memory (chains of 2048 measured 1 % faster).

@@ -57,3 +57,48 @@ def test_swiglu_keeps_the_small_end_of_silu(dtype, up):
     _within(du, ru, tol(ru, gv, 1.0), "d_up")
     # s (1 + g (1 - s)): the terms are s and |g| s
     _within(dg, rg, tol(np.abs(uv) * R.sigmoid(gv) * (1 + np.abs(gv)), gv, abs(up)), "d_gate")
+
+
+# ---------------------------------------------------------------------------
+# weight gradient: operands whose errors do not average out
+# ---------------------------------------------------------------------------
+def _wgrad_bound(T, dtype, mag, x_mag):
+    """Inside the bound of include/iso.h: sixteen products at a time, each cut
+    below 2^-25 of the largest term, the running sum below 2^-23 of itself;
+    chains rounded."""
+    P = T if dtype == BF else 3 * T
+    return (min(P, 1024) * 5 * 2.0 ** -27 + (P / 1024 + 2) * U) * mag + (2.0 ** -133 * x_mag if dtype == F32 else 0)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T", [9, 100, 1024, 3000, 8192])
+@pytest.mark.parametrize("kind", ["one sign", 2.0 ** -20, 2.0 ** -25, 2.0 ** -26, 2.0 ** -30, "rising"])
+def test_wgrad_of_operands_of_one_sign(kind, T, dtype):
+    M, N, g = 264, 160, torch.Generator().manual_seed(1)
+    x = torch.ones(T, N)
+    if kind == "one sign":
+        dy, x = 0.5 + torch.rand(T, M, generator=g), 0.5 + torch.rand(T, N, generator=g)
+    elif kind == "rising":
+        dy = torch.exp2(torch.linspace(-30, 0, T))[:, None].expand(T, M).clone()
+    else:                                     # one large product, then small ones
+        dy = torch.full((T, M), kind)
+        dy[0] = 1.0
+    dy, p = dy.to(DEV, dtype), iso.act_pack(x.to(DEV, BF))
+    xh, d = _np(iso.act_unpack(p)), _np(dy)
+    ref = d.T @ xh
+    got = iso.act_wgrad(dy, p)
+    _within(got, ref, _wgrad_bound(T, dtype, d.T @ xh, xh.sum(0)) + U * ref, f"{kind}")
+    _within(iso.act_wgrad(-dy, p), -ref, _wgrad_bound(T, dtype, d.T @ xh, xh.sum(0)) + U * ref, f"-{kind}")
+
+
+@pytest.mark.parametrize("size", [2.0 ** -105, 2.0 ** -112, 2.0 ** -125, 2.0 ** -140])
+@pytest.mark.parametrize("T", [9, 40, 2000])
+def test_wgrad_of_tiny_gradients(T, size):
+    """A binary32 dY near and below the least normal number."""
+    g = torch.Generator().manual_seed(2)
+    dy = (torch.randn(T, 270, generator=g) * size).to(DEV)
+    p = iso.act_pack((torch.randn(T, 150, generator=g) * 2.0 ** 30).to(DEV))
+    xh, d = _np(iso.act_unpack(p, dtype=F32)), _np(dy)
+    mag, x_mag = np.abs(d).T @ np.abs(xh), np.abs(xh).sum(0)
+    ref = d.T @ xh
+    _within(iso.act_wgrad(dy, p), ref, _wgrad_bound(T, F32, mag, x_mag) + U * np.abs(ref) + 2.0 ** -149, f"{size}")
