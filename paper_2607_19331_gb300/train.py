@@ -5,10 +5,12 @@ and the token embedding with its gradient.
 Argument marshalling only, as in ``api``; every step of the computation runs in
 libiso_gb300.so.  The common form of a call (outputs allocated by it, on the
 current stream) is marshalled by the host module ``_iso_train``
-(csrc/train_binding.cpp), any other form here.  Matrices are 2-D CUDA tensors (tokens in rows), bfloat16 or
-float32, with unit stride along a row and any row stride.  Work is enqueued on
-``stream`` (default: the current stream), where tensors that a call allocates
-belong too; nothing waits for the device.
+(csrc/train_binding.cpp), any other form here.  Matrices are 2-D CUDA tensors
+(tokens in rows), bfloat16 or float32, with unit stride along a row and any row
+stride.  Work is enqueued on ``stream`` (default: the current stream), where
+tensors that a call allocates belong too; nothing waits for the device.  The
+calls stand outside autograd: inputs that require a gradient are taken as they
+are and results carry no graph; gradients come from the calls that name them.
 """
 from __future__ import annotations
 

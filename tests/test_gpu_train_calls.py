@@ -187,3 +187,10 @@ def test_both_forms_of_a_call_refuse_alike():
     for n, (common, other) in enumerate(pairs):
         a, b = _refusal(common), _refusal(other)
         assert a is not None and a == b, (n, a, b)
+
+
+def test_results_carry_no_graph():
+    table, i8 = torch.nn.Parameter(_rand(61, 20, 64)), torch.arange(8, device=DEV)
+    results = [iso.embed(table, i8), iso.embed(table, i8, status=True)[0], iso.act_unpack(iso.act_pack(table)),
+               iso.swiglu_pack(table, table)[0], iso.act_wgrad(table, iso.act_pack(table)), iso.embed_grad(table[:8], i8, 20)]
+    assert not any(t.requires_grad for t in results)
