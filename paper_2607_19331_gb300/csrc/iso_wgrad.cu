@@ -827,8 +827,11 @@ int32_t iso_act_wgrad(const iso_mat* dY, const iso_act* pack, const iso_mat* out
     g.ldo = out->ld;
     g.out_dtype = out->dtype;
     g.out_vec = rows_aligned(out);
-    // a bulk copy's rows are 16 bytes apart at least and start on such boundaries
-    g.out_copy = p.split > 1 || (!accumulate && g.out_vec && (out->ld * elem_size(out->dtype)) % 16 == 0);
+    // A bulk copy's rows start on 16-byte boundaries and end on them: at the last
+    // column it clips whole 16-byte words only, and what stands beside G in a
+    // wider buffer is not the call's to write.  (The parts' rows are padded.)
+    const int es = elem_size(out->dtype);
+    g.out_copy = p.split > 1 || (!accumulate && g.out_vec && (out->ld * es) % 16 == 0 && (N * es) % 16 == 0);
     float* const parts = reinterpret_cast<float*>(ws + p.parts);
     if (p.split > 1)
         ISO_TRY(out_map(&maps.out, parts, ISO_F32, M, N, p.ld_part, p.split));

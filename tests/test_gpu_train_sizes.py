@@ -60,6 +60,28 @@ def test_wgrad_of_many_tiles(T, M, N, dtype, out, accumulate):
     assert torch.equal(got, again)
 
 
+@pytest.mark.parametrize("out", [BF, F32])
+@pytest.mark.parametrize("T,M", [(5, 40), (40, 300), (700, 129)])
+@pytest.mark.parametrize("N", [1, 2, 3, 4, 5, 6, 7, 8, 31, 33, 127, 130, 254, 255, 257, 1022])
+def test_wgrad_writes_its_columns_alone(N, T, M, out):
+    """G as a range of columns of a wider buffer, its rows on 16-byte boundaries
+    or off them."""
+    x, dy = _rand(14, T, N), _rand(15, T, M)
+    p = iso.act_pack(x)
+    want = iso.act_wgrad(dy, p, dtype=out)
+    xh = iso.act_unpack(p, dtype=F32).double()
+    ref, mag = dy.double().t() @ xh, dy.double().abs().t() @ xh.abs()
+    eps = 4 * U * (8 + np.sqrt(T))
+    _within(want, ref, eps * mag + ROUND[out] * (1 + 2 * U) * (ref.abs() + eps * mag) + U * ref.abs() + 2.0 ** -126, "wgrad")
+    for ld, at in (((N + 15) // 8 * 8, 8), ((N + 15) // 8 * 8, 3), (N + 9, 8)):
+        buf = torch.full(((M + 1) * ld + 16,), -3.0, dtype=out, device=DEV)
+        view = torch.as_strided(buf, (M, N), (ld, 1), at)
+        iso.act_wgrad(dy, p, out=view)
+        assert torch.equal(view, want)
+        view.fill_(-3.0)
+        assert bool((buf == -3.0).all()), (ld, at)
+
+
 # ---------------------------------------------------------------------------
 # embedding gradient
 # ---------------------------------------------------------------------------
