@@ -500,9 +500,9 @@ int32_t iso_act_unpack(const iso_act* pack, const iso_mat* out, void* stream);
  * P the products of an entry: the tokens, three times as many for a binary32
  * dY.  (A chain of P rounded binary32 additions is bounded by P 2^-24.)  The
  * workspace is scratch of the size iso_act_wgrad_workspace_size returns for the
- * same arguments, 256-byte aligned.  status (device, may be NULL): ISO_OK or ISO_ERR_TIMEOUT; entries
- * whose sums a give-up left unfinished are NaN, whether or not there is a
- * status. */
+ * same arguments, 256-byte aligned.  status (device, may be NULL): ISO_OK or
+ * ISO_ERR_TIMEOUT; entries whose sums a give-up left unfinished are NaN, whether
+ * or not there is a status. */
 int32_t iso_act_wgrad_workspace_size(const iso_mat* dY, const iso_act* pack, const iso_mat* out, size_t* bytes);
 int32_t iso_act_wgrad(const iso_mat* dY, const iso_act* pack, const iso_mat* out, int32_t accumulate,
                       void* workspace, size_t ws_bytes, int32_t* status, void* stream);

@@ -105,7 +105,10 @@ def make_stats(tensors, K, topk: IsoTopkCfg, device, with_gram=True) -> Stats:
 
 
 class Workspace:
-    """Caller-owned scratch for the library, one growing torch buffer."""
+    """Caller-owned scratch for the library, one growing torch buffer.  A call of
+    this module without one uses one buffer per device, for calls of one thread
+    on one stream; calls of several threads or streams, and calls captured in a
+    graph, bring a workspace each."""
 
     def __init__(self, device=None):
         self.device = torch.device(device or "cuda")

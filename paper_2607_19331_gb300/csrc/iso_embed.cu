@@ -51,10 +51,12 @@ constexpr long long SORT_ONE_CTA = 2048;
 constexpr int SORT_SMEM = (SORT_WARPS * SORT_BINS + SORT_BINS + 32 + 4) * (int)sizeof(uint32_t);
 constexpr int FILL_TPB = 256;
 constexpr int FILL_CHUNK = 8192;                        // bytes of zeros a warp writes
-// Up to this many tokens are sorted by counting.  Measured, the accumulating
-// gradient of 152064 x 64 whole, that against the radix sort: 33 tokens 9.1 / 12.1
-// us, 100 tokens 11.0 / 14.2, 333 tokens 12.8 / 15.1, 512 tokens 15.0 / 15.8 (500
-// rows: 15.2 / 13.2).
+// Up to this many tokens are sorted by counting: the longest list at which that
+// led for every table.  Measured, the accumulating gradient of 64 columns whole,
+// that against the radix sort: 256 tokens of 500 rows (one pass) 11.5 / 12.5 us,
+// of 152064 rows (two) 11.5 / 14.8; 333 tokens 12.8 / 12.7 and 12.9 / 15.3; 512
+// tokens 15.3 / 13.5 and 15.2 / 16.4; 1000 tokens 30 / 16 and 29 / 19.  So where
+// the radix sort takes two passes the limit could be near 512.
 constexpr int SORT_RANK = 256;
 // Up to this many chunks the zeros ride along with the sort of one CTA: one launch
 // less (about 3 us of host time); 32 MB take about 5 us there.
