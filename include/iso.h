@@ -83,8 +83,10 @@ typedef enum {
     ISO_ERR_TIMEOUT = -9,      /* (device) a kernel's wait for its own bulk copies gave up
                                   after its limit; the outputs are unspecified unless the
                                   call says otherwise */
-    ISO_ERR_INDEX = -10        /* (device) a token id outside the embedding table that is not
-                                  the padding id; that token counts as padding */
+    ISO_ERR_INDEX = -10        /* (device) a token id outside the embedding table (the
+                                  vocabulary) that is not the padding id; that token (slot)
+                                  counts as padding.  Attention: an offset of a sequence
+                                  that is not ascending or not within the rows */
 } iso_status;
 
 #define ISO_MAX_EXPERTS 8
@@ -551,6 +553,123 @@ int32_t iso_embed_grad_workspace_size(int64_t n, int64_t cols, size_t* bytes);
 int32_t iso_embed_grad(const iso_mat* dY, const void* ids, int32_t ids_i64, int64_t pad_id, float scale,
                        const iso_mat* grad, int32_t accumulate, void* workspace, size_t ws_bytes, int32_t* status,
                        void* stream);
+
+/* ---- Training step: rotary positions --------------------------------------
+ *
+ * A row of x holds heads of head_dim channels side by side (cols a multiple of
+ * head_dim).  The first rot_dim channels of a head are rot_dim / 2 pairs: pair i
+ * is channels (i, i + rot_dim / 2), or with neighbours = 1 channels
+ * (2 i, 2 i + 1).  In row t it turns by the angle a = freq[i] * p, p row t's
+ * position on axis axis[i]:
+ *   (u, w) -> (u cos a - w sin a, u sin a + w cos a);
+ * further channels are copied.  inverse = 1 turns by -a, which is the gradient
+ * of the turn.  The angle is taken modulo a whole turn in 64-bit fixed point, so
+ * it is as exact for far positions as for near ones (|error| <= 2^-30 +
+ * |p| 2^-63 turns beside freq's own); products and sums are binary32, rounded
+ * once.  positions holds axes rows of x->rows positions (int32, or int64 with
+ * positions_i64 = 1), ld_positions apart, any sign.  y has x's shape and dtype; it
+ * is x itself (same data and stride) or shares no byte with it. */
+#define ISO_ROPE_MAX_PAIRS 128
+#define ISO_ROPE_MAX_AXES 4
+typedef struct {
+    int32_t head_dim;          /* >= 1 */
+    int32_t rot_dim;           /* even, 0 .. min(head_dim, 2 ISO_ROPE_MAX_PAIRS) */
+    int32_t axes;              /* 1 .. ISO_ROPE_MAX_AXES */
+    int32_t neighbours;        /* pairs of neighbouring channels (1) or of the two halves (0) */
+    int32_t inverse;
+    int32_t reserved;          /* must be 0 */
+    const double*  freq;       /* host: rot_dim / 2 angles per position, in radians, finite */
+    const int32_t* axis;       /* host: rot_dim / 2 values in [0, axes) */
+} iso_rope_cfg;
+int32_t iso_rope(const iso_mat* x, const void* positions, int32_t positions_i64, int64_t ld_positions,
+                 const iso_rope_cfg* cfg, const iso_mat* y, void* stream);
+
+/* ---- Training step: attention ----------------------------------------------
+ *
+ * Packed sequences: sequence s has the queries q_ends[s] .. q_ends[s + 1] - 1
+ * (rows of q and out) and the keys k_ends[s] .. k_ends[s + 1] - 1 (rows of k and
+ * v); without q_ends one sequence of all rows.  Offsets are int32 on the device,
+ * ascending and within the rows; others are reported as ISO_ERR_INDEX through
+ * status, nothing outside the matrices is touched and the outputs are
+ * unspecified.  Rows that belong to no sequence have no part and are not written.
+ * q, out hold heads x head_dim columns, k, v kv_heads x head_dim; query head h
+ * uses key head h / (heads / kv_heads).
+ *
+ * Query i of a sequence of n queries and m keys stands at position i + m - n
+ * among its keys.  It sees key j if j <= i + m - n (causal = 1) and, with a
+ * window, j > i + m - n - window; without causal it sees every key.  What is not
+ * seen has no part in the result, whatever it holds.  Over the seen keys
+ *   lse_i = log sum_j exp(scale q_i.k_j),   out_i = sum_j exp(scale q_i.k_j - lse_i) v_j;
+ * a query that sees none has out = 0 and lse = -Inf.
+ *
+ * BF16: products of the inputs are exact, sums, softmax statistics and lse
+ * binary32; the weights exp(...) are rounded to bfloat16 before their product with v
+ * (2^-8 each at most, relative), out once more.  Head dimensions that are multiples of 8,
+ * with rows and bases on 16-byte boundaries, run on the tensor cores, any other
+ * call on the CUDA cores in binary32 throughout, as F32 does. */
+#define ISO_ATTN_MAX_DIM 128
+typedef struct {
+    int32_t heads, kv_heads;   /* >= 1, kv_heads a divisor of heads */
+    int32_t head_dim;          /* 1 .. ISO_ATTN_MAX_DIM */
+    int32_t causal;
+    int64_t window;            /* keys a query sees at most, with causal; 0: no limit */
+    float   scale;             /* finite, > 0 */
+    int32_t n_seqs;            /* 0 without q_ends */
+    const int32_t* q_ends;     /* device, n_seqs + 1 offsets; NULL: one sequence of all rows */
+    const int32_t* k_ends;     /* device, n_seqs + 1 offsets; NULL: the queries' (k, v have q's rows) */
+} iso_attn_cfg;
+
+/* out <- attention, lse (float, heads rows of q->rows values) <- the log-sum-exp.
+ * All matrices share a dtype.  out and lse overlap no input and not each other.
+ * Workspace: scratch, 256-byte aligned.  status (device, may be NULL): ISO_OK,
+ * ISO_ERR_INDEX or ISO_ERR_TIMEOUT (rows that a give-up left unfinished are NaN). */
+int32_t iso_attn_workspace_size(const iso_mat* q, const iso_mat* k, const iso_attn_cfg* cfg, size_t* bytes);
+int32_t iso_attn(const iso_mat* q, const iso_mat* k, const iso_mat* v, const iso_attn_cfg* cfg, const iso_mat* out,
+                 float* lse, void* workspace, size_t ws_bytes, int32_t* status, void* stream);
+
+/* The gradients from dout and what the forward pass kept, the weights P_ij =
+ * exp(scale q_i.k_j - lse_i) computed again:
+ *   delta_i = sum_d dout_id out_id,   dS_ij = P_ij (dout_i.v_j - delta_i),
+ *   dv_j = sum_i P_ij dout_i,  dk_j = scale sum_i dS_ij q_i,  dq_i = scale sum_j dS_ij k_j,
+ * dk and dv summed over the query heads of their key head.  Shapes and dtype are
+ * those of q, k and v.  Sums are binary32 in an order fixed by the sizes and
+ * offsets, so equal inputs give equal bits; for BF16 P and dS are rounded to
+ * bfloat16 before their products, and each gradient once.  Gradients overlap no
+ * input, nor each other; they may be column ranges of one buffer. */
+int32_t iso_attn_grad_workspace_size(const iso_mat* q, const iso_mat* k, const iso_attn_cfg* cfg, size_t* bytes);
+int32_t iso_attn_grad(const iso_mat* dout, const iso_mat* q, const iso_mat* k, const iso_mat* v, const iso_mat* out,
+                      const float* lse, const iso_attn_cfg* cfg, const iso_mat* dq, const iso_mat* dk,
+                      const iso_mat* dv, void* workspace, size_t ws_bytes, int32_t* status, void* stream);
+
+/* ---- Training step: distillation from a teacher's top logits ---------------
+ *
+ * Row t of the teacher has logits for the vocabulary entries ids[t][0 .. K - 1]
+ * (int32, or int64 with ids_i64 = 1; K columns, contiguous).  An id of -1 is an unused slot; any other id
+ * outside the vocabulary is one too, and is reported as ISO_ERR_INDEX through
+ * status.  An id may occur several times.  With tau the temperature,
+ *   p_k = softmax over the used slots of teacher_tk / tau,   lse = log sum_v exp(z_v / tau),
+ *   loss = tau^2 sum_k p_k (log p_k - z_{ids_k} / tau + lse),
+ *   dlogits_v = dloss tau (exp(z_v / tau - lse) - sum of p_k over the slots with ids_k = v):
+ * the divergence of the student from the teacher's distribution over its top
+ * entries.  K = 1 is the cross-entropy of one target.  A slot with p_k = 0 adds 0.
+ * A row without a used slot, or whose used slots are all -Inf, has loss 0 and
+ * gradient 0.  A student row of -Inf alone has lse = -Inf, and NaN as loss and
+ * gradient; one with a NaN or +Inf has NaN for all three.  loss and lse have a
+ * float per row.  Statistics and the gradient are binary32, the gradient rounded
+ * once to dlogits' type (that of the logits).  dlogits may be the logits
+ * themselves (same data and stride); else it overlaps no input. */
+#define ISO_DISTILL_MAX_TOP 2048
+
+/* loss and lse; with dlogits (then dloss is needed too, a float per row) also the gradient, the
+ * logits read once for both. */
+int32_t iso_distill(const iso_mat* logits, const void* ids, int32_t ids_i64, const iso_mat* teacher,
+                    float temperature, float* loss, float* lse, const float* dloss, const iso_mat* dlogits,
+                    int32_t* status, void* stream);
+
+/* The gradient alone, from lse. */
+int32_t iso_distill_grad(const float* dloss, const iso_mat* logits, const void* ids, int32_t ids_i64,
+                         const iso_mat* teacher, float temperature, const float* lse, const iso_mat* dlogits,
+                         int32_t* status, void* stream);
 
 /* Static description of a status code. */
 const char* iso_error_string(int32_t status);

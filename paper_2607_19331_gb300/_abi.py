@@ -80,12 +80,28 @@ class IsoAct(ctypes.Structure):
                 ("cols", ctypes.c_int64), ("ld_codes", ctypes.c_int64), ("ld_exps", ctypes.c_int64)]
 
 
+class IsoRopeCfg(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("neighbours", ctypes.c_int32), ("inverse", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("freq", ctypes.c_void_p), ("axis", ctypes.c_void_p)]
+
+
+class IsoAttnCfg(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("window", ctypes.c_int64), ("scale", ctypes.c_float),
+                ("n_seqs", ctypes.c_int32), ("q_ends", ctypes.c_void_p), ("k_ends", ctypes.c_void_p)]
+
+
 ISO_ACT_GROUP = 32
+ISO_ROPE_MAX_PAIRS, ISO_ROPE_MAX_AXES = 128, 4
+ISO_ATTN_MAX_DIM = 128
+ISO_DISTILL_MAX_TOP = 2048
 
 # (name, restype, argtypes) for every entry point of include/iso.h
 P = ctypes.c_void_p
 PT = ctypes.POINTER(IsoTensor)
 PM, PA = ctypes.POINTER(IsoMat), ctypes.POINTER(IsoAct)
+PR, PC = ctypes.POINTER(IsoRopeCfg), ctypes.POINTER(IsoAttnCfg)
 I32, I64, SZ = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
 PROTOTYPES = [
     ("iso_num_units", I32, [PT, I32, ctypes.POINTER(IsoTopkCfg), ctypes.POINTER(I64)]),
@@ -124,6 +140,13 @@ PROTOTYPES = [
     ("iso_embed", I32, [PM, P, I32, I64, I64, ctypes.c_float, PM, P, P]),
     ("iso_embed_grad_workspace_size", I32, [I64, I64, ctypes.POINTER(SZ)]),
     ("iso_embed_grad", I32, [PM, P, I32, I64, ctypes.c_float, PM, I32, P, SZ, P, P]),
+    ("iso_rope", I32, [PM, P, I32, I64, PR, PM, P]),
+    ("iso_attn_workspace_size", I32, [PM, PM, PC, ctypes.POINTER(SZ)]),
+    ("iso_attn", I32, [PM, PM, PM, PC, PM, P, P, SZ, P, P]),
+    ("iso_attn_grad_workspace_size", I32, [PM, PM, PC, ctypes.POINTER(SZ)]),
+    ("iso_attn_grad", I32, [PM, PM, PM, PM, PM, P, PC, PM, PM, PM, P, SZ, P, P]),
+    ("iso_distill", I32, [PM, P, I32, PM, ctypes.c_float, P, P, P, PM, P, P]),
+    ("iso_distill_grad", I32, [P, PM, P, I32, PM, ctypes.c_float, P, PM, P, P]),
     ("iso_error_string", ctypes.c_char_p, [I32]),
     ("iso_launch_count", ctypes.c_uint64, []),
     ("iso_force_two_pass", ctypes.c_int32, [ctypes.c_int32]),
