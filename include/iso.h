@@ -641,6 +641,11 @@ int32_t iso_attn_grad(const iso_mat* dout, const iso_mat* q, const iso_mat* k, c
                       const float* lse, const iso_attn_cfg* cfg, const iso_mat* dq, const iso_mat* dk,
                       const iso_mat* dv, void* workspace, size_t ws_bytes, int32_t* status, void* stream);
 
+/* Diagnostics: the time after which a wait of the attention kernels gives up, for
+ * the calls that follow (2 s; the time that another process has the GPU counts
+ * little).  ns < 0 changes nothing.  Returns the limit before the call. */
+int64_t iso_attn_wait_ns(int64_t ns);
+
 /* ---- Training step: distillation from a teacher's top logits ---------------
  *
  * Row t of the teacher has logits for the vocabulary entries ids[t][0 .. K - 1]

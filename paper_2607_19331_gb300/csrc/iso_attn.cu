@@ -8,194 +8,40 @@
 // a tile of queries and goes over the keys; S and dP are formed in both (seven
 // products instead of five), and every sum has a fixed order.
 //
-// The CUDA-core kernels take any type, head dimension, stride and alignment, in
-// binary32 throughout: tiles of 64 x 64 in shared memory as binary32, 256 threads
-// with 4 x 4 of S and 4 x (dim / 16) of a sum each.  A product takes two 16-byte
-// shared loads per sixteen multiply-adds and is bound by those.
+// The CUDA-core kernels (tiles in iso_attn_simt.cuh) take any type, head
+// dimension, stride and alignment, in binary32 throughout.
 #include "iso_attn.cuh"
+#include "iso_attn_simt.cuh"
+#include "iso_attn_tc.cuh"
+#include "iso_tc.cuh"
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 namespace iso {
 namespace {
 
-constexpr int SA_B = 64;                 // rows and columns of a tile
-constexpr int SA_TPB = 256;
-constexpr int SA_PP = SA_B + 4;          // row of a P tile: no bank twice in eight lanes' 16-byte loads
-
-template <int DP>
-constexpr int sa_pitch() { return DP + 4; }
-
-// rows row0 .. row0 + 63 of a head into shared memory; `valid` of them exist,
-// the others and channels past dim are 0
-template <typename T, int DP>
-__device__ __forceinline__ void sa_load(float* s, const void* base, long long ld, long long row0, int valid, int col0, int dim) {
-    for (int i = threadIdx.x; i < SA_B * DP; i += SA_TPB) {
-        const int r = i / DP, d = i - r * DP;
-        s[r * sa_pitch<DP>() + d] =
-            r < valid && d < dim ? to_f32(static_cast<const T*>(base)[(row0 + r) * ld + col0 + d]) : 0.0f;
-    }
-}
-
-// acc[i][j] = A[ty + 16 i] . B[tx + 16 j]
-template <int DP>
-__device__ __forceinline__ void sa_dot(const float* a, const float* b, int ty, int tx, float (&acc)[4][4]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = 0.0f;
-#pragma unroll 2
-    for (int d = 0; d < DP; d += 4) {
-        float4 x[4], y[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[i] = *reinterpret_cast<const float4*>(a + (ty + 16 * i) * sa_pitch<DP>() + d);
-            y[i] = *reinterpret_cast<const float4*>(b + (tx + 16 * i) * sa_pitch<DP>() + d);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                acc[i][j] = fmaf(x[i].x, y[j].x, acc[i][j]);
-                acc[i][j] = fmaf(x[i].y, y[j].y, acc[i][j]);
-                acc[i][j] = fmaf(x[i].z, y[j].z, acc[i][j]);
-                acc[i][j] = fmaf(x[i].w, y[j].w, acc[i][j]);
-            }
-    }
-}
-
-// acc[i][4 j + c] += sum_k P[ty + 16 i][k] V[k][4 tx + 64 j + c], k over the
-// columns [lo[i], hi[i]) of each row: what is masked is not multiplied, so a NaN
-// there stays out
-template <int DP>
-__device__ __forceinline__ void sa_mul(const float* p, const float* v, int ty, int tx, const int (&lo)[4], const int (&hi)[4],
-                                       float (&acc)[4][DP / 16]) {
-    const bool full = lo[0] <= 0 && lo[1] <= 0 && lo[2] <= 0 && lo[3] <= 0 && hi[0] >= SA_B && hi[1] >= SA_B &&
-                      hi[2] >= SA_B && hi[3] >= SA_B;
-    auto go = [&](auto masked) {
-#pragma unroll 1
-        for (int k = 0; k < SA_B; k += 4) {
-            float4 w[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float4*>(p + (ty + 16 * i) * SA_PP + k);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-#pragma unroll
-                for (int j = 0; j < DP / 64; ++j) {
-                    const float4 x = *reinterpret_cast<const float4*>(v + (k + c) * sa_pitch<DP>() + 4 * tx + 64 * j);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float s = c == 0 ? w[i].x : c == 1 ? w[i].y : c == 2 ? w[i].z : w[i].w;
-                        if (!decltype(masked)::value || (k + c >= lo[i] && k + c < hi[i])) {
-                            acc[i][4 * j] = fmaf(s, x.x, acc[i][4 * j]);
-                            acc[i][4 * j + 1] = fmaf(s, x.y, acc[i][4 * j + 1]);
-                            acc[i][4 * j + 2] = fmaf(s, x.z, acc[i][4 * j + 2]);
-                            acc[i][4 * j + 3] = fmaf(s, x.w, acc[i][4 * j + 3]);
-                        }
-                    }
-                }
-            }
-        }
-    };
-    if (full) go(std::false_type{});
-    else go(std::true_type{});
-}
-
-template <typename T, int DP>
-__device__ __forceinline__ void sa_store(void* base, long long ld, long long row0, int valid, int col0, int dim, int ty, int tx,
-                                         const float (&acc)[4][DP / 16], const float (&by)[4]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = ty + 16 * i;
-        if (r >= valid) continue;
-        T* o = static_cast<T*>(base) + (row0 + r) * ld + col0;
-#pragma unroll
-        for (int j = 0; j < DP / 64; ++j)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const int d = 4 * tx + 64 * j + c;
-                if (d < dim) from_f32(acc[i][4 * j + c] * by[i], o[d]);
-            }
-    }
-}
-
-__device__ __forceinline__ float row_max(float x) {      // over the 16 lanes of a row
-#pragma unroll
-    for (int o = 8; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
-    return x;
-}
-__device__ __forceinline__ float row_sum(float x) {
-#pragma unroll
-    for (int o = 8; o; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
-    return x;
-}
-
 template <typename T, int DP>
 __global__ void __launch_bounds__(SA_TPB) k_simt_attn(AttnArgs g) {
-    extern __shared__ __align__(16) float sa_smem[];
-    constexpr int TILE = SA_B * sa_pitch<DP>();
-    float *const sq = sa_smem, *const sk = sq + TILE, *const sv = sk + TILE, *const sp = sv + TILE;
-    const int h = blockIdx.x % g.heads, kh = h / g.group, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    extern __shared__ __align__(16) float sa_smem_[];
     AttnTile t;
-    if (!attn_find_tile(g, blockIdx.x / g.heads, SA_B, false, t)) return;
-    const int rows = min(SA_B, t.nq - t.first);
-    sa_load<T, DP>(sq, g.q, g.ldq, (long long)t.q0 + t.first, rows, h * g.head_dim, g.head_dim);
-    int lo[4], hi[4], first, last, unused;
-    float m[4], l[4], acc[4][DP / 16] = {};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        attn_keys_of(g, t, t.first + min(ty + 16 * i, rows - 1), lo[i], hi[i]);
-        m[i] = -INFINITY;
-        l[i] = 0.0f;
-    }
-    attn_keys_of(g, t, t.first, first, unused);
-    attn_keys_of(g, t, t.first + rows - 1, unused, last);
-    for (int k0 = first / SA_B * SA_B; k0 < last; k0 += SA_B) {
-        const int keys = min(SA_B, t.nk - k0);
-        __syncthreads();
-        sa_load<T, DP>(sk, g.k, g.ldk, (long long)t.k0 + k0, keys, kh * g.head_dim, g.head_dim);
-        sa_load<T, DP>(sv, g.v, g.ldv, (long long)t.k0 + k0, keys, kh * g.head_dim, g.head_dim);
-        __syncthreads();
-        float s[4][4];
-        sa_dot<DP>(sq, sk, ty, tx, s);
-        int a[4], b[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            a[i] = lo[i] - k0;
-            b[i] = hi[i] - k0;
-            float top = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int c = tx + 16 * j;
-                s[i][j] = c >= a[i] && c < b[i] ? s[i][j] * g.scale : -INFINITY;
-                top = fmaxf(top, s[i][j]);
-            }
-            const float to = fmaxf(m[i], row_max(top));
-            const float base = to == -INFINITY ? 0.0f : to, by = expf(m[i] - base);     // 0 before the first seen key
-            m[i] = to;
-            float sum = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float p = expf(s[i][j] - base);
-                sp[(ty + 16 * i) * SA_PP + tx + 16 * j] = p;
-                sum += p;
-            }
-            l[i] = l[i] * by + row_sum(sum);
-#pragma unroll
-            for (int c = 0; c < DP / 16; ++c) acc[i][c] *= by;
-        }
-        __syncthreads();
-        sa_mul<DP>(sp, sv, ty, tx, a, b, acc);
-    }
-    float inv[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        inv[i] = l[i] == 0.0f ? 0.0f : 1.0f / l[i];
-        const int r = ty + 16 * i;
-        if (tx == 0 && r < rows) g.lse[(long long)h * g.q_rows + t.q0 + t.first + r] = m[i] + logf(l[i]);
-    }
-    sa_store<T, DP>(const_cast<void*>(g.out), g.ldo, (long long)t.q0 + t.first, rows, h * g.head_dim, g.head_dim, ty, tx, acc, inv);
+    if (attn_find_tile(g, blockIdx.x / g.heads, SA_B, false, t)) simt_attn<T, DP>(g, t, blockIdx.x % g.heads, sa_smem_);
+}
+template <typename T, int DP>
+__global__ void __launch_bounds__(SA_TPB) k_simt_grad_kv(AttnArgs g) {
+    extern __shared__ __align__(16) float sa_smem_[];
+    const int kv_heads = g.heads / g.group, kh = blockIdx.x % kv_heads;
+    AttnTile t;
+    if (attn_find_tile(g, blockIdx.x / kv_heads, SA_B, true, t))
+        simt_grad_kv<T, DP, T>(g, t, kh, kh * g.group, (kh + 1) * g.group, static_cast<T*>(g.dk), g.lddk, static_cast<T*>(g.dv),
+                               g.lddv, sa_smem_);
+}
+template <typename T, int DP>
+__global__ void __launch_bounds__(SA_TPB) k_simt_grad_q(AttnArgs g) {
+    extern __shared__ __align__(16) float sa_smem_[];
+    AttnTile t;
+    if (attn_find_tile(g, blockIdx.x / g.heads, SA_B, false, t)) simt_grad_q<T, DP>(g, t, blockIdx.x % g.heads, sa_smem_);
 }
 
 // delta[h][i] = sum_d dout_id out_id: a warp per row and head
@@ -214,120 +60,6 @@ __global__ void __launch_bounds__(256) k_attn_delta(AttnArgs g) {
     for (int k = 16; k; k >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, k);
     if (lane == 0) g.delta[(long long)h * g.q_rows + row] = s;
 }
-
-// dk and dv of 64 keys of one key head
-template <typename T, int DP>
-__global__ void __launch_bounds__(SA_TPB) k_simt_grad_kv(AttnArgs g) {
-    extern __shared__ __align__(16) float sa_smem[];
-    constexpr int TILE = SA_B * sa_pitch<DP>();
-    float *const sk = sa_smem, *const sv = sk + TILE, *const sq = sv + TILE, *const sd = sq + TILE, *const sp = sd + TILE,
-                 *const ss = sp + SA_B * SA_PP;
-    __shared__ float lse[SA_B], delta[SA_B];
-    const int kv_heads = g.heads / g.group, kh = blockIdx.x % kv_heads, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    AttnTile t;
-    if (!attn_find_tile(g, blockIdx.x / kv_heads, SA_B, true, t)) return;
-    const int keys = min(SA_B, t.nk - t.first);
-    sa_load<T, DP>(sk, g.k, g.ldk, (long long)t.k0 + t.first, keys, kh * g.head_dim, g.head_dim);
-    sa_load<T, DP>(sv, g.v, g.ldv, (long long)t.k0 + t.first, keys, kh * g.head_dim, g.head_dim);
-    int lo[4], hi[4], first, last, unused;
-    float ak[4][DP / 16] = {}, av[4][DP / 16] = {};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) attn_queries_of(g, t, t.first + min(ty + 16 * i, keys - 1), lo[i], hi[i]);
-    attn_queries_of(g, t, t.first, first, unused);
-    attn_queries_of(g, t, t.first + keys - 1, unused, last);
-    for (int h = kh * g.group; h < (kh + 1) * g.group; ++h) {
-        for (int q0 = first / SA_B * SA_B; q0 < last; q0 += SA_B) {
-            const int rows = min(SA_B, t.nq - q0);
-            __syncthreads();
-            sa_load<T, DP>(sq, g.q, g.ldq, (long long)t.q0 + q0, rows, h * g.head_dim, g.head_dim);
-            sa_load<T, DP>(sd, g.dout, g.lddo, (long long)t.q0 + q0, rows, h * g.head_dim, g.head_dim);
-            if (threadIdx.x < SA_B) {
-                const long long at = (long long)h * g.q_rows + t.q0 + q0 + threadIdx.x;
-                lse[threadIdx.x] = (int)threadIdx.x < rows ? g.lse[at] : 0.0f;
-                delta[threadIdx.x] = (int)threadIdx.x < rows ? g.delta[at] : 0.0f;
-            }
-            __syncthreads();
-            float s[4][4], dp[4][4];
-            sa_dot<DP>(sk, sq, ty, tx, s);
-            sa_dot<DP>(sv, sd, ty, tx, dp);
-            int a[4], b[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                a[i] = lo[i] - q0;
-                b[i] = hi[i] - q0;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int c = tx + 16 * j;
-                    const bool seen = c >= a[i] && c < b[i];
-                    const float p = seen ? expf(s[i][j] * g.scale - lse[c]) : 0.0f;
-                    sp[(ty + 16 * i) * SA_PP + c] = p;
-                    ss[(ty + 16 * i) * SA_PP + c] = seen ? p * (dp[i][j] - delta[c]) : 0.0f;
-                }
-            }
-            __syncthreads();
-            sa_mul<DP>(sp, sd, ty, tx, a, b, av);
-            sa_mul<DP>(ss, sq, ty, tx, a, b, ak);
-        }
-    }
-    const float one[4] = {1.0f, 1.0f, 1.0f, 1.0f}, scale[4] = {g.scale, g.scale, g.scale, g.scale};
-    sa_store<T, DP>(g.dk, g.lddk, (long long)t.k0 + t.first, keys, kh * g.head_dim, g.head_dim, ty, tx, ak, scale);
-    sa_store<T, DP>(g.dv, g.lddv, (long long)t.k0 + t.first, keys, kh * g.head_dim, g.head_dim, ty, tx, av, one);
-}
-
-// dq of 64 queries of one head
-template <typename T, int DP>
-__global__ void __launch_bounds__(SA_TPB) k_simt_grad_q(AttnArgs g) {
-    extern __shared__ __align__(16) float sa_smem[];
-    constexpr int TILE = SA_B * sa_pitch<DP>();
-    float *const sq = sa_smem, *const sd = sq + TILE, *const sk = sd + TILE, *const sv = sk + TILE, *const ss = sv + TILE;
-    const int h = blockIdx.x % g.heads, kh = h / g.group, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    AttnTile t;
-    if (!attn_find_tile(g, blockIdx.x / g.heads, SA_B, false, t)) return;
-    const int rows = min(SA_B, t.nq - t.first);
-    sa_load<T, DP>(sq, g.q, g.ldq, (long long)t.q0 + t.first, rows, h * g.head_dim, g.head_dim);
-    sa_load<T, DP>(sd, g.dout, g.lddo, (long long)t.q0 + t.first, rows, h * g.head_dim, g.head_dim);
-    int lo[4], hi[4], first, last, unused;
-    float lse[4], delta[4], acc[4][DP / 16] = {};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = min(ty + 16 * i, rows - 1);
-        attn_keys_of(g, t, t.first + r, lo[i], hi[i]);
-        const long long at = (long long)h * g.q_rows + t.q0 + t.first + r;
-        lse[i] = g.lse[at];
-        delta[i] = g.delta[at];
-    }
-    attn_keys_of(g, t, t.first, first, unused);
-    attn_keys_of(g, t, t.first + rows - 1, unused, last);
-    for (int k0 = first / SA_B * SA_B; k0 < last; k0 += SA_B) {
-        const int keys = min(SA_B, t.nk - k0);
-        __syncthreads();
-        sa_load<T, DP>(sk, g.k, g.ldk, (long long)t.k0 + k0, keys, kh * g.head_dim, g.head_dim);
-        sa_load<T, DP>(sv, g.v, g.ldv, (long long)t.k0 + k0, keys, kh * g.head_dim, g.head_dim);
-        __syncthreads();
-        float s[4][4], dp[4][4];
-        sa_dot<DP>(sq, sk, ty, tx, s);
-        sa_dot<DP>(sd, sv, ty, tx, dp);
-        int a[4], b[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            a[i] = lo[i] - k0;
-            b[i] = hi[i] - k0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int c = tx + 16 * j;
-                const bool seen = c >= a[i] && c < b[i];
-                ss[(ty + 16 * i) * SA_PP + c] = seen ? expf(s[i][j] * g.scale - lse[i]) * (dp[i][j] - delta[i]) : 0.0f;
-            }
-        }
-        __syncthreads();
-        sa_mul<DP>(ss, sk, ty, tx, a, b, acc);
-    }
-    const float scale[4] = {g.scale, g.scale, g.scale, g.scale};
-    sa_store<T, DP>(g.dq, g.lddq, (long long)t.q0 + t.first, rows, h * g.head_dim, g.head_dim, ty, tx, acc, scale);
-}
-
-template <int DP>
-constexpr int sa_smem(int tiles, int weights) { return (tiles * SA_B * sa_pitch<DP>() + weights * SA_B * SA_PP) * 4; }
 
 template <typename K>
 int simt_launch(K kernel, long long grid, int smem, const AttnArgs& g, cudaStream_t s) {
@@ -420,7 +152,51 @@ AttnArgs attn_args(const iso_mat* q, const iso_mat* k, const iso_mat* v, const i
 }
 size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
 
+// what tensor copies can take: heads and rows on 16-byte boundaries
+bool copies_take(const iso_mat* m) {
+    return (reinterpret_cast<uintptr_t>(m->data) & 15u) == 0 && (m->ld * 2) % 16 == 0;
+}
+template <typename... M>
+bool on_tensor_cores(const iso_attn_cfg* c, const M*... m) {
+    return c->head_dim % 8 == 0 && ((m->dtype == ISO_BF16) && ...) && (copies_take(m) && ...) && ((m->rows > 0) && ...);
+}
+
+constexpr uint64_t ATTN_WAIT_NS = 2000000000;      // a wait gives up after this long, unless told otherwise
+std::atomic<uint64_t> g_attn_wait_ns{ATTN_WAIT_NS};
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                 CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled() {
+    static EncodeTiled fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        return cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+                       q == cudaDriverEntryPointSuccess
+                   ? reinterpret_cast<EncodeTiled>(p)
+                   : nullptr;
+    }();
+    return fn;
+}
+
 }  // namespace
+
+uint64_t attn_wait_ns() { return g_attn_wait_ns.load(std::memory_order_relaxed); }
+
+int tc::head_map(CUtensorMap* map, const void* base, long long rows, int heads, int head_dim, long long ld) {
+    EncodeTiled fn = encode_tiled();
+    if (!fn) return ISO_ERR_CUDA;
+    const cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)rows};
+    const cuuint64_t strides[2] = {(cuuint64_t)head_dim * 2, (cuuint64_t)ld * 2};
+    const cuuint32_t box[3] = {(cuuint32_t)BOX, 1, (cuuint32_t)ROWS};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? ISO_OK
+               : ISO_ERR_CUDA;
+}
+
 }  // namespace iso
 
 using namespace iso;
@@ -457,8 +233,13 @@ int32_t iso_attn(const iso_mat* q, const iso_mat* k, const iso_mat* v, const iso
 int32_t iso_attn_grad_workspace_size(const iso_mat* q, const iso_mat* k, const iso_attn_cfg* cfg, size_t* bytes) {
     if (!bytes) return ISO_ERR_ARG;
     ISO_TRY(check_qk(q, k, cfg));
-    *bytes = round256((size_t)q->rows * cfg->heads * 4) + 256;
+    *bytes = round256((size_t)q->rows * cfg->heads * 4) + round256(attn_grad_plan(q->rows, k->rows, *cfg).bytes) + 256;
     return ISO_OK;
+}
+
+int64_t iso_attn_wait_ns(int64_t ns) {
+    return (int64_t)(ns < 0 ? g_attn_wait_ns.load(std::memory_order_relaxed)
+                            : g_attn_wait_ns.exchange((uint64_t)ns, std::memory_order_relaxed));
 }
 
 int32_t iso_attn_grad(const iso_mat* dout, const iso_mat* q, const iso_mat* k, const iso_mat* v, const iso_mat* out,
@@ -494,6 +275,9 @@ int32_t iso_attn_grad(const iso_mat* dout, const iso_mat* q, const iso_mat* k, c
             if ((warps + 7) / 8 > EXTENT_LIMIT) return ISO_ERR_UNSUPPORTED;
             TRAIN_LAUNCH((k_attn_delta<T><<<(unsigned)((warps + 7) / 8), 256, 0, s>>>(g)));
         }
+        if (on_tensor_cores(cfg, q, k, v, dout))
+            return attn_grad_tc(g, attn_grad_plan(q->rows, k->rows, *cfg),
+                                reinterpret_cast<float*>(static_cast<char*>(workspace) + round256((size_t)q->rows * cfg->heads * 4)), s);
         return simt_backward<T, decltype(dp)::value>(g, s);
     });
 }

@@ -1,0 +1,199 @@
+// iso_tc.cuh -- the fifth-generation tensor cores as the attention kernels use
+// them (one CTA per product): tiles of 128 rows by tensor copies, bf16 products
+// with their accumulator (and a bf16 A operand) in tensor memory, bounded waits.
+#pragma once
+
+#include <cuda.h>
+
+#include "iso_train.cuh"
+#include "iso_internal.cuh"
+
+namespace iso {
+namespace tc {
+
+constexpr int ROWS = 128;                      // rows of a tile
+constexpr int BOX = 64;                        // channels of one copy: 128 bytes, the swizzle's row
+constexpr int BOX_BYTES = ROWS * BOX * 2;
+
+// kind::f16, fp32 accumulator, bf16 operands, M = 128, N = n; b_rows: B's
+// contraction runs over its rows ("MN-major") instead of along them
+constexpr uint32_t idesc(int n, bool b_rows) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | (b_rows ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) |
+           ((uint32_t)(ROWS >> 4) << 24);
+}
+// Shared-memory descriptors of a tile in the 128-byte swizzle (atoms of eight
+// rows, 1024 bytes): the high word for both, the low word is the start address in
+// 16-byte words and, where the contraction runs over rows, the distance of the
+// next 64 channels.
+constexpr uint32_t DESC_HI = (1024u >> 4) | 1u << 14 | 2u << 29;
+constexpr uint32_t DESC_LO_ALONG = 1u << 16, DESC_LO_ROWS = (uint32_t)(BOX_BYTES >> 4) << 16;
+
+// D (+)= A B^T, A and B tiles in shared memory, contraction along their rows
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t desc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+                 "mov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n\t}"
+                 :: "r"(d), "r"(a_lo), "r"(b_lo), "r"(DESC_HI), "r"(desc), "r"(accumulate) : "memory");
+}
+// D (+)= A B, A in tensor memory (two bf16 a column, the lower half first)
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t desc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+                 "mov.b64 b, {%2, %3};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}"
+                 :: "r"(d), "r"(a), "r"(b_lo), "r"(DESC_HI), "r"(desc), "r"(accumulate) : "memory");
+}
+// D = A B^T over DP channels: two tiles of 128 rows (DP / 64 boxes each)
+template <int DP>
+__device__ __forceinline__ void product_along(uint32_t d, uint32_t a, uint32_t b) {
+    const uint32_t al = DESC_LO_ALONG + (a >> 4), bl = DESC_LO_ALONG + (b >> 4);
+#pragma unroll
+    for (uint32_t k = 0; k < DP / 16; ++k) {
+        const uint32_t at = (k / 4) * (BOX_BYTES >> 4) + (k % 4) * 2;
+        mma_ss(d, al + at, bl + at, idesc(ROWS, false), k > 0);
+    }
+}
+// D (+)= A B: A [128 x 128] bf16 in tensor memory, its columns 0 .. 63 from `a`
+// on (32 words), 64 .. 127 from `a_half` on; B the tile's 128 rows of DP channels
+template <int DP>
+__device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t a_half, uint32_t b, uint32_t accumulate) {
+    const uint32_t bl = DESC_LO_ROWS + (b >> 4);
+#pragma unroll
+    for (uint32_t k = 0; k < 8; ++k)
+        mma_ts(d, (k < 4 ? a : a_half) + (k % 4) * 8, bl + k * (2048u >> 4), idesc(DP, true), k > 0 ? 1u : accumulate);
+}
+
+// arrive on `bar` once the products issued so far are done
+__device__ __forceinline__ void commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ void before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// 32 consecutive words of this thread's row of tensor memory; usable after the
+// wait, which takes them as operands so that no use is moved before it
+__device__ __forceinline__ void load32(uint32_t at, float (&v)[32]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+                   "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+                   "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
+                   "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+                 : "r"(at));
+}
+__device__ __forceinline__ void loaded(float (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                   "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]), "+f"(v[15]),
+                   "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]), "+f"(v[22]), "+f"(v[23]),
+                   "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]), "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+                 :: "memory");
+}
+__device__ __forceinline__ void store16(uint32_t at, const uint32_t* w) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 :: "r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]),
+                    "r"(w[8]), "r"(w[9]), "r"(w[10]), "r"(w[11]), "r"(w[12]), "r"(w[13]), "r"(w[14]), "r"(w[15])
+                 : "memory");
+}
+__device__ __forceinline__ void store32(uint32_t at, const float (&v)[32]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+                 :: "r"(at), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]),
+                    "f"(v[8]), "f"(v[9]), "f"(v[10]), "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]),
+                    "f"(v[16]), "f"(v[17]), "f"(v[18]), "f"(v[19]), "f"(v[20]), "f"(v[21]), "f"(v[22]), "f"(v[23]),
+                    "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]), "f"(v[28]), "f"(v[29]), "f"(v[30]), "f"(v[31])
+                 : "memory");
+}
+__device__ __forceinline__ void stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void alloc_all(uint32_t slot) {       // the whole tensor memory of the SM
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(slot) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void free_all(uint32_t at) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(at) : "memory");
+}
+
+// 64 channels of 128 rows of one head: coordinates channel, head, row
+__device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int channel, int head, int row, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+                 " [%0], [%1, {%2, %3, %4}], [%5];"
+                 :: "r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(channel), "r"(head), "r"(row), "r"(bar) : "memory");
+}
+// a tile of DP channels, announced on its barrier
+template <int DP>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int head, int row, uint32_t bar) {
+    mbar_arrive_tx(bar, DP / BOX * BOX_BYTES);
+#pragma unroll
+    for (int b = 0; b < DP / BOX; ++b) load_box(dst + b * BOX_BYTES, map, b * BOX, head, row, bar);
+}
+// Rows from `from` on of a tile of DP channels become zero: rows behind a
+// sequence's end, whose contents (another sequence's, or anything) must not meet a
+// weight of 0 in a product.  By a whole warp, before the products read the tile.
+template <int DP>
+__device__ __forceinline__ void clear_rows(unsigned char* tile, int from) {
+    if (from >= ROWS) return;
+    const int lane = threadIdx.x & 31;
+    for (int b = 0; b < DP / BOX; ++b)
+        for (int i = from * 8 + lane; i < ROWS * 8; i += 32)
+            reinterpret_cast<uint4*>(tile + b * BOX_BYTES)[i] = make_uint4(0u, 0u, 0u, 0u);
+    fence_proxy_async_smem();
+    __syncwarp();
+}
+
+__device__ __forceinline__ uint64_t now_ns() {
+    uint64_t t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
+__device__ __forceinline__ bool probe(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Bounded waits of a CTA.  A wait that gives up sets the flag, and with it every
+// other wait of the CTA ends.
+struct Waits {
+    uint64_t limit_ns;
+    volatile int* gave_up;
+    __device__ __forceinline__ bool one(uint32_t bar, uint32_t parity, uint64_t limit, bool heed) const {
+        WaitClock clock;
+        for (int spin = 0; spin < MBAR_SPIN_LIMIT; ++spin) {
+            if (probe(bar, parity)) return true;
+            if ((spin & 31) == 31 && ((heed && *gave_up) || clock.look(now_ns(), limit))) return false;
+        }
+        return false;
+    }
+    __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
+        if (one(bar, parity, limit_ns, true)) return true;
+        *gave_up = 1;
+        return false;
+    }
+    // one answer for the whole warp
+    __device__ __forceinline__ bool warp(uint32_t bar, uint32_t parity) const {
+        return __all_sync(0xFFFFFFFFu, (*this)(bar, parity));
+    }
+    // for what is in flight in any case (a copy, a product): not cut short by the flag
+    __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) const { one(bar, parity, 2000000000u, false); }
+};
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ void arrive_warp(uint32_t bar) {      // one arrival for the warp's accesses so far
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
+}
+
+// Host: the tensor map of a matrix of heads, boxes of 64 channels x 1 head x 128
+// rows in the 128-byte swizzle; channels past the head's and rows past the matrix
+// read as zero.  Rows and heads must start on 16-byte boundaries.
+int head_map(CUtensorMap* map, const void* base, long long rows, int heads, int head_dim, long long ld);
+
+}  // namespace tc
+}  // namespace iso
