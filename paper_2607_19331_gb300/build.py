@@ -23,7 +23,7 @@ BINDING = os.path.join(BUILD, "_iso_train.so")
 STAMP = os.path.join(BUILD, "_iso_train.txt")    # the torch that BINDING was built for, and its commands
 SOURCES = ["iso_api.cu", "iso_select.cu", "iso_apply.cu", "iso_merge.cu", "iso_block.cu", "iso_fused.cu",
            "iso_gemm.cu", "iso_frame.cu", "iso_range.cu", "iso_act.cu", "iso_wgrad.cu", "iso_embed.cu", "iso_rope.cu", "iso_distill.cu",
-           "iso_attn.cu", "iso_attn_grad.cu"]
+           "iso_attn.cu", "iso_attn_fwd.cu", "iso_attn_grad.cu"]
 HEADERS = ["iso_internal.cuh", "iso_kernels.cuh", "iso_gemm.cuh", "iso_train.cuh", "iso_attn.cuh",
            "iso_attn_tc.cuh", "iso_attn_simt.cuh", "iso_tc.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

@@ -26,7 +26,8 @@ template <typename T, int DP>
 __global__ void __launch_bounds__(SA_TPB) k_simt_attn(AttnArgs g) {
     extern __shared__ __align__(16) float sa_smem_[];
     AttnTile t;
-    if (attn_find_tile(g, blockIdx.x / g.heads, SA_B, false, t)) simt_attn<T, DP>(g, t, blockIdx.x % g.heads, sa_smem_);
+    if (attn_find_tile(g, blockIdx.x / g.heads, SA_B, false, t))
+        simt_attn<T, DP, T>(g, t, blockIdx.x % g.heads, 0, t.nk, static_cast<T*>(const_cast<void*>(g.out)), g.ldo, g.lse, sa_smem_);
 }
 template <typename T, int DP>
 __global__ void __launch_bounds__(SA_TPB) k_simt_grad_kv(AttnArgs g) {
@@ -206,7 +207,7 @@ extern "C" {
 int32_t iso_attn_workspace_size(const iso_mat* q, const iso_mat* k, const iso_attn_cfg* cfg, size_t* bytes) {
     if (!bytes) return ISO_ERR_ARG;
     ISO_TRY(check_qk(q, k, cfg));
-    *bytes = 256;
+    *bytes = round256(attn_plan(q->rows, k->rows, *cfg).bytes) + 256;
     return ISO_OK;
 }
 
@@ -220,11 +221,14 @@ int32_t iso_attn(const iso_mat* q, const iso_mat* k, const iso_mat* v, const iso
     const Bytes2D in[5] = {bytes_of(q), bytes_of(k), bytes_of(v), ends_bytes(cfg->q_ends, cfg->n_seqs), ends_bytes(cfg->k_ends, cfg->n_seqs)};
     const Bytes2D outs[2] = {bytes_of(out), floats(lse, (uint64_t)q->rows * cfg->heads)};
     if (overlap(in, outs)) return ISO_ERR_ARG;
-    if (!workspace || ws_bytes < 256 || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return ISO_ERR_WORKSPACE;
+    size_t need = 0;
+    ISO_TRY(iso_attn_workspace_size(q, k, cfg, &need));
+    if (!workspace || ws_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return ISO_ERR_WORKSPACE;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (status && cudaMemsetAsync(status, 0, sizeof(int32_t), s) != cudaSuccess) return ISO_ERR_CUDA;
     if (q->rows == 0) return ISO_OK;
     const AttnArgs g = attn_args(q, k, v, out, lse, cfg, status);
+    if (on_tensor_cores(cfg, q, k, v)) return attn_tc(g, attn_plan(q->rows, k->rows, *cfg), static_cast<float*>(workspace), s);
     return by_kind(q->dtype, cfg->head_dim, [&](auto* t, auto dp) -> int {
         return simt_forward<std::remove_pointer_t<decltype(t)>, decltype(dp)::value>(g, s);
     });

@@ -36,7 +36,6 @@ namespace {
 
 using namespace tc;
 
-constexpr float LOG2E = 1.4426950408889634f;
 constexpr int GR_COMPUTE = 8;
 constexpr int GR_THREADS = (GR_COMPUTE + 3) * 32;
 constexpr int KV_Q_STAGES = 3, KV_DO_STAGES = 2, Q_K_STAGES = 3, Q_V_STAGES = 2;
@@ -54,39 +53,6 @@ struct GradTile {
     static_assert(sa_smem<DP>(4, 2) <= (2 + KV_Q_STAGES + KV_DO_STAGES) * TILE + 2 * ROWS * 4 &&
                   sa_smem<DP>(4, 1) <= (2 + Q_K_STAGES + Q_V_STAGES) * TILE, "the rows done over fit where the tiles were");
 };
-
-__device__ __forceinline__ unsigned char* align1024(unsigned char* p) {
-    return reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(p) + 1023) & ~(uintptr_t)1023);
-}
-
-// One row of an accumulator out, 32 columns at a time: all lanes call it.  Whether
-// all it wrote is finite.
-template <typename O, int DP>
-__device__ __forceinline__ bool write_row(uint32_t at, O* row, bool valid, int dim, bool vec, float by, bool nan, bool none) {
-    float odd = 0.0f;                  // 0, or NaN after a value that is not finite
-#pragma unroll
-    for (int c = 0; c < DP; c += 32) {
-        float v[32];
-        __syncwarp();                  // a load of tensor memory takes all lanes
-        if (!none) {
-            load32(at + c, v);
-            loaded(v);
-        }
-#pragma unroll
-        for (int j = 0; j < 32; j += 8) {
-            if (!valid || c + j >= dim) continue;
-            float x[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[i] = nan ? __int_as_float(0x7FFFFFFF) : none ? 0.0f : v[j + i] * by;
-                odd = fmaf(x[i], 0.0f, odd);
-            }
-            if (vec) put8(row + c + j, x);
-            else store8<false>(row, c + j, dim, x);
-        }
-    }
-    return odd == 0.0f;
-}
 
 // The 64 weights of this thread's row and half: p = exp2(c s - lse2), 0 outside
 // [from, to) where the tile is masked

@@ -132,9 +132,11 @@ __device__ __forceinline__ float row_sum(float x) {
     return x;
 }
 
-// out and lse of 64 queries (from t.first on) of head h
-template <typename T, int DP>
-__device__ __noinline__ void simt_attn(const AttnArgs& g, const AttnTile& t, int h, float* smem) {
+// out and lse of 64 queries (from t.first on) of head h over the keys [begin, end),
+// into rows of their own matrix and vector
+template <typename T, int DP, typename O>
+__device__ __noinline__ void simt_attn(const AttnArgs& g, const AttnTile& t, int h, int begin, int end, O* out, long long ldo,
+                                       float* lse, float* smem) {
     constexpr int TILE = SA_B * sa_pitch<DP>();
     float *const sq = smem, *const sk = sq + TILE, *const sv = sk + TILE, *const sp = sv + TILE;
     const int kh = h / g.group, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
@@ -145,11 +147,15 @@ __device__ __noinline__ void simt_attn(const AttnArgs& g, const AttnTile& t, int
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         attn_keys_of(g, t, t.first + min(ty + 16 * i, rows - 1), lo[i], hi[i]);
+        lo[i] = max(lo[i], begin);
+        hi[i] = min(hi[i], end);
         m[i] = -INFINITY;
         l[i] = 0.0f;
     }
     attn_keys_of(g, t, t.first, first, unused);
     attn_keys_of(g, t, t.first + rows - 1, unused, last);
+    first = max(first, begin);
+    last = min(last, end);
     for (int k0 = first / SA_B * SA_B; k0 < last; k0 += SA_B) {
         const int keys = min(SA_B, t.nk - k0);
         sa_sync();
@@ -192,9 +198,9 @@ __device__ __noinline__ void simt_attn(const AttnArgs& g, const AttnTile& t, int
     for (int i = 0; i < 4; ++i) {
         inv[i] = l[i] == 0.0f ? 0.0f : 1.0f / l[i];
         const int r = ty + 16 * i;
-        if (tx == 0 && r < rows) g.lse[(long long)h * g.q_rows + t.q0 + t.first + r] = m[i] + logf(l[i]);
+        if (tx == 0 && r < rows) lse[(long long)h * g.q_rows + t.q0 + t.first + r] = m[i] + logf(l[i]);
     }
-    sa_store<T, DP>(const_cast<void*>(g.out), g.ldo, (long long)t.q0 + t.first, rows, h * g.head_dim, g.head_dim, ty, tx, acc, inv);
+    sa_store<O, DP>(out, ldo, (long long)t.q0 + t.first, rows, h * g.head_dim, g.head_dim, ty, tx, acc, inv);
 }
 
 // dk and dv of 64 keys (from t.first on) of key head kh, over the query heads

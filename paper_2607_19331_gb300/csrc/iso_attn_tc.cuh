@@ -9,6 +9,16 @@ namespace iso {
 // the time after which a wait of these kernels gives up, ns
 uint64_t attn_wait_ns();
 
+// Forward (iso_attn_fwd.cu).  Parts that the keys are cut into, and the bytes of
+// the parts' sums.
+struct AttnPlan {
+    int parts;
+    size_t bytes;
+};
+AttnPlan attn_plan(long long q_rows, long long k_rows, const iso_attn_cfg& c);
+// `part`: AttnPlan::bytes
+int attn_tc(const AttnArgs& g, const AttnPlan& p, float* part, cudaStream_t s);
+
 // Backward (iso_attn_grad.cu).  Parts of a key head's query heads that have sums
 // of their own, and the bytes of those sums.
 struct AttnGradPlan {

@@ -11,6 +11,7 @@
 namespace iso {
 namespace tc {
 
+constexpr float LOG2E = 1.4426950408889634f;
 constexpr int ROWS = 128;                      // rows of a tile
 constexpr int BOX = 64;                        // channels of one copy: 128 bytes, the swizzle's row
 constexpr int BOX_BYTES = ROWS * BOX * 2;
@@ -188,6 +189,39 @@ __device__ __forceinline__ float ex2(float x) {
 __device__ __forceinline__ void arrive_warp(uint32_t bar) {      // one arrival for the warp's accesses so far
     __syncwarp();
     if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
+}
+
+__device__ __forceinline__ unsigned char* align1024(unsigned char* p) {
+    return reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(p) + 1023) & ~(uintptr_t)1023);
+}
+
+// One row of an accumulator out, 32 columns at a time: all lanes call it.  Whether
+// all it wrote is finite.
+template <typename O, int DP>
+__device__ __forceinline__ bool write_row(uint32_t at, O* row, bool valid, int dim, bool vec, float by, bool nan, bool none) {
+    float odd = 0.0f;                  // 0, or NaN after a value that is not finite
+#pragma unroll
+    for (int c = 0; c < DP; c += 32) {
+        float v[32];
+        __syncwarp();                  // a load of tensor memory takes all lanes
+        if (!none) {
+            load32(at + c, v);
+            loaded(v);
+        }
+#pragma unroll
+        for (int j = 0; j < 32; j += 8) {
+            if (!valid || c + j >= dim) continue;
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[i] = nan ? __int_as_float(0x7FFFFFFF) : none ? 0.0f : v[j + i] * by;
+                odd = fmaf(x[i], 0.0f, odd);
+            }
+            if (vec) put8(row + c + j, x);
+            else store8<false>(row, c + j, dim, x);
+        }
+    }
+    return odd == 0.0f;
 }
 
 // Host: the tensor map of a matrix of heads, boxes of 64 channels x 1 head x 128
