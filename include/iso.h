@@ -591,7 +591,8 @@ int32_t iso_rope(const iso_mat* x, const void* positions, int32_t positions_i64,
  * v); without q_ends one sequence of all rows.  Offsets are int32 on the device,
  * ascending and within the rows; others are reported as ISO_ERR_INDEX through
  * status, nothing outside the matrices is touched and the outputs are
- * unspecified.  Rows that belong to no sequence have no part and are not written.
+ * unspecified.  Rows that belong to no sequence have no part, and are not written
+ * unless zero_rest asks for it.
  * q, out hold heads x head_dim columns, k, v kv_heads x head_dim; query head h
  * uses key head h / (heads / kv_heads).
  *
@@ -617,6 +618,8 @@ typedef struct {
     int32_t n_seqs;            /* 0 without q_ends */
     const int32_t* q_ends;     /* device, n_seqs + 1 offsets; NULL: one sequence of all rows */
     const int32_t* k_ends;     /* device, n_seqs + 1 offsets; NULL: the queries' (k, v have q's rows) */
+    int32_t zero_rest;         /* 1: rows of the outputs that belong to no sequence are written 0 */
+    int32_t reserved;          /* must be 0 */
 } iso_attn_cfg;
 
 /* out <- attention, lse (float, heads rows of q->rows values) <- the log-sum-exp.

@@ -89,7 +89,8 @@ class IsoRopeCfg(ctypes.Structure):
 class IsoAttnCfg(ctypes.Structure):
     _fields_ = [("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
                 ("causal", ctypes.c_int32), ("window", ctypes.c_int64), ("scale", ctypes.c_float),
-                ("n_seqs", ctypes.c_int32), ("q_ends", ctypes.c_void_p), ("k_ends", ctypes.c_void_p)]
+                ("n_seqs", ctypes.c_int32), ("q_ends", ctypes.c_void_p), ("k_ends", ctypes.c_void_p),
+                ("zero_rest", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 ISO_ACT_GROUP = 32

@@ -22,6 +22,51 @@
 namespace iso {
 namespace {
 
+// Zeros in the rows of up to three outputs, and the columns of lse, that belong to
+// no sequence: before the first one and behind the last.
+struct Rest {
+    void* at[3];
+    long long ld[3];
+    int32_t rows[3], cols[3];            // cols: bytes of a row / 2
+    const int32_t* ends[3];
+    float* lse;
+    int32_t n_seqs, heads;
+};
+__global__ void __launch_bounds__(256) k_zero_rest(const __grid_constant__ Rest z) {
+    auto each = [&](int m, auto f) {
+        const int first = min(max(z.ends[m][0], 0), z.rows[m]), last = max(first, min(max(z.ends[m][z.n_seqs], 0), z.rows[m]));
+        for (int r = blockIdx.x; r < first + z.rows[m] - last; r += gridDim.x) f(r < first ? r : last + r - first);
+    };
+    for (int m = 0; m < 3; ++m) {
+        if (!z.at[m]) continue;
+        each(m, [&](int row) {
+            uint16_t* p = static_cast<uint16_t*>(z.at[m]) + row * z.ld[m];
+            for (int c = threadIdx.x; c < z.cols[m]; c += blockDim.x) p[c] = 0;
+            if (m == 0 && z.lse)
+                for (int h = threadIdx.x; h < z.heads; h += blockDim.x) z.lse[(long long)h * z.rows[0] + row] = 0.0f;
+        });
+    }
+}
+int zero_rest(const AttnArgs& g, const iso_mat* a, const iso_mat* b, const iso_mat* c, float* lse, cudaStream_t s) {
+    if (g.n_seqs == 0) return ISO_OK;
+    Rest z{};
+    const iso_mat* mats[3] = {a, b, c};
+    for (int m = 0; m < 3; ++m) {
+        if (!mats[m] || mats[m]->rows == 0) continue;
+        const int halves = elem_size(mats[m]->dtype) / 2;
+        z.at[m] = mats[m]->data;
+        z.ld[m] = mats[m]->ld * halves;
+        z.rows[m] = (int)mats[m]->rows;
+        z.cols[m] = (int)(mats[m]->cols * halves);
+        z.ends[m] = m == 0 ? g.q_ends : g.k_ends;
+    }
+    z.lse = lse;
+    z.n_seqs = g.n_seqs;
+    z.heads = g.heads;
+    TRAIN_LAUNCH((k_zero_rest<<<(unsigned)std::min(train_sms(), 152), 256, 0, s>>>(z)));
+    return ISO_OK;
+}
+
 template <typename T, int DP>
 __global__ void __launch_bounds__(SA_TPB) k_simt_attn(AttnArgs g) {
     extern __shared__ __align__(16) float sa_smem_[];
@@ -88,6 +133,7 @@ int by_kind(int32_t dtype, int dim, F&& f) {
 int check_cfg(const iso_attn_cfg* c) {
     if (!c || c->heads < 1 || c->kv_heads < 1 || c->heads % c->kv_heads || c->head_dim < 1) return ISO_ERR_ARG;
     if ((c->causal != 0 && c->causal != 1) || c->window < 0 || (c->window && !c->causal)) return ISO_ERR_ARG;
+    if ((c->zero_rest != 0 && c->zero_rest != 1) || c->reserved != 0) return ISO_ERR_ARG;
     if (!(c->scale > 0.0f) || !std::isfinite(c->scale) || c->n_seqs < 0) return ISO_ERR_ARG;
     if ((c->n_seqs > 0) != (c->q_ends != nullptr) || (c->k_ends && !c->q_ends)) return ISO_ERR_ARG;
     if ((reinterpret_cast<uintptr_t>(c->q_ends) | reinterpret_cast<uintptr_t>(c->k_ends)) & 3u) return ISO_ERR_ALIGN;
@@ -228,6 +274,7 @@ int32_t iso_attn(const iso_mat* q, const iso_mat* k, const iso_mat* v, const iso
     if (status && cudaMemsetAsync(status, 0, sizeof(int32_t), s) != cudaSuccess) return ISO_ERR_CUDA;
     if (q->rows == 0) return ISO_OK;
     const AttnArgs g = attn_args(q, k, v, out, lse, cfg, status);
+    if (cfg->zero_rest) ISO_TRY(zero_rest(g, out, nullptr, nullptr, lse, s));
     if (on_tensor_cores(cfg, q, k, v)) return attn_tc(g, attn_plan(q->rows, k->rows, *cfg), static_cast<float*>(workspace), s);
     return by_kind(q->dtype, cfg->head_dim, [&](auto* t, auto dp) -> int {
         return simt_forward<std::remove_pointer_t<decltype(t)>, decltype(dp)::value>(g, s);
@@ -272,6 +319,7 @@ int32_t iso_attn_grad(const iso_mat* dout, const iso_mat* q, const iso_mat* k, c
     g.dq = dq->data; g.dk = dk->data; g.dv = dv->data;
     g.lddq = dq->ld; g.lddk = dk->ld; g.lddv = dv->ld;
     g.delta = static_cast<float*>(workspace);
+    if (cfg->zero_rest) ISO_TRY(zero_rest(g, dq, dk, dv, nullptr, s));
     return by_kind(q->dtype, cfg->head_dim, [&](auto* t, auto dp) -> int {
         using T = std::remove_pointer_t<decltype(t)>;
         if (q->rows) {

@@ -7,31 +7,33 @@
 // logits once:
 //   k_distill       a cluster of 1 ... 8 CTAs holds a whole row in registers, as
 //                   it was loaded (up to ten 16-byte words a thread), so every
-//                   load of a row is in flight at once; statistics per thread,
-//                   then warp, CTA and cluster (distributed shared memory), and
-//                   the gradient from the same registers.  The K entries are
-//                   gathered beside the row and put right after it, by the CTA
-//                   that owns their columns.
+//                   load of a row is in flight at once; statistics per warp, CTA
+//                   and cluster (distributed shared memory), and the gradient
+//                   from the same registers.  A warp of its own takes the
+//                   teacher's side beside the loads: its softmax, the logits at
+//                   its ids, the loss, and after the row the entries at the ids, each
+//                   by the CTA that owns its column.
 //   k_distill_long  rows that do not fit, or whose logits and gradient do not
 //                   sit alike in 16-byte words: one CTA a row, two passes.
 // A row off a 16-byte boundary is taken as its words from the first boundary on;
 // the entries before and behind them (under one word each) go one by one.
-// Statistics: each thread keeps its maximum m and sum of exp(x - m); pairs are
-// joined as (max, s1 exp(m1 - max) + s2 exp(m2 - max)) in a fixed order.
+// Statistics: a warp takes its maximum m and its sum of exp((x - m) / tau), and
+// sums of several warps and CTAs are joined as sum of s_i exp((m_i - m) / tau), m
+// the largest m_i, in a fixed order.  In the exponents m / tau is a level, rounded
+// once, that lse takes back: exp(x / tau - level) then has one rounding, of a
+// number that is small where the weight is not.
 #include "iso_train.cuh"
 #include "iso_internal.cuh"
 
 #include <algorithm>
 #include <cmath>
-#include <cooperative_groups.h>
-
-namespace cg = cooperative_groups;
 
 namespace iso {
 namespace {
 
 constexpr int DI_MAX_CLUSTER = 8;
 constexpr int DI_MAX_WORDS = 10;         // 16-byte words of a row a thread holds
+constexpr int DI_WARP_TOP = 128;         // up to this many slots the teacher's warp adds up equal ids alone
 constexpr float LOG2E = 1.4426950408889634f;
 
 struct DistillArgs {
@@ -46,17 +48,13 @@ struct DistillArgs {
     int32_t* status;
     long long ldz, ldt, ldg;
     int32_t rows, vocab, top;
-    int32_t ids_i64, teacher_f32;
+    int32_t ids_i64, teacher_f32, cluster;
     float tau, inv_tau;
 };
 
-// m = -Inf where nothing was seen (then s = 0)
-struct Stat {
-    float m, s;
-};
-// exp(x / tau) for a bf16 row by the hardware's exponential (2 ulp, far below the
-// rounding of the gradient, and random beside one another in the sum), for a
-// binary32 row by expf
+// exp(x / tau - level): of a bf16 row by the hardware's exponential (2 ulp, far
+// below the rounding of the gradient, and random beside one another in the sum) of
+// base 2, of a binary32 row by expf.
 template <bool FAST>
 struct Exp {
     float c;
@@ -70,47 +68,88 @@ struct Exp {
             return expf(x);
         }
     }
-    __device__ __forceinline__ float below(float x, float top) const { return of((x - top) * c); }   // exp((x - top) / tau)
-    // exp(x / tau - m), m given as level(m)
-    __device__ __forceinline__ float level(float m) const { return FAST ? m * LOG2E : m; }
-    __device__ __forceinline__ float against(float x, float l) const { return of(fmaf(x, c, -l)); }
-};
-__device__ __forceinline__ Stat join(Stat a, Stat b) {
-    const float m = fmaxf(a.m, b.m);
-    // equal maxima (two infinities of one sign among them) need no scaling
-    const float sa = a.m == m ? a.s : a.s * expf(a.m - m), sb = b.m == m ? b.s : b.s * expf(b.m - m);
-    return {m, sa + sb};
-}
-__device__ __forceinline__ Stat warp_join(Stat a) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        const Stat b = {__shfl_xor_sync(0xFFFFFFFFu, a.m, o), __shfl_xor_sync(0xFFFFFFFFu, a.s, o)};
-        a = join(a, b);
+    // of a maximum; 0 where there is none, so that -Inf weighs 0
+    __device__ __forceinline__ float level(float m) const { return m == -INFINITY ? 0.0f : m * c; }
+    __device__ __forceinline__ float level_of(float lse) const { return FAST ? lse * LOG2E : lse; }
+    __device__ __forceinline__ float lse(float level, float s) const {
+        return FAST ? (level + log2f(s)) * 0.6931471805599453f : level + logf(s);
     }
-    return a;
+    __device__ __forceinline__ float at(float x, float level) const { return of(fmaf(x, c, -level)); }
+};
+
+// two at a time
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void parts_of(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// m: the largest entry (-Inf: none); s: the sum of exp(x / tau - level(m))
+struct Stat {
+    float m, s;
+};
+template <bool FAST>
+__device__ __forceinline__ Stat join_lanes(Stat a, int lanes, const Exp<FAST>& ex) {     // of `lanes` lanes (a power of two)
+    float m = a.m;
+    for (int o = lanes / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    float s = a.m == m ? a.s : a.s * ex.of(ex.level(a.m) - ex.level(m));
+    if (a.m == -INFINITY) s = a.s;                  // 0, or NaN
+    for (int o = lanes / 2; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    return {m, s};
 }
 
 __device__ __forceinline__ long long id_at(const DistillArgs& g, long long i) {
     return g.ids_i64 ? static_cast<const long long*>(g.ids)[i] : (long long)static_cast<const int*>(g.ids)[i];
 }
+__device__ __forceinline__ float warp_sum(float s) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    return s;
+}
 
-// The teacher's side of a row, in shared memory of each CTA: ids (-1: unused),
-// probabilities, and the logits at the ids.
+// The teacher's side of a row, in shared memory of each CTA
 struct Top {
-    int* id;
-    float* p;
-    float* z;
+    int* id;                 // -1: unused
+    float* p;                // probabilities
+    float* z;                // logits at the ids
+    float* mass;             // probabilities of all slots of the id together
 };
+__device__ __forceinline__ Top top_of(float* smem, int n) {
+    return {reinterpret_cast<int*>(smem), smem + n, smem + 2 * n, smem + 3 * n};
+}
+constexpr int DI_TOP_BYTES = 16;
 
-// NT threads; t.z must be gathered by the caller.  Returns false where the row
-// has no used slot with a finite weight (loss and gradient 0).
-template <int NT>
-__device__ __forceinline__ bool teacher_side(const DistillArgs& g, int row, const Top& t, float* red) {
+__device__ __forceinline__ float mass_of(const Top& t, int top, int id) {
+    float p = 0.0f;
+    for (int j = 0; j < top; ++j) p += t.id[j] == id ? t.p[j] : 0.0f;
+    return p;
+}
+
+// By one warp; z is read at the ids in [from, to).  Whether the row has a used slot
+// with a weight (else its loss and gradient are 0).
+template <typename T>
+__device__ __forceinline__ bool teacher_side(const DistillArgs& g, int row, const T* z, const Top& t, int from, int to) {
+    const int lane = threadIdx.x & 31;
     float m = -INFINITY;
     bool nan = false;
-    for (int k = threadIdx.x; k < g.top; k += NT) {
-        const long long v = id_at(g, (long long)row * g.top + k);
-        const long long at = (long long)row * g.ldt + k;
+    for (int k = lane; k < g.top; k += 32) {
+        const long long v = id_at(g, (long long)row * g.top + k), at = (long long)row * g.ldt + k;
         const bool used = v >= 0 && v < g.vocab;
         if (!used && v != -1 && g.status) atomicCAS(g.status, 0, (int32_t)ISO_ERR_INDEX);
         float x = -INFINITY;
@@ -119,74 +158,57 @@ __device__ __forceinline__ bool teacher_side(const DistillArgs& g, int row, cons
                                : __bfloat162float(static_cast<const __nv_bfloat16*>(g.teacher)[at])) * g.inv_tau;
         t.id[k] = used ? (int)v : -1;
         t.p[k] = x;
+        t.z[k] = v >= from && v < to ? to_f32(z[v]) : 0.0f;
         m = fmaxf(m, x);
         nan |= x != x;
     }
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
     nan = __any_sync(0xFFFFFFFFu, nan);
-    if (lane == 0) red[warp] = nan ? __int_as_float(0x7FFFFFFF) : m;
-    __syncthreads();
-    m = -INFINITY;
-    nan = false;
-#pragma unroll
-    for (int w = 0; w < NT / 32; ++w) {
-        const float x = red[w];
-        m = fmaxf(m, x);
-        nan |= x != x;
-    }
     if (m == -INFINITY && !nan) return false;
-    if (nan) m = __int_as_float(0x7FFFFFFF);
     float s = 0.0f;
-    for (int k = threadIdx.x; k < g.top; k += NT) {
-        const float x = t.id[k] < 0 ? 0.0f : expf(t.p[k] - m);
+    for (int k = lane; k < g.top; k += 32) {
+        const float x = t.id[k] < 0 ? 0.0f : expf(t.p[k] - (nan ? __int_as_float(0x7FFFFFFF) : m));
         t.p[k] = x;
         s += x;
     }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-    __syncthreads();
-    if (lane == 0) red[warp] = s;
-    __syncthreads();
-    s = 0.0f;
-#pragma unroll
-    for (int w = 0; w < NT / 32; ++w) s += red[w];
-    for (int k = threadIdx.x; k < g.top; k += NT) t.p[k] = t.p[k] / s;
+    s = warp_sum(s);
+    for (int k = lane; k < g.top; k += 32) t.p[k] = t.p[k] / s;
+    __syncwarp();
+    if (g.grad && g.top <= DI_WARP_TOP)
+        for (int k = lane; k < g.top; k += 32) t.mass[k] = mass_of(t, g.top, t.id[k]);
     return true;
 }
 
-// sum_k p_k (log p_k - z_k / tau + lse), by the whole CTA, in a fixed order
-template <int NT>
-__device__ __forceinline__ float divergence(const DistillArgs& g, const Top& t, float lse, float* red) {
+// sum_k p_k (log p_k - z_k / tau + lse), by one warp
+__device__ __forceinline__ float divergence(const DistillArgs& g, const Top& t, float lse) {
     float s = 0.0f;
-    for (int k = threadIdx.x; k < g.top; k += NT) {
+    for (int k = threadIdx.x & 31; k < g.top; k += 32) {
         const float p = t.p[k];
         if (t.id[k] >= 0 && p != 0.0f) s += p * (logf(p) - (t.z[k] * g.inv_tau - lse));
     }
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-    __syncthreads();
-    if (lane == 0) red[warp] = s;
-    __syncthreads();
-    s = 0.0f;
-#pragma unroll
-    for (int w = 0; w < NT / 32; ++w) s += red[w];
-    return s;
+    return warp_sum(s);
 }
 
-// The entries at the teacher's ids among columns [c0, c1): the probabilities of
-// all slots with the id, in slot order, off the student's.  Slots of one id write
-// the same value.  q(z) is the student's probability.
-template <int NT, typename T, typename Q>
-__device__ __forceinline__ void put_right(const DistillArgs& g, const Top& t, T* grad, int c0, int c1, float scale, Q q) {
-    for (int k = threadIdx.x; k < g.top; k += NT) {
+// The entries at the teacher's ids among columns [c0, c1), after the row: slots of
+// one id write the same value.  q(z): scale times the student's probability.  By
+// the whole CTA of `warps` warps, the last of them the teacher's.
+template <typename T, typename Q>
+__device__ __forceinline__ void put_right(const DistillArgs& g, const Top& t, T* grad, int c0, int c1, float scale, int warps, Q q) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (g.top <= DI_WARP_TOP) {
+        if (warp != warps - 1) return;
+        for (int k = lane; k < g.top; k += 32)
+            if (t.id[k] >= c0 && t.id[k] < c1) from_f32(q(t.z[k]) - scale * t.mass[k], grad[t.id[k]]);
+        return;
+    }
+    for (int k = warp; k < g.top; k += warps) {       // many slots: a warp adds up each id's
         const int id = t.id[k];
         if (id < c0 || id >= c1) continue;
         float p = 0.0f;
-        for (int j = 0; j < g.top; ++j) p += t.id[j] == id ? t.p[j] : 0.0f;
-        from_f32(scale * (q(t.z[k]) - p), grad[id]);
+        for (int j = lane; j < g.top; j += 32) p += t.id[j] == id ? t.p[j] : 0.0f;
+        p = warp_sum(p);
+        if (lane == 0) from_f32(q(t.z[k]) - scale * p, grad[id]);
     }
 }
 
@@ -194,23 +216,41 @@ template <typename T>
 struct Word {                            // 16 bytes of a row
     static constexpr int N = 16 / sizeof(T);
     uint4 w;
-    __device__ __forceinline__ void get(float (&v)[N]) const {
-        if constexpr (sizeof(T) == 2) {
-            bf16x2_to_f32(w.x, v[0], v[1]);
-            bf16x2_to_f32(w.y, v[2], v[3]);
-            bf16x2_to_f32(w.z, v[4], v[5]);
-            bf16x2_to_f32(w.w, v[6], v[7]);
-        } else {
-            v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y);
-            v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
+    __device__ __forceinline__ void get(uint64_t (&v)[N / 2]) const {
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            if constexpr (sizeof(T) == 2) {
+                float a, b;
+                bf16x2_to_f32(u[i], a, b);
+                v[i] = pair_of(a, b);
+            } else {
+                v[i] = pair_of(__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]));
+            }
         }
     }
-    __device__ __forceinline__ void set(const float (&v)[N]) {
-        if constexpr (sizeof(T) == 2)
-            w = make_uint4(f32_to_bf16x2(v[0], v[1]), f32_to_bf16x2(v[2], v[3]), f32_to_bf16x2(v[4], v[5]),
-                           f32_to_bf16x2(v[6], v[7]));
-        else
-            w = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    __device__ __forceinline__ void set(const uint64_t (&v)[N / 2]) {
+        uint32_t u[4];
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+            float a, b;
+            parts_of(v[i], a, b);
+            if constexpr (sizeof(T) == 2) u[i] = f32_to_bf16x2(a, b);
+            else {
+                u[2 * i] = __float_as_uint(a);
+                u[2 * i + 1] = __float_as_uint(b);
+            }
+        }
+        w = make_uint4(u[0], u[1], u[2], u[3]);
+    }
+    __device__ __forceinline__ float top() const {      // a NaN counts as nothing
+        if constexpr (sizeof(T) == 2) {
+            const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&w);
+            const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+            return fmaxf(__low2float(m), __high2float(m));
+        } else {
+            return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
+        }
     }
 };
 
@@ -220,175 +260,242 @@ __device__ __forceinline__ int entries_before(const T* row, int n) {
     const int off = (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15u)) & 15u) / (int)sizeof(T);
     return min(off, n);
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-// m and s of a thread's entries so far, with one more value
-__device__ __forceinline__ void add_one(Stat& a, float x) {
-    const float m = fmaxf(a.m, x);
-    if (m == -INFINITY) {
-        a.s += x == x ? 0.0f : x;        // a NaN beside nothing else
-        return;
-    }
-    a.s = (a.m == m ? a.s : a.s * expf(a.m - m)) + expf(x - m);
-    a.m = m;
-}
+template <int THREADS>
+__device__ __forceinline__ void sync_some(int barrier) { asm volatile("bar.sync %0, %1;" :: "r"(barrier), "n"(THREADS) : "memory"); }
+template <int THREADS>
+__device__ __forceinline__ void arrive_some(int barrier) { asm volatile("bar.arrive %0, %1;" :: "r"(barrier), "n"(THREADS) : "memory"); }
 
+// NT threads hold the row, 32 more are the teacher's.  The row does not wait for
+// the teacher's side, a chain of loads, before its own entries are out: a row
+// without any is cleared afterwards.  Only in place the gradient waits until the
+// logits at the ids have been read.
 template <typename T, int NT, int WORDS>
-__global__ void __launch_bounds__(NT, NT * WORDS <= 2560 ? 2 : 1) k_distill(DistillArgs g) {
-    constexpr int N = Word<T>::N;
+__global__ void __launch_bounds__(NT + 32, NT == 512 ? 2 : NT == 256 ? 4 : 6) k_distill(const __grid_constant__ DistillArgs g) {
+    constexpr int N = Word<T>::N, WARPS = NT / 32;
     constexpr bool FAST = sizeof(T) == 2;
     extern __shared__ float di_smem[];
-    __shared__ float red[NT / 32];
-    __shared__ Stat parts[NT / 32], mine;
-    const Top t = {reinterpret_cast<int*>(di_smem), di_smem + g.top, di_smem + 2 * g.top};
-    cg::cluster_group cluster = cg::this_cluster();
-    const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const int row = (int)(blockIdx.x / C);
+    __shared__ Stat parts[WARPS], of_cta[DI_MAX_CLUSTER];
+    __shared__ int any_s;
+    const Top t = top_of(di_smem, g.top);
+    const int C = g.cluster, rank = C > 1 ? (int)(blockIdx.x % C) : 0;
+    const int row = (int)(blockIdx.x / C), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const bool joint = g.lse_in == nullptr;
+    if (C > 1 && joint) cluster_arrive();
     const T* z = static_cast<const T*>(g.z) + (long long)row * g.ldz;
     T* grad = g.grad ? static_cast<T*>(g.grad) + (long long)row * g.ldg : nullptr;
+    const bool in_place = g.grad == g.z;
+    const Exp<FAST> ex(g.inv_tau);
 
     // this CTA's words of the row; entry e of the row is column e
     const int before = entries_before(z, g.vocab), words = (g.vocab - before) / N;
     const int share = (words + C - 1) / C, w0 = min(words, rank * share), w1 = min(words, w0 + share);
     const int behind = before + words * N;                       // the entries from here on go one by one
     const int c0 = rank == 0 ? 0 : before + w0 * N, c1 = rank == C - 1 ? g.vocab : before + w1 * N;
-    Word<T> x[WORDS];
-#pragma unroll
-    for (int i = 0; i < WORDS; ++i) {
-        const int w = w0 + i * NT + (int)threadIdx.x;
-        if (w < w1) x[i].w = __ldcs(reinterpret_cast<const uint4*>(z + before) + w);
-    }
-    // one entry a thread: before the words with the first CTA, behind them with the last
-    int single = -1;
-    if (rank == 0 && (int)threadIdx.x < before) single = threadIdx.x;
-    const int back = NT - 1 - (int)threadIdx.x;                  // NT > two words' entries: another thread
-    if (rank == C - 1 && behind + back < g.vocab) single = behind + back;
-    const float xs = single >= 0 ? to_f32(z[single]) : -INFINITY;
-
-    const bool any = teacher_side<NT>(g, row, t, red);
-    // the logits at the ids: all of them for the loss, those of this CTA's columns
-    // for the gradient (in place, others may be overwritten already)
-    const int from = rank == 0 && !g.lse_in ? 0 : c0, to = rank == 0 && !g.lse_in ? g.vocab : c1;
-    for (int k = threadIdx.x; k < g.top; k += NT) t.z[k] = t.id[k] >= from && t.id[k] < to ? to_f32(z[t.id[k]]) : 0.0f;
-
-    const Exp<FAST> ex(g.inv_tau);
-    float m, inv_s = 1.0f, lse;
-    if (g.lse_in) {
-        m = lse = g.lse_in[row];
-        __syncthreads();
-    } else {
+    // of the CTA's partial sums: the cluster's maximum (as a level) and sum
+    auto all_of = [&](Stat a) {
+        a.m = __shfl_sync(0xFFFFFFFFu, a.m, 0);
+        a.s = __shfl_sync(0xFFFFFFFFu, a.s, 0);
+        return a;
+    };
+    auto of_warps = [&] {
         Stat a = {-INFINITY, 0.0f};
+        if (lane < WARPS) a = parts[lane];
+        return all_of(join_lanes(a, WARPS, ex));
+    };
+    auto of_ctas = [&] {
+        Stat a = {-INFINITY, 0.0f};
+        if (lane < C) a = of_cta[lane];
+        return all_of(join_lanes(a, DI_MAX_CLUSTER, ex));
+    };
+    const float dloss = grad ? g.dloss[row] : 0.0f;
+    const float lse_in = joint ? 0.0f : g.lse_in[row];
+    float level = 0.0f, by = 0.0f, xs = -INFINITY;
+    int single = -1;
+    if (warp < WARPS) {
+        Word<T> x[WORDS];
+        const uint4* at = reinterpret_cast<const uint4*>(z + before) + w0 + threadIdx.x;
 #pragma unroll
-        for (int i = 0; i < WORDS; ++i) {
-            if (w0 + i * NT + (int)threadIdx.x >= w1) continue;
-            float v[N];
-            x[i].get(v);
-            float top = v[0];
+        for (int i = 0; i < WORDS; ++i)
+            if (w0 + i * NT + (int)threadIdx.x < w1) x[i].w = __ldcs(at + i * NT);
+        // one entry a thread: before the words with the first CTA, behind them with the last
+        if (rank == 0 && (int)threadIdx.x < before) single = threadIdx.x;
+        const int back = NT - 1 - (int)threadIdx.x;              // NT > two words' entries: another thread
+        if (rank == C - 1 && behind + back < g.vocab) single = behind + back;
+        if (single >= 0) xs = to_f32(z[single]);
+        float inv_s = 1.0f;
+        if (joint) {
+            Stat a = {xs, 0.0f};
 #pragma unroll
-            for (int j = 1; j < N; ++j) top = fmaxf(top, v[j]);
-            a.m = fmaxf(a.m, top);
-        }
-        a.m = fmaxf(a.m, xs);
-        // a thread whose entries are all -Inf (or NaN) sums against 0
-        const float base = a.m == -INFINITY ? 0.0f : a.m;
+            for (int i = 0; i < WORDS; ++i)
+                if (w0 + i * NT + (int)threadIdx.x < w1) a.m = fmaxf(a.m, x[i].top());
+            if (a.m != a.m) a.m = -INFINITY;                     // (xs alone may be NaN)
 #pragma unroll
-        for (int i = 0; i < WORDS; ++i) {
-            if (w0 + i * NT + (int)threadIdx.x >= w1) continue;
-            float v[N];
-            x[i].get(v);
+            for (int o = 16; o; o >>= 1) a.m = fmaxf(a.m, __shfl_xor_sync(0xFFFFFFFFu, a.m, o));
+            level = ex.level(a.m);
+            const uint64_t cc = pair_of(ex.c, ex.c), ll = pair_of(-level, -level);
+            uint64_t sum = pair_of(0.0f, 0.0f);
 #pragma unroll
-            for (int j = 0; j < N; ++j) a.s += ex.below(v[j], base);
-        }
-        a.s += ex.below(xs, base);
-        a.m *= g.inv_tau;
-        a = warp_join(a);
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        if (lane == 0) parts[warp] = a;
-        __syncthreads();
-        a = parts[0];
+            for (int i = 0; i < WORDS; ++i) {
+                if (w0 + i * NT + (int)threadIdx.x >= w1) continue;
+                uint64_t v[N / 2];
+                x[i].get(v);
 #pragma unroll
-        for (int w = 1; w < NT / 32; ++w) a = join(a, parts[w]);
-        if (C > 1) {
-            if (threadIdx.x == 0) mine = a;
-            cluster.sync();              // also: every CTA has gathered its entries, the row may be overwritten
-            a = *cluster.map_shared_rank(&mine, 0);
-            for (int r = 1; r < C; ++r) a = join(a, *cluster.map_shared_rank(&mine, r));
-        }
-        m = a.m;
-        inv_s = 1.0f / a.s;
-        lse = m + logf(a.s);
-        if (rank == 0) {
-            const float d = any ? divergence<NT>(g, t, lse, red) : 0.0f;
-            if (threadIdx.x == 0) {
-                g.loss[row] = any ? g.tau * g.tau * d : 0.0f;
-                g.lse[row] = lse;
+                for (int j = 0; j < N / 2; ++j) {
+                    float p, q;
+                    parts_of(fma2(v[j], cc, ll), p, q);
+                    sum = add2(sum, pair_of(ex.of(p), ex.of(q)));
+                }
             }
+            float p, q;
+            parts_of(sum, p, q);
+            a.s = warp_sum(p + q + (single >= 0 ? ex.at(xs, level) : 0.0f));
+            if (lane == 0) parts[warp] = a;
+            if (C == 1) arrive_some<NT + 32>(2);                 // for the teacher's warp
+            if (C > 1 || grad) {
+                sync_some<NT>(1);
+                a = of_warps();
+            }
+            if (C > 1) {
+                cluster_wait();          // every CTA of the cluster runs
+                if (warp == 0 && lane < C) {
+                    uint32_t to;
+                    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_u32(&of_cta[rank])), "r"(lane));
+                    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" :: "r"(to), "f"(a.m), "f"(a.s) : "memory");
+                }
+                __syncwarp();
+                cluster_arrive();
+                cluster_wait();
+                a = of_ctas();
+            } else if (in_place) {
+                sync_some<NT + 32>(3);   // the logits at the ids have been read
+            }
+            level = ex.level(a.m);
+            inv_s = 1.0f / a.s;
+        } else {
+            level = ex.level_of(lse_in);
+            if (in_place) sync_some<NT + 32>(3);
+        }
+        by = dloss * g.tau * inv_s;
+        if (grad) {
+            const uint64_t cc = pair_of(ex.c, ex.c), ll = pair_of(-level, -level), bb = pair_of(by, by);
+            uint4* out = reinterpret_cast<uint4*>(grad + before) + w0 + threadIdx.x;
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) {
+                if (w0 + i * NT + (int)threadIdx.x >= w1) continue;
+                uint64_t v[N / 2];
+                x[i].get(v);
+#pragma unroll
+                for (int j = 0; j < N / 2; ++j) {
+                    float p, q;
+                    parts_of(fma2(v[j], cc, ll), p, q);
+                    v[j] = mul2(pair_of(ex.of(p), ex.of(q)), bb);
+                }
+                x[i].set(v);
+                __stcs(out + i * NT, x[i].w);
+            }
+            if (single >= 0) from_f32(by * ex.at(xs, level), grad[single]);
+        }
+    } else {
+        if (C > 1 && joint) {
+            cluster_wait();
+            if (!in_place) cluster_arrive();
+        }
+        // the logits at the ids: all of them for the loss, those of this CTA's columns
+        // for the gradient (in place, others may be overwritten already)
+        const bool all = rank == 0 && joint;
+        const bool any = (grad || rank == 0) && teacher_side(g, row, z, t, all ? 0 : c0, all ? g.vocab : c1);
+        if (lane == 0) any_s = any;
+        if (C > 1 && joint) {
+            if (in_place) cluster_arrive();
+            cluster_wait();
+        } else if (in_place) {
+            sync_some<NT + 32>(3);
+        }
+        if (joint) {
+            if (C == 1) sync_some<NT + 32>(2);
+            const Stat a = C > 1 ? of_ctas() : of_warps();
+            level = ex.level(a.m);
+            by = dloss * g.tau / a.s;
+            if (rank == 0) {
+                const float lse = a.m == -INFINITY && a.s == 0.0f ? -INFINITY : ex.lse(level, a.s);
+                const float d = any ? divergence(g, t, lse) : 0.0f;
+                if (lane == 0) {
+                    g.loss[row] = any ? g.tau * g.tau * d : 0.0f;
+                    g.lse[row] = lse;
+                }
+            }
+        } else {
+            level = ex.level_of(lse_in);
+            by = dloss * g.tau;
         }
     }
-    if (grad) {
-        const float scale = any ? g.dloss[row] * g.tau : 0.0f;
-        const float level = ex.level(m);
-        auto q = [&](float v) { return ex.against(v, level) * inv_s; };      // (from lse alone: s = 1)
-        uint4* out = reinterpret_cast<uint4*>(grad + before);
-#pragma unroll
-        for (int i = 0; i < WORDS; ++i) {
-            const int w = w0 + i * NT + (int)threadIdx.x;
-            if (w >= w1) continue;
-            float v[N];
-            x[i].get(v);
-#pragma unroll
-            for (int j = 0; j < N; ++j) v[j] = any ? scale * q(v[j]) : 0.0f;
-            x[i].set(v);
-            __stcs(out + w, x[i].w);
-        }
-        if (single >= 0) from_f32(any ? scale * q(xs) : 0.0f, grad[single]);
-        __syncthreads();
-        if (any) put_right<NT>(g, t, grad, c0, c1, scale, q);
+    if (!grad) return;
+    __syncthreads();
+    if (any_s) {
+        put_right(g, t, grad, c0, c1, dloss * g.tau, WARPS + 1, [&](float v) { return by * ex.at(v, level); });
+    } else {
+        for (int c = c0 + (int)threadIdx.x; c < c1; c += NT + 32) from_f32(0.0f, grad[c]);
     }
-    if (C > 1 && !g.lse_in) cluster.sync();      // the others have read this CTA's statistics
 }
 
 // Any row: one CTA, the logits read once for the statistics and once more for
 // the gradient, entry by entry.
 template <typename T, int NT>
-__global__ void __launch_bounds__(NT) k_distill_long(DistillArgs g) {
+__global__ void __launch_bounds__(NT) k_distill_long(const __grid_constant__ DistillArgs g) {
+    constexpr int WARPS = NT / 32;
     extern __shared__ float di_smem[];
-    __shared__ float red[NT / 32];
-    __shared__ Stat parts[NT / 32];
-    const Top t = {reinterpret_cast<int*>(di_smem), di_smem + g.top, di_smem + 2 * g.top};
-    const int row = (int)blockIdx.x;
+    __shared__ Stat parts[WARPS];
+    __shared__ int any_s;
+    const Top t = top_of(di_smem, g.top);
+    const int row = (int)blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const T* z = static_cast<const T*>(g.z) + (long long)row * g.ldz;
-    const bool any = teacher_side<NT>(g, row, t, red);
-    for (int k = threadIdx.x; k < g.top; k += NT) t.z[k] = t.id[k] >= 0 ? to_f32(z[t.id[k]]) : 0.0f;
-    float m, inv_s = 1.0f;
-    if (g.lse_in) {
-        m = g.lse_in[row];
-        __syncthreads();
-    } else {
-        Stat a = {-INFINITY, 0.0f};
-#pragma unroll 4
-        for (int c = threadIdx.x; c < g.vocab; c += NT) add_one(a, to_f32(z[c]) * g.inv_tau);
-        a = warp_join(a);
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const Exp<false> ex(g.inv_tau);
+    if (warp == WARPS - 1) {
+        const bool any = teacher_side(g, row, z, t, 0, g.vocab);
+        if (lane == 0) any_s = any;
+    }
+    Stat a = {-INFINITY, 0.0f};
+    if (!g.lse_in) {
+#pragma unroll 8
+        for (int c = threadIdx.x; c < g.vocab; c += NT) a.m = fmaxf(a.m, to_f32(z[c]));
+#pragma unroll
+        for (int o = 16; o; o >>= 1) a.m = fmaxf(a.m, __shfl_xor_sync(0xFFFFFFFFu, a.m, o));
+        const float level = ex.level(a.m);
+#pragma unroll 8
+        for (int c = threadIdx.x; c < g.vocab; c += NT) a.s += ex.at(to_f32(z[c]), level);
+        a.s = warp_sum(a.s);
         if (lane == 0) parts[warp] = a;
-        __syncthreads();
-        a = parts[0];
-        for (int w = 1; w < NT / 32; ++w) a = join(a, parts[w]);
-        m = a.m;
+    }
+    __syncthreads();
+    const bool any = any_s;
+    float level, inv_s = 1.0f;
+    if (g.lse_in) {
+        level = ex.level_of(g.lse_in[row]);
+    } else {
+        a = {-INFINITY, 0.0f};
+        if (lane < WARPS) a = parts[lane];
+        a = join_lanes(a, WARPS, ex);
+        level = ex.level(a.m);
         inv_s = 1.0f / a.s;
-        const float lse = m + logf(a.s), d = any ? divergence<NT>(g, t, lse, red) : 0.0f;
-        if (threadIdx.x == 0) {
-            g.loss[row] = any ? g.tau * g.tau * d : 0.0f;
-            g.lse[row] = lse;
+        if (warp == WARPS - 1) {
+            const float lse = a.m == -INFINITY && a.s == 0.0f ? -INFINITY : ex.lse(level, a.s);
+            const float d = any ? divergence(g, t, lse) : 0.0f;
+            if (lane == 0) {
+                g.loss[row] = any ? g.tau * g.tau * d : 0.0f;
+                g.lse[row] = lse;
+            }
         }
     }
     if (!g.grad) return;
     T* grad = static_cast<T*>(g.grad) + (long long)row * g.ldg;
-    const float scale = any ? g.dloss[row] * g.tau : 0.0f;
-    auto q = [&](float v) { return expf(v * g.inv_tau - m) * inv_s; };
-#pragma unroll 4
-    for (int c = threadIdx.x; c < g.vocab; c += NT) from_f32(any ? scale * q(to_f32(z[c])) : 0.0f, grad[c]);
+    const float scale = any ? g.dloss[row] * g.tau : 0.0f, by = scale * inv_s;
+#pragma unroll 8
+    for (int c = threadIdx.x; c < g.vocab; c += NT) from_f32(any ? by * ex.at(to_f32(z[c]), level) : 0.0f, grad[c]);
     __syncthreads();
-    if (any) put_right<NT>(g, t, grad, 0, g.vocab, scale, q);
+    if (any) put_right(g, t, grad, 0, g.vocab, scale, WARPS, [&](float v) { return by * ex.at(v, level); });
 }
 
 int check_distill(const iso_mat* z, const void* ids, int32_t ids_i64, const iso_mat* teacher, float tau,
@@ -409,11 +516,12 @@ int check_distill(const iso_mat* z, const void* ids, int32_t ids_i64, const iso_
 Bytes2D flat(const void* p, uint64_t bytes) { return {reinterpret_cast<uintptr_t>(p), 1, bytes, bytes}; }
 
 template <typename T, int NT, int WORDS>
-int launch_rows(const DistillArgs& g, int cluster, cudaStream_t s) {
+int launch_rows(DistillArgs g, int cluster, cudaStream_t s) {
+    g.cluster = cluster;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)g.rows * (unsigned)cluster);
-    cfg.blockDim = dim3(NT);
-    cfg.dynamicSmemBytes = (size_t)g.top * 12;
+    cfg.blockDim = dim3(NT + 32);
+    cfg.dynamicSmemBytes = (size_t)g.top * DI_TOP_BYTES;
     cfg.stream = s;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeClusterDimension;
@@ -433,18 +541,16 @@ int launch_distill(const DistillArgs& g, cudaStream_t s) {
                                    (g.rows == 1 || (g.ldz - g.ldg) * (long long)sizeof(T) % 16 == 0));
     const int words = g.vocab / N;
     if (!alike || words > DI_MAX_CLUSTER * 512 * DI_MAX_WORDS || (long long)g.rows * DI_MAX_CLUSTER > EXTENT_LIMIT) {
-        TRAIN_LAUNCH((k_distill_long<T, 1024><<<(unsigned)g.rows, 1024, (size_t)g.top * 12, s>>>(g)));
+        TRAIN_LAUNCH((k_distill_long<T, 1024><<<(unsigned)g.rows, 1024, (size_t)g.top * DI_TOP_BYTES, s>>>(g)));
         return ISO_OK;
     }
     if (words <= 128 * 4) return words <= 128 ? launch_rows<T, 128, 1>(g, 1, s) : launch_rows<T, 128, 4>(g, 1, s);
+    if (words > DI_MAX_CLUSTER * 256 * DI_MAX_WORDS) return launch_rows<T, 512, DI_MAX_WORDS>(g, DI_MAX_CLUSTER, s);
     // the smallest cluster that holds a row; larger ones while they leave SMs idle
     int C = 1;
-    while (words > C * 512 * DI_MAX_WORDS) C *= 2;
-    while (C < DI_MAX_CLUSTER && (long long)g.rows * C * 2 <= train_sms() && words > C * 512) C *= 2;
-    const int need = (words + C * 512 - 1) / (C * 512);
-    if (need <= 2) return launch_rows<T, 512, 2>(g, C, s);
-    if (need <= 5) return launch_rows<T, 512, 5>(g, C, s);
-    return launch_rows<T, 512, DI_MAX_WORDS>(g, C, s);
+    while (words > C * 256 * DI_MAX_WORDS) C *= 2;
+    while (C < DI_MAX_CLUSTER && (long long)g.rows * C * 2 <= train_sms() && words > C * 256) C *= 2;
+    return words <= C * 256 * 5 ? launch_rows<T, 256, 5>(g, C, s) : launch_rows<T, 256, DI_MAX_WORDS>(g, C, s);
 }
 
 int run_distill(DistillArgs& g, const iso_mat* z, const void* ids, int32_t ids_i64, const iso_mat* teacher, float tau,

@@ -21,8 +21,12 @@ import torch
 from . import _abi
 from ._abi import IsoAttnCfg, IsoMat, IsoRopeCfg, check, lib
 from .api import Workspace
-from .train import _byref, _done, _here, _load_native, _mat, _new, _ptr, _scratch, _status
-from . import train as _train
+from . import train
+from .train import _byref, _done, _here, _mat, _new, _ptr, _scratch, _status
+
+
+def _native():
+    return train._native or train._load_native()
 
 
 def _vector(t: torch.Tensor, name: str, dtype, shape) -> int:
@@ -52,7 +56,7 @@ class RopePlan:
     """How heads turn by their positions (iso_rope_cfg): per pair of channels an
     angle per position and the axis its position is on.  Made once, by rope_plan."""
 
-    __slots__ = ("head_dim", "rot_dim", "axes", "pairs", "freq", "axis", "_forward", "_inverse")
+    __slots__ = ("head_dim", "rot_dim", "axes", "pairs", "freq", "axis", "_cfg", "_at")
 
     def __init__(self, head_dim: int, freq: Sequence[float], axis: Sequence[int], axes: int, pairs: str = "halves"):
         if pairs not in ("halves", "neighbours"):
@@ -68,9 +72,10 @@ class RopePlan:
             raise ValueError(f"{n} pairs do not fit a head of {head_dim} (or are more than {_abi.ISO_ROPE_MAX_PAIRS})")
         self.head_dim, self.rot_dim, self.axes, self.pairs = int(head_dim), 2 * n, int(axes), pairs
         self.freq, self.axis = (ctypes.c_double * max(n, 1))(*freq), (ctypes.c_int32 * max(n, 1))(*axis)
-        self._forward, self._inverse = (
-            IsoRopeCfg(self.head_dim, 2 * n, self.axes, int(pairs == "neighbours"), inverse, 0,
-                       ctypes.addressof(self.freq), ctypes.addressof(self.axis)) for inverse in (0, 1))
+        # the turn and the turn back, and their addresses
+        self._cfg = tuple(IsoRopeCfg(self.head_dim, 2 * n, self.axes, int(pairs == "neighbours"), inverse, 0,
+                                     ctypes.addressof(self.freq), ctypes.addressof(self.axis)) for inverse in (0, 1))
+        self._at = tuple(ctypes.addressof(c) for c in self._cfg)
 
     def __repr__(self):
         return f"RopePlan(head_dim={self.head_dim}, rot_dim={self.rot_dim}, axes={self.axes}, pairs={self.pairs!r})"
@@ -123,12 +128,15 @@ def _positions(positions: torch.Tensor, rows: int, axes: int):
     return positions.data_ptr(), i64, ld
 
 
-def _rope(x, positions, plan, out, stream, cfg, name):
+def _rope(x, positions, plan, out, stream, inverse, name):
     if not isinstance(plan, RopePlan):
         raise TypeError("plan must be a RopePlan")
+    if out is None and stream is None:
+        return _done(_native().rope(x, positions, plan._at[inverse], name), "iso_rope")
     if stream is not None:
         with torch.cuda.stream(stream):
-            return _rope(x, positions, plan, out, None, cfg, name)
+            return _rope(x, positions, plan, out, None, inverse, name)
+    cfg = plan._cfg[inverse]
     dx = _mat(x, name)
     ptr, i64, ld = _positions(positions, dx.rows, plan.axes)
     s = _here(x, positions, out)
@@ -145,13 +153,13 @@ def rope(x: torch.Tensor, positions: torch.Tensor, plan: RopePlan, out: Optional
     """x, heads of plan.head_dim side by side, turned by its rows' positions
     (iso_rope): int32 or int64 [axes, rows], or [rows] for one axis.  ``out`` may
     be x."""
-    return _rope(x, positions, plan, out, stream, plan._forward if isinstance(plan, RopePlan) else None, "x")
+    return _rope(x, positions, plan, out, stream, 0, "x")
 
 
 def rope_grad(dy: torch.Tensor, positions: torch.Tensor, plan: RopePlan, out: Optional[torch.Tensor] = None,
               stream=None) -> torch.Tensor:
     """The gradient of rope's input: dy turned back (iso_rope with inverse)."""
-    return _rope(dy, positions, plan, out, stream, plan._inverse if isinstance(plan, RopePlan) else None, "dy")
+    return _rope(dy, positions, plan, out, stream, 1, "dy")
 
 
 # ---------------------------------------------------------------------------
@@ -167,7 +175,7 @@ def _ends(t: Optional[torch.Tensor], name: str):
     return t.data_ptr(), t.numel() - 1
 
 
-def _attn_cfg(q: IsoMat, heads, kv_heads, scale, causal, window, seqs, kv_seqs) -> IsoAttnCfg:
+def _attn_cfg(q: IsoMat, heads, kv_heads, scale, causal, window, seqs, kv_seqs, zero_rest=False) -> IsoAttnCfg:
     heads = int(heads)
     kv_heads = heads if kv_heads is None else int(kv_heads)
     if heads < 1 or kv_heads < 1 or heads % kv_heads:
@@ -184,21 +192,8 @@ def _attn_cfg(q: IsoMat, heads, kv_heads, scale, causal, window, seqs, kv_seqs) 
     scale = dim ** -0.5 if scale is None else float(scale)
     if not (scale > 0 and math.isfinite(scale)):
         raise ValueError("scale must be positive and finite")
-    return IsoAttnCfg(heads, kv_heads, dim, int(bool(causal)), min(window, 1 << 40), scale, n, qe, ke)
-
-
-def _rows_new(like: IsoMat, packed: bool, dtype, device):
-    """A new matrix of like's shape; zeros where rows may belong to no sequence."""
-    t, m = _new(like.rows, like.cols, dtype, device)
-    if packed:
-        t.zero_()
-    return t, m
-
-
-def _lse(lse: Optional[torch.Tensor], heads: int, rows: int, packed: bool, device):
-    if lse is None:
-        lse = (torch.zeros if packed else torch.empty)((heads, rows), dtype=torch.float32, device=device)
-    return lse, _vector(lse, "lse", torch.float32, (heads, rows))
+    return IsoAttnCfg(heads, kv_heads, dim, int(bool(causal)), min(window, 1 << 40), scale, n, qe, ke,
+                      int(zero_rest), 0)
 
 
 def attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, heads: int, kv_heads: Optional[int] = None,
@@ -211,20 +206,25 @@ def attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, heads: int, kv_heads
     head_dim^-0.5; ``window`` limits the keys a query sees (0: no limit).
     ``seqs`` holds the packed sequences' offsets and their end (int32 on the
     device), ``kv_seqs`` the keys' where they differ: queries stand at the end of
-    their sequence's keys.  Rows of no sequence are not written, and zero in
-    tensors that the call allocates.  With status=True the device status comes
-    third."""
+    their sequence's keys.  Rows of no sequence are zero in tensors that the call
+    allocates; it does not write them where both out and lse are given.  With
+    status=True the device status comes third."""
+    if out is None and lse is None and workspace is None and stream is None and not status:
+        return _done(_native().attn(q, k, v, heads, heads if kv_heads is None else kv_heads, scale, bool(causal), window or 0,
+                                    seqs, kv_seqs), "iso_attn")
     if stream is not None:
         with torch.cuda.stream(stream):
             return attn(q, k, v, heads, kv_heads, scale, causal, window, seqs, kv_seqs, out, lse, workspace, status)
     dq, dk, dv = _mat(q, "q"), _mat(k, "k"), _mat(v, "v")
-    cfg = _attn_cfg(dq, heads, kv_heads, scale, causal, window, seqs, kv_seqs)
+    cfg = _attn_cfg(dq, heads, kv_heads, scale, causal, window, seqs, kv_seqs, out is None or lse is None)
     s = _here(q, k, v, seqs, kv_seqs, out, lse)
     if out is None:
-        out, do = _rows_new(dq, seqs is not None, q.dtype, q.device)
+        out, do = _new(dq.rows, dq.cols, q.dtype, q.device)
     else:
         do = _mat(out, "out")
-    lse, lptr = _lse(lse, cfg.heads, dq.rows, seqs is not None, q.device)
+    if lse is None:
+        lse = torch.empty((cfg.heads, dq.rows), dtype=torch.float32, device=q.device)
+    lptr = _vector(lse, "lse", torch.float32, (cfg.heads, dq.rows))
     ws, st, L, nb = _scratch(workspace, q.device), _status(status, q.device), lib(), ctypes.c_size_t(0)
     check(L.iso_attn_workspace_size(_byref(dq), _byref(dk), _byref(cfg), _byref(nb)), "iso_attn")
     check(L.iso_attn(_byref(dq), _byref(dk), _byref(dv), _byref(cfg), _byref(do), lptr, *ws.get(nb.value), _ptr(st), s),
@@ -239,18 +239,22 @@ def attn_grad(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Ten
               workspace: Optional[Workspace] = None, status=False, stream=None):
     """(dq, dk, dv) from the gradient of attn's out, its inputs, out and lse, with
     attn's other arguments (iso_attn_grad).  ``grads`` gives the tensors to write,
-    possibly column ranges of one buffer.  The same inputs give the same bits.
-    With status=True the device status comes fourth."""
+    possibly column ranges of one buffer; their rows of no sequence are not
+    written (those of tensors that the call allocates are zero).  The same inputs
+    give the same bits.  With status=True the device status comes fourth."""
+    if grads is None and workspace is None and stream is None and not status:
+        return _done(_native().attn_grad(dout, q, k, v, out, lse, heads, heads if kv_heads is None else kv_heads, scale,
+                                         bool(causal), window or 0, seqs, kv_seqs), "iso_attn_grad")
     if stream is not None:
         with torch.cuda.stream(stream):
             return attn_grad(dout, q, k, v, out, lse, heads, kv_heads, scale, causal, window, seqs, kv_seqs, grads,
                              workspace, status)
     mq, mk, mv, mo, md = _mat(q, "q"), _mat(k, "k"), _mat(v, "v"), _mat(out, "out"), _mat(dout, "dout")
-    cfg = _attn_cfg(mq, heads, kv_heads, scale, causal, window, seqs, kv_seqs)
+    cfg = _attn_cfg(mq, heads, kv_heads, scale, causal, window, seqs, kv_seqs, grads is None)
     lptr = _vector(lse, "lse", torch.float32, (cfg.heads, mq.rows))
     s = _here(q, k, v, out, dout, lse, seqs, kv_seqs)
     if grads is None:
-        made = [_rows_new(m, seqs is not None, t.dtype, t.device) for m, t in ((mq, q), (mk, k), (mv, v))]
+        made = [_new(m.rows, m.cols, t.dtype, t.device) for m, t in ((mq, q), (mk, k), (mv, v))]
     else:
         if len(grads) != 3:
             raise ValueError("grads needs dq, dk and dv")
@@ -291,6 +295,8 @@ def distill(logits: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, temp
     ``dloss`` (float32 per row) also the gradient of the logits, third, read in
     the same pass; into ``out``, which may be the logits.  With status=True the
     device status comes last."""
+    if out is None and stream is None and not status:
+        return _done(_native().distill(logits, ids, teacher, _tau(temperature), dloss), "iso_distill")
     if stream is not None:
         with torch.cuda.stream(stream):
             return distill(logits, ids, teacher, temperature, dloss, out, status)
@@ -317,6 +323,8 @@ def distill_grad(dloss: torch.Tensor, logits: torch.Tensor, ids: torch.Tensor, t
                  lse: torch.Tensor, temperature=1.0, out: Optional[torch.Tensor] = None, status=False, stream=None):
     """The gradient of distill's logits from that of its loss and its lse
     (iso_distill_grad); ``out`` may be the logits."""
+    if out is None and stream is None and not status:
+        return _done(_native().distill_grad(dloss, logits, ids, teacher, lse, _tau(temperature)), "iso_distill_grad")
     if stream is not None:
         with torch.cuda.stream(stream):
             return distill_grad(dloss, logits, ids, teacher, lse, temperature, out, status)

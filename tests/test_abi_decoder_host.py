@@ -90,8 +90,8 @@ def test_rope_plans():
 # ---------------------------------------------------------------------------
 # attention
 # ---------------------------------------------------------------------------
-def cfg(heads=4, kv=2, dim=64, causal=1, window=0, scale=0.125, n=0, q_ends=None, k_ends=None):
-    return IsoAttnCfg(heads, kv, dim, causal, window, scale, n, q_ends, k_ends)
+def cfg(heads=4, kv=2, dim=64, causal=1, window=0, scale=0.125, n=0, q_ends=None, k_ends=None, rest=0, reserved=0):
+    return IsoAttnCfg(heads, kv, dim, causal, window, scale, n, q_ends, k_ends, rest, reserved)
 
 
 def attn(q=None, k=None, v=None, out=None, c=None, lse=5 * A, ws=WS, n=BIG, status=None):
@@ -102,7 +102,7 @@ def attn(q=None, k=None, v=None, out=None, c=None, lse=5 * A, ws=WS, n=BIG, stat
 def test_attention_refusals():
     for bad in (cfg(heads=0), cfg(kv=0), cfg(kv=3), cfg(dim=0), cfg(causal=2), cfg(window=-1), cfg(window=4, causal=0),
                 cfg(scale=0.0), cfg(scale=-1.0), cfg(scale=math.nan), cfg(scale=math.inf), cfg(n=-1), cfg(n=2),
-                cfg(q_ends=6 * A), cfg(k_ends=6 * A)):
+                cfg(q_ends=6 * A), cfg(k_ends=6 * A), cfg(rest=2), cfg(reserved=1)):
         assert attn(c=bad) == ARG
     assert attn(c=cfg(n=1, q_ends=6 * A + 2)) == ALIGN
     assert attn(c=cfg(dim=129)) == UNSUPPORTED
