@@ -64,6 +64,31 @@ __device__ __forceinline__ void key_tiles(const FwdArgs& a, const AttnTile& t, i
     end = t0 + (int)((long long)n * (part + 1) / a.parts);
 }
 
+// A CTA's rows done over in binary32 (iso_attn_simt.cuh), by 256 of its threads.
+// Not inlined: nothing of it is held in registers before.
+template <int DP>
+__device__ __noinline__ void again_rows(const FwdArgs& a, float* smem) {
+    const AttnArgs& g = a.g;
+    const int part = blockIdx.x % a.parts, h = blockIdx.x / a.parts % g.heads;
+    AttnTile t;
+    if (!attn_find_tile(g, blockIdx.x / a.parts / g.heads, FW_ROWS, false, t)) return;
+    const long long width = (long long)g.heads * g.head_dim;
+    const int rows = min(FW_ROWS, t.nq - t.first), last = t.first + rows;
+    for (int x = 0; x < 2; ++x) {
+        int begin, end;
+        key_tiles(a, t, t.first, min(ROWS, last - t.first), part, begin, end);
+        for (const int stop = min(last, t.first + ROWS); t.first < stop; t.first += SA_B) {
+            if (a.parts > 1)
+                simt_attn<__nv_bfloat16, DP, float>(g, t, h, begin * ROWS, end * ROWS, a.part + (long long)part * g.q_rows * width, width,
+                                                    a.part + (long long)a.parts * g.q_rows * width + (long long)part * g.heads * g.q_rows, smem);
+            else
+                simt_attn<__nv_bfloat16, DP, __nv_bfloat16>(g, t, h, begin * ROWS, end * ROWS, static_cast<__nv_bfloat16*>(const_cast<void*>(g.out)),
+                                                            g.ldo, g.lse, smem);
+            sa_sync();
+        }
+    }
+}
+
 template <int DP>
 __global__ void __launch_bounds__(FW_THREADS, 1)
 k_tc_attn(const __grid_constant__ FwdMaps maps, const __grid_constant__ FwdArgs a) {
@@ -162,7 +187,7 @@ k_tc_attn(const __grid_constant__ FwdMaps maps, const __grid_constant__ FwdArgs 
             if (!wait.warp(p_ready(x), (uint32_t)j & 1u)) return false;
             after_sync();
             if (lane == 0) {
-                product_rows<DP>(O(x), S(x), S(x) + 32, smem_u32(sv) + (uint32_t)(i % FW_V_STAGES) * TILE, j > 0);
+                product_rows<DP, 128>(O(x), S(x), smem_u32(sv) + (uint32_t)(i % FW_V_STAGES) * TILE, j > 0);
                 commit(o_done(x));
             }
             __syncwarp();
@@ -296,23 +321,7 @@ k_tc_attn(const __grid_constant__ FwdMaps maps, const __grid_constant__ FwdArgs 
         after_sync();
         free_all(tmem);
     }
-    if (*again && !*gave_up && warp < FW_COMPUTE) {
-        const int all = t.first + rows, base = t.first;
-        for (; t.first < all; t.first += SA_B) {
-            const int x = (t.first - base) / ROWS;
-            float* const f = reinterpret_cast<float*>(smem);
-            const int k_begin = begin[x] * ROWS, k_end = has[x] ? end[x] * ROWS : 0;
-            if (a.parts > 1) {
-                const long long width = (long long)g.heads * g.head_dim;
-                simt_attn<__nv_bfloat16, DP, float>(g, t, h, k_begin, k_end, a.part + (long long)part * g.q_rows * width, width,
-                                                    a.part + (long long)a.parts * g.q_rows * width + (long long)part * g.heads * g.q_rows, f);
-            } else {
-                simt_attn<__nv_bfloat16, DP, __nv_bfloat16>(g, t, h, k_begin, k_end, static_cast<__nv_bfloat16*>(const_cast<void*>(g.out)),
-                                                            g.ldo, g.lse, f);
-            }
-            sa_sync();
-        }
-    }
+    if (*again && !*gave_up && warp < SA_TPB / 32) again_rows<DP>(a, reinterpret_cast<float*>(smem));
 }
 
 // The parts of a row of one head put together: lse = log sum e^lse_p, out = sum

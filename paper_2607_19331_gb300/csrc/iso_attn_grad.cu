@@ -20,9 +20,9 @@
 //                    S = Q K^T, dP = dO V^T, dS = P (dP - delta), dQ += dS K
 //                  with two buffers of scores; dS lies over its scores.
 // Tensor memory is full in both (4 x 128 columns).
-// Eight warps compute, four on each half of a tile's columns; one warp copies,
-// one issues products; in k_tc_grad_kv one more brings lse and delta, which are
-// per column there.
+// GR_COMPUTE warps compute, four on each GR_COLS of a tile's columns; one warp
+// copies, one issues products; in k_tc_grad_kv one more brings lse and delta, which
+// are per column there.
 #include "iso_attn.cuh"
 #include "iso_attn_simt.cuh"
 #include "iso_attn_tc.cuh"
@@ -36,7 +36,8 @@ namespace {
 
 using namespace tc;
 
-constexpr int GR_COMPUTE = 8;
+constexpr int GR_COMPUTE = 8;            // warps that compute, four on each GR_COLS columns of a tile
+constexpr int GR_COLS = 128 * 4 / GR_COMPUTE;
 constexpr int GR_THREADS = (GR_COMPUTE + 3) * 32;
 constexpr int KV_Q_STAGES = 3, KV_DO_STAGES = 2, Q_K_STAGES = 3, Q_V_STAGES = 2;
 
@@ -54,12 +55,47 @@ struct GradTile {
                   sa_smem<DP>(4, 1) <= (2 + Q_K_STAGES + Q_V_STAGES) * TILE, "the rows done over fit where the tiles were");
 };
 
-// The 64 weights of this thread's row and half: p = exp2(c s - lse2), 0 outside
-// [from, to) where the tile is masked
-template <bool MASKED>
-__device__ __forceinline__ float weight(float s, float c, float lse2, int at, int from, int to) {
-    const float p = ex2(fmaf(s, c, -lse2));
-    return !MASKED || (at >= from && at < to) ? p : 0.0f;
+// The weights of COLS columns of this thread's row, p = exp2(c s - lse2), with the
+// columns outside [from, to) 0 in a masked tile; neg_lse2(j): -lse2 of columns 2 j, 2 j + 1
+template <bool MASKED, int COLS, typename L>
+__device__ __forceinline__ void weights(const float (&s)[COLS], uint64_t (&p)[COLS / 2], uint64_t c, int from, int to, L neg_lse2) {
+#pragma unroll
+    for (int j = 0; j < COLS / 2; ++j) {
+        float x, y;
+        parts_of(fma2(pair_of(s[2 * j], s[2 * j + 1]), c, neg_lse2(j)), x, y);
+        x = ex2(x);
+        y = ex2(y);
+        if (MASKED && !(2 * j >= from && 2 * j < to)) x = 0.0f;
+        if (MASKED && !(2 * j + 1 >= from && 2 * j + 1 < to)) y = 0.0f;
+        p[j] = pair_of(x, y);
+    }
+}
+// dS = P (dP - delta) as bf16; what is not seen is 0 whatever dP is there
+template <bool MASKED, int COLS, typename L>
+__device__ __forceinline__ void score_grads(const float (&d)[COLS], const uint64_t (&p)[COLS / 2], uint32_t (&w)[COLS / 2], int from, int to,
+                                            L neg_delta) {
+#pragma unroll
+    for (int j = 0; j < COLS / 2; ++j) {
+        float x, y;
+        parts_of(mul2(add2(pair_of(d[2 * j], d[2 * j + 1]), neg_delta(j)), p[j]), x, y);
+        if (MASKED && !(2 * j >= from && 2 * j < to)) x = 0.0f;
+        if (MASKED && !(2 * j + 1 >= from && 2 * j + 1 < to)) y = 0.0f;
+        w[j] = f32_to_bf16x2(x, y);
+    }
+}
+// COLS columns of this thread's row
+template <int COLS>
+__device__ __forceinline__ void load_cols(uint32_t at, float (&v)[COLS]) {
+#pragma unroll
+    for (int c = 0; c < COLS / 32; ++c) load32(at + 32 * c, reinterpret_cast<float (&)[32]>(v[32 * c]));
+#pragma unroll
+    for (int c = 0; c < COLS / 32; ++c) loaded(reinterpret_cast<float (&)[32]>(v[32 * c]));
+}
+template <int COLS>
+__device__ __forceinline__ void store_cols(uint32_t at, const uint32_t (&w)[COLS / 2]) {
+#pragma unroll
+    for (int c = 0; c < COLS / 32; ++c) store16(at + 16 * c, w + 16 * c);
+    stored();
 }
 
 struct GradArgs {
@@ -70,6 +106,36 @@ struct GradArgs {
     int32_t parts;               // (keys) parts of a key head's query heads, each with its own sums
     float* part;                 // (keys) parts > 1: [part][dk, dv][k_rows][kv_heads dim]
 };
+
+// A CTA's rows done over in binary32 (iso_attn_simt.cuh), by 256 of its threads.
+// Not inlined: nothing of it is held in registers before.
+template <int DP>
+__device__ __noinline__ void again_kv(const GradArgs& a, float* smem) {
+    const AttnArgs& g = a.g;
+    const int kv_heads = g.heads / g.group, part = blockIdx.x % a.parts, kh = blockIdx.x / a.parts % kv_heads;
+    const int h0 = kh * g.group + g.group * part / a.parts, h1 = kh * g.group + g.group * (part + 1) / a.parts;
+    AttnTile t;
+    if (!attn_find_tile(g, blockIdx.x / a.parts / kv_heads, ROWS, true, t)) return;
+    const long long width = (long long)kv_heads * g.head_dim;
+    float* const o = a.part + (long long)(part * 2) * g.k_rows * width;
+    for (const int last = t.first + min(ROWS, t.nk - t.first); t.first < last; t.first += SA_B) {
+        if (a.parts > 1)
+            simt_grad_kv<__nv_bfloat16, DP, float>(g, t, kh, h0, h1, o, width, o + g.k_rows * width, width, smem);
+        else
+            simt_grad_kv<__nv_bfloat16, DP, __nv_bfloat16>(g, t, kh, h0, h1, static_cast<__nv_bfloat16*>(g.dk), g.lddk,
+                                                           static_cast<__nv_bfloat16*>(g.dv), g.lddv, smem);
+        sa_sync();
+    }
+}
+template <int DP>
+__device__ __noinline__ void again_q(const GradArgs& a, float* smem) {
+    AttnTile t;
+    if (!attn_find_tile(a.g, blockIdx.x / a.g.heads, ROWS, false, t)) return;
+    for (const int last = t.first + min(ROWS, t.nq - t.first); t.first < last; t.first += SA_B) {
+        simt_grad_q<__nv_bfloat16, DP>(a.g, t, blockIdx.x % a.g.heads, smem);
+        sa_sync();
+    }
+}
 
 template <int DP>
 __global__ void __launch_bounds__(GR_THREADS, 1)
@@ -179,7 +245,7 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
             if (!(ok = wait.warp(p_ready, (uint32_t)i & 1u))) break;
             after_sync();
             if (lane == 0) {
-                product_rows<DP>(dV, S, S + 64, do_at(i), i > 0);
+                product_rows<DP, GR_COLS>(dV, S, do_at(i), i > 0);
                 commit(do_empty(i % KV_DO_STAGES));
             }
             __syncwarp();
@@ -187,7 +253,7 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
             if (!(ok = wait.warp(ds_ready, (uint32_t)i & 1u))) break;
             after_sync();
             if (lane == 0) {
-                product_rows<DP>(dK, dP, dP + 64, q_at(i), i > 0);
+                product_rows<DP, GR_COLS>(dK, dP, q_at(i), i > 0);
                 commit(q_empty(i % KV_Q_STAGES));
             }
             __syncwarp();
@@ -199,7 +265,7 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
             wait.drain(done, 0);
         }
     } else if (warp == GR_COMPUTE + 2) {
-        // lse and delta of a step's queries: four a lane.  A query behind the
+        // -lse log2 e and -delta of a step's queries: four a lane.  A query behind the
         // sequence's end has an infinite lse, so that its weights are 0.
         int i = 0;
         bool ok = true;
@@ -211,8 +277,8 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const bool in = first + 32 * j < t.nq;
-                    l[j] = in ? g.lse[at + 32 * j] * LOG2E : INFINITY;
-                    d[j] = in ? g.delta[at + 32 * j] : 0.0f;
+                    l[j] = in ? -g.lse[at + 32 * j] * LOG2E : -INFINITY;
+                    d[j] = in ? -g.delta[at + 32 * j] : 0.0f;
                 }
                 if (!(ok = wait.warp(lse_empty, (uint32_t)(i + 1) & 1u))) break;
 #pragma unroll
@@ -224,98 +290,61 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
                 arrive_warp(delta_full);
             }
     } else {
-        const int half = warp >> 2, r = (warp & 3) * 32 + lane;
-        const uint32_t at = ((uint32_t)(warp & 3) * 32) << 16, s_at = S + at + half * 64, d_at = dP + at + half * 64;
+        const int group = warp >> 2, r = (warp & 3) * 32 + lane;
+        const uint32_t at = ((uint32_t)(warp & 3) * 32) << 16, s_at = S + at + group * GR_COLS, d_at = dP + at + group * GR_COLS;
         int from, to;
         attn_queries_of(g, t, t.first + min(r, keys - 1), from, to);
+        const uint64_t c = pair_of(a.scale2, a.scale2);
+        const ulonglong2* const neg_lse = reinterpret_cast<const ulonglong2*>(lse_s + group * GR_COLS);
+        const ulonglong2* const neg_delta = reinterpret_cast<const ulonglong2*>(delta_s + group * GR_COLS);
         bool ok = true;
         for (int i = 0; i < steps; ++i) {
             const uint32_t ph = (uint32_t)i & 1u;
-            const int q0 = (tile0 + i % tiles) * ROWS + half * 64;
+            const int q0 = (tile0 + i % tiles) * ROWS + group * GR_COLS;
             const int f = from - q0, e = to - q0;                 // this thread's columns that are seen
-            const bool masked = !__all_sync(0xFFFFFFFFu, f <= 0 && e >= 64);
-            float p[64];
+            const bool masked = !__all_sync(0xFFFFFFFFu, f <= 0 && e >= GR_COLS);
+            uint64_t p[GR_COLS / 2];
+            float v[GR_COLS];
+            uint32_t w[GR_COLS / 2];
             if (!(ok = wait.warp(lse_full, ph) && wait.warp(s_full, ph))) break;
             after_sync();
-            {
-                float v[2][32];
-                load32(s_at, v[0]);
-                loaded(v[0]);
-                load32(s_at + 32, v[1]);
-                auto form = [&](auto m, int c) {
+            load_cols<GR_COLS>(s_at, v);
+            auto l = [&](int j) { return j & 1 ? neg_lse[j / 2].y : neg_lse[j / 2].x; };
+            if (masked) weights<true, GR_COLS>(v, p, c, f, e, l);
+            else weights<false, GR_COLS>(v, p, c, f, e, l);
 #pragma unroll
-                    for (int j = 0; j < 32; j += 4) {
-                        const float4 l = *reinterpret_cast<const float4*>(lse_s + half * 64 + c * 32 + j);
-                        p[c * 32 + j] = weight<decltype(m)::value>(v[c][j], a.scale2, l.x, c * 32 + j, f, e);
-                        p[c * 32 + j + 1] = weight<decltype(m)::value>(v[c][j + 1], a.scale2, l.y, c * 32 + j + 1, f, e);
-                        p[c * 32 + j + 2] = weight<decltype(m)::value>(v[c][j + 2], a.scale2, l.z, c * 32 + j + 2, f, e);
-                        p[c * 32 + j + 3] = weight<decltype(m)::value>(v[c][j + 3], a.scale2, l.w, c * 32 + j + 3, f, e);
-                    }
-                };
-                uint32_t w[32];
-                if (masked) form(std::true_type{}, 0);
-                else form(std::false_type{}, 0);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) w[j] = f32_to_bf16x2(p[2 * j], p[2 * j + 1]);
-                loaded(v[1]);
-                store16(s_at, w);
-                if (masked) form(std::true_type{}, 1);
-                else form(std::false_type{}, 1);
-#pragma unroll
-                for (int j = 16; j < 32; ++j) w[j] = f32_to_bf16x2(p[2 * j], p[2 * j + 1]);
-                store16(s_at + 16, w + 16);
-                stored();
-            }
+            for (int j = 0; j < GR_COLS / 2; ++j) w[j] = bf16_of(p[j]);
+            store_cols<GR_COLS>(s_at, w);
             before_sync();
             arrive_warp(p_ready);
-            arrive_warp(lse_empty);
+            if (lane == 0) mbar_arrive(lse_empty);
             if (!(ok = wait.warp(delta_full, ph) && wait.warp(dp_full, ph))) break;
             after_sync();
-            {
-                float v[2][32];
-                load32(d_at, v[0]);
-                loaded(v[0]);
-                load32(d_at + 32, v[1]);
-                auto form = [&](int c, uint32_t* w) {
-#pragma unroll
-                    for (int j = 0; j < 32; j += 4) {
-                        const float4 d = *reinterpret_cast<const float4*>(delta_s + half * 64 + c * 32 + j);
-                        float x[4] = {v[c][j] - d.x, v[c][j + 1] - d.y, v[c][j + 2] - d.z, v[c][j + 3] - d.w};
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            x[k] *= p[c * 32 + j + k];
-                            if (masked && !(c * 32 + j + k >= f && c * 32 + j + k < e)) x[k] = 0.0f;   // (0 times what is not seen)
-                        }
-                        w[j / 2] = f32_to_bf16x2(x[0], x[1]);
-                        w[j / 2 + 1] = f32_to_bf16x2(x[2], x[3]);
-                    }
-                };
-                uint32_t w[16];
-                form(0, w);
-                loaded(v[1]);
-                store16(d_at, w);
-                form(1, w);
-                store16(d_at + 16, w);
-                stored();
-            }
+            load_cols<GR_COLS>(d_at, v);
+            auto d = [&](int j) { return j & 1 ? neg_delta[j / 2].y : neg_delta[j / 2].x; };
+            if (masked) score_grads<true, GR_COLS>(v, p, w, f, e, d);
+            else score_grads<false, GR_COLS>(v, p, w, f, e, d);
+            store_cols<GR_COLS>(d_at, w);
             before_sync();
             arrive_warp(ds_ready);
-            arrive_warp(delta_empty);
+            if (lane == 0) mbar_arrive(delta_empty);
         }
-        // dV by the first half's warps, dK by the second's: a row a thread
+        // dV by the first half of the warps, dK by the second: a row a thread, DP / PER columns
+        constexpr int PER = GR_COMPUTE / 8, WIDE = DP / PER;
+        const int half = group / PER, from_col = group % PER * WIDE;
         if (steps > 0) ok = ok && wait.warp(done, 0);
         after_sync();
         const bool nan = !ok || (steps > 0 && *gave_up), none = steps == 0;
-        const uint32_t acc = (half ? dK : dV) + at;
+        const uint32_t acc = (half ? dK : dV) + at + from_col;
         const float by = half ? g.scale : 1.0f;
         const long long row = (long long)t.k0 + t.first + r;
         if (a.parts > 1) {
             const long long width = (long long)kv_heads * g.head_dim;
-            float* o = a.part + ((long long)(part * 2 + (half ? 0 : 1)) * g.k_rows + row) * width + (long long)kh * g.head_dim;
-            if (!write_row<float, DP>(acc, o, r < keys, g.head_dim, g.head_dim % 4 == 0, by, nan, none)) *again = 1;
+            float* o = a.part + ((long long)(part * 2 + (half ? 0 : 1)) * g.k_rows + row) * width + (long long)kh * g.head_dim + from_col;
+            if (!write_row<float, WIDE>(acc, o, r < keys, g.head_dim - from_col, true, by, nan, none)) *again = 1;
         } else {
-            __nv_bfloat16* o = static_cast<__nv_bfloat16*>(half ? g.dk : g.dv) + row * (half ? g.lddk : g.lddv) + (long long)kh * g.head_dim;
-            if (!write_row<__nv_bfloat16, DP>(acc, o, r < keys, g.head_dim, a.vec, by, nan, none)) *again = 1;
+            __nv_bfloat16* o = static_cast<__nv_bfloat16*>(half ? g.dk : g.dv) + row * (half ? g.lddk : g.lddv) + (long long)kh * g.head_dim + from_col;
+            if (!write_row<__nv_bfloat16, WIDE>(acc, o, r < keys, g.head_dim - from_col, a.vec, by, nan, none)) *again = 1;
         }
         before_sync();
     }
@@ -325,21 +354,7 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
         after_sync();
         free_all(tmem);
     }
-    if (*again && !*gave_up && warp < GR_COMPUTE) {
-        float* const f = reinterpret_cast<float*>(smem);
-        const int last = t.first + keys;
-        for (; t.first < last; t.first += SA_B) {
-            if (a.parts > 1) {
-                const long long width = (long long)kv_heads * g.head_dim;
-                float* const o = a.part + (long long)(part * 2) * g.k_rows * width;
-                simt_grad_kv<__nv_bfloat16, DP, float>(g, t, kh, h0, h1, o, width, o + g.k_rows * width, width, f);
-            } else {
-                simt_grad_kv<__nv_bfloat16, DP, __nv_bfloat16>(g, t, kh, h0, h1, static_cast<__nv_bfloat16*>(g.dk), g.lddk,
-                                                               static_cast<__nv_bfloat16*>(g.dv), g.lddv, f);
-            }
-            sa_sync();
-        }
-    }
+    if (*again && !*gave_up && warp < SA_TPB / 32) again_kv<DP>(a, reinterpret_cast<float*>(smem));
 }
 
 template <int DP>
@@ -438,8 +453,7 @@ k_tc_grad_q(const __grid_constant__ GradMaps maps, const __grid_constant__ GradA
             if (i + 1 < steps && !(ok = values(i + 1))) break;                     // dP(i) has been read
             after_sync();
             if (lane == 0) {
-                const uint32_t x = S + (i & 1) * 128;
-                product_rows<DP>(dQ, x, x + 64, k_at(i), i > 0);
+                product_rows<DP, GR_COLS>(dQ, S + (i & 1) * 128, k_at(i), i > 0);
                 commit(k_empty(i % Q_K_STAGES));
             }
             __syncwarp();
@@ -450,73 +464,44 @@ k_tc_grad_q(const __grid_constant__ GradMaps maps, const __grid_constant__ GradA
             wait.drain(done, 0);
         }
     } else if (warp < GR_COMPUTE) {
-        const int half = warp >> 2, r = (warp & 3) * 32 + lane;
-        const uint32_t at = ((uint32_t)(warp & 3) * 32) << 16, d_at = dP + at + half * 64;
+        const int group = warp >> 2, r = (warp & 3) * 32 + lane;
+        const uint32_t at = ((uint32_t)(warp & 3) * 32) << 16, d_at = dP + at + group * GR_COLS;
         int from, to;
         attn_keys_of(g, t, t.first + min(r, rows - 1), from, to);
         const long long stat = (long long)h * g.q_rows + t.q0 + t.first + min(r, rows - 1);
-        const float lse2 = g.lse[stat] * LOG2E, delta = g.delta[stat];
+        const float neg_lse = -g.lse[stat] * LOG2E, neg_delta = -g.delta[stat];
+        const uint64_t c = pair_of(a.scale2, a.scale2), ll = pair_of(neg_lse, neg_lse), dd = pair_of(neg_delta, neg_delta);
         bool ok = true;
         for (int i = 0; i < steps; ++i) {
-            const uint32_t s_at = S + (i & 1) * 128 + at + half * 64;
-            const int k0 = (tile0 + i) * ROWS + half * 64;
+            const uint32_t s_at = S + (i & 1) * 128 + at + group * GR_COLS;
+            const int k0 = (tile0 + i) * ROWS + group * GR_COLS;
             const int f = from - k0, e = to - k0;
-            const bool masked = !__all_sync(0xFFFFFFFFu, f <= 0 && e >= 64);
-            float p[64];
+            const bool masked = !__all_sync(0xFFFFFFFFu, f <= 0 && e >= GR_COLS);
+            uint64_t p[GR_COLS / 2];
+            float v[GR_COLS];
+            uint32_t w[GR_COLS / 2];
             if (!(ok = wait.warp(s_full + 8u * (i & 1), (uint32_t)(i >> 1) & 1u))) break;
             after_sync();
-            {
-                float v[2][32];
-                load32(s_at, v[0]);
-                loaded(v[0]);
-                load32(s_at + 32, v[1]);
-                auto form = [&](auto m, int c) {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        p[c * 32 + j] = weight<decltype(m)::value>(v[c][j], a.scale2, lse2, c * 32 + j, f, e);
-                };
-                if (masked) form(std::true_type{}, 0);
-                else form(std::false_type{}, 0);
-                loaded(v[1]);
-                if (masked) form(std::true_type{}, 1);
-                else form(std::false_type{}, 1);
-            }
+            load_cols<GR_COLS>(s_at, v);
+            if (masked) weights<true, GR_COLS>(v, p, c, f, e, [&](int) { return ll; });
+            else weights<false, GR_COLS>(v, p, c, f, e, [&](int) { return ll; });
             if (!(ok = wait.warp(dp_full, (uint32_t)i & 1u))) break;
             after_sync();
-            {
-                float v[2][32];
-                load32(d_at, v[0]);
-                loaded(v[0]);
-                load32(d_at + 32, v[1]);
-                auto form = [&](int c, uint32_t* w) {
-#pragma unroll
-                    for (int j = 0; j < 32; j += 2) {
-                        float x = (v[c][j] - delta) * p[c * 32 + j], y = (v[c][j + 1] - delta) * p[c * 32 + j + 1];
-                        if (masked) {                              // (0 times what is not seen)
-                            if (!(c * 32 + j >= f && c * 32 + j < e)) x = 0.0f;
-                            if (!(c * 32 + j + 1 >= f && c * 32 + j + 1 < e)) y = 0.0f;
-                        }
-                        w[j / 2] = f32_to_bf16x2(x, y);
-                    }
-                };
-                uint32_t w[16];
-                form(0, w);
-                loaded(v[1]);
-                store16(s_at, w);
-                form(1, w);
-                store16(s_at + 16, w);
-                stored();
-            }
+            load_cols<GR_COLS>(d_at, v);
+            if (masked) score_grads<true, GR_COLS>(v, p, w, f, e, [&](int) { return dd; });
+            else score_grads<false, GR_COLS>(v, p, w, f, e, [&](int) { return dd; });
+            store_cols<GR_COLS>(s_at, w);
             before_sync();
             arrive_warp(ds_ready);
         }
         if (steps > 0) ok = ok && wait.warp(done, 0);
         after_sync();
-        // dQ: half of the columns by each half's warps
+        // dQ: a row a thread, some columns of it each group
+        constexpr int WIDE = DP * 4 / GR_COMPUTE;
         const bool nan = !ok || (steps > 0 && *gave_up), none = steps == 0;
-        __nv_bfloat16* o = static_cast<__nv_bfloat16*>(g.dq) + ((long long)t.q0 + t.first + r) * g.lddq + (long long)h * g.head_dim;
-        if (!write_row<__nv_bfloat16, DP / 2>(dQ + at + half * (DP / 2), o + half * (DP / 2), r < rows,
-                                              g.head_dim - half * (DP / 2), a.vec, g.scale, nan, none))
+        const int from_col = group * WIDE;
+        __nv_bfloat16* o = static_cast<__nv_bfloat16*>(g.dq) + ((long long)t.q0 + t.first + r) * g.lddq + (long long)h * g.head_dim + from_col;
+        if (!write_row<__nv_bfloat16, WIDE>(dQ + at + from_col, o, r < rows, g.head_dim - from_col, a.vec, g.scale, nan, none))
             *again = 1;
         before_sync();
     }
@@ -526,13 +511,7 @@ k_tc_grad_q(const __grid_constant__ GradMaps maps, const __grid_constant__ GradA
         after_sync();
         free_all(tmem);
     }
-    if (*again && !*gave_up && warp < GR_COMPUTE) {
-        const int last = t.first + rows;
-        for (; t.first < last; t.first += SA_B) {
-            simt_grad_q<__nv_bfloat16, DP>(g, t, h, reinterpret_cast<float*>(smem));
-            sa_sync();
-        }
-    }
+    if (*again && !*gave_up && warp < SA_TPB / 32) again_q<DP>(a, reinterpret_cast<float*>(smem));
 }
 
 // dk and dv: the parts' sums in order.  Eight columns a thread.

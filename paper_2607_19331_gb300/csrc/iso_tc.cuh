@@ -53,14 +53,14 @@ __device__ __forceinline__ void product_along(uint32_t d, uint32_t a, uint32_t b
         mma_ss(d, al + at, bl + at, idesc(ROWS, false), k > 0);
     }
 }
-// D (+)= A B: A [128 x 128] bf16 in tensor memory, its columns 0 .. 63 from `a`
-// on (32 words), 64 .. 127 from `a_half` on; B the tile's 128 rows of DP channels
-template <int DP>
-__device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t a_half, uint32_t b, uint32_t accumulate) {
+// D (+)= A B: A [128 x 128] bf16 in tensor memory, each COLS columns of it (COLS / 2
+// words) at the place of as many binary32 ones; B the tile's 128 rows of DP channels
+template <int DP, int COLS>
+__device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b, uint32_t accumulate) {
     const uint32_t bl = DESC_LO_ROWS + (b >> 4);
 #pragma unroll
     for (uint32_t k = 0; k < 8; ++k)
-        mma_ts(d, (k < 4 ? a : a_half) + (k % 4) * 8, bl + k * (2048u >> 4), idesc(DP, true), k > 0 ? 1u : accumulate);
+        mma_ts(d, a + k * 16 / COLS * COLS + k * 16 % COLS / 2, bl + k * (2048u >> 4), idesc(DP, true), k > 0 ? 1u : accumulate);
 }
 
 // arrive on `bar` once the products issued so far are done
@@ -181,6 +181,33 @@ struct Waits {
     __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) const { one(bar, parity, 2000000000u, false); }
 };
 
+// two binary32 numbers at a time
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void parts_of(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t bf16_of(uint64_t v) {
+    float a, b;
+    parts_of(v, a, b);
+    return f32_to_bf16x2(a, b);
+}
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
