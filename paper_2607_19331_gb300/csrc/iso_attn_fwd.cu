@@ -172,11 +172,14 @@ k_tc_attn(const __grid_constant__ FwdMaps maps, const __grid_constant__ FwdArgs 
         }
     } else if (warp == FW_COMPUTE + 1) {
         // products (the whole warp waits and clears, one lane issues)
+        Slot<FW_K_STAGES> ks;                        // K of the next scores
+        Slot<FW_V_STAGES> vs;
+        const uint32_t q_s = smem_u32(sq), k_s = smem_u32(sk), v_s = smem_u32(sv);
         auto in = [&](int x, int i) { return u0 + i >= begin[x] && u0 + i < end[x]; };
         auto scores = [&](int x, int i) {                                          // S = Q K^T
             if (!in(x, i)) return;
-            if (lane == 0) {
-                product_along<DP>(S(x), smem_u32(sq) + x * TILE, smem_u32(sk) + (uint32_t)(i % FW_K_STAGES) * TILE);
+            if (elected()) {
+                product_along<DP>(S(x), q_s + (uint32_t)x * TILE, k_s + (uint32_t)ks.at * TILE);
                 commit(s_full(x));
             }
             __syncwarp();
@@ -186,43 +189,45 @@ k_tc_attn(const __grid_constant__ FwdMaps maps, const __grid_constant__ FwdArgs 
             const int j = u0 + i - begin[x];
             if (!wait.warp(p_ready(x), (uint32_t)j & 1u)) return false;
             after_sync();
-            if (lane == 0) {
-                product_rows<DP, 128>(O(x), S(x), smem_u32(sv) + (uint32_t)(i % FW_V_STAGES) * TILE, j > 0);
+            if (elected()) {
+                product_rows<DP, 128>(O(x), S(x), v_s + (uint32_t)vs.at * TILE, j > 0);
                 commit(o_done(x));
             }
             __syncwarp();
             return true;
         };
-        auto keys = [&](int i) { return wait.warp(k_full(i % FW_K_STAGES), (uint32_t)(i / FW_K_STAGES) & 1u); };
-        bool ok = steps > 0 && (!has[0] || wait.warp(q_full(0), 0)) && (!has[1] || wait.warp(q_full(1), 0)) && keys(0);
+        bool ok = steps > 0 && (!has[0] || wait.warp(q_full(0), 0)) && (!has[1] || wait.warp(q_full(1), 0)) &&
+                  wait.warp(k_full(0), 0);
         if (ok) {
             after_sync();
             scores(0, 0);
             scores(1, 0);
-            if (lane == 0) commit(k_empty(0));
+            if (elected()) commit(k_empty(0));
             __syncwarp();
+            ks.next();
         }
         for (int i = 0; ok && i < steps; ++i) {
-            const int vs = i % FW_V_STAGES;
-            if (!(ok = wait.warp(v_full(vs), (uint32_t)(i / FW_V_STAGES) & 1u))) break;
-            clear_rows<DP>(sv + vs * TILE, t.nk - (u0 + i) * ROWS);
+            if (!(ok = wait.warp(v_full(vs.at), vs.parity))) break;
+            if (i == steps - 1) clear_rows<DP>(sv + vs.at * TILE, t.nk - (u0 + i) * ROWS);
             if (!(ok = sums(0, i))) break;
             if (i + 1 < steps) {
-                if (!(ok = keys(i + 1))) break;
+                if (!(ok = wait.warp(k_full(ks.at), ks.parity))) break;
                 after_sync();
                 scores(0, i + 1);
             }
             if (!(ok = sums(1, i))) break;
-            if (lane == 0) commit(v_empty(vs));
+            if (elected()) commit(v_empty(vs.at));
             __syncwarp();
+            vs.next();
             if (i + 1 < steps) {
                 scores(1, i + 1);
-                if (lane == 0) commit(k_empty((i + 1) % FW_K_STAGES));
+                if (elected()) commit(k_empty(ks.at));
                 __syncwarp();
+                ks.next();
             }
         }
         // no product runs on when the tensor memory is freed, after a give-up either
-        if (lane == 0 && steps > 0) {
+        if (steps > 0 && elected()) {
             commit(done);
             wait.drain(done, 0);
         }

@@ -212,55 +212,61 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
             for (int i = max(0, nd - KV_DO_STAGES); i < nd; ++i) wait.drain(do_full(i % KV_DO_STAGES), (uint32_t)(i / KV_DO_STAGES) & 1u);
         }
     } else if (warp == GR_COMPUTE + 1) {
-        // products (the whole warp waits and clears, one lane issues)
-        auto q_at = [&](int i) { return smem_u32(sq) + (uint32_t)(i % KV_Q_STAGES) * TILE; };
-        auto do_at = [&](int i) { return smem_u32(sd) + (uint32_t)(i % KV_DO_STAGES) * TILE; };
-        auto valid = [&](int i) { return t.nq - (tile0 + i % tiles) * ROWS; };     // rows of step i's query tile
-        auto scores = [&](int i) {                                                 // S^T = K Q^T
-            const int s = i % KV_Q_STAGES;
-            if (!wait.warp(q_full(s), (uint32_t)(i / KV_Q_STAGES) & 1u)) return false;
-            clear_rows<DP>(sq + s * TILE, valid(i));
+        // products (the whole warp waits and clears, one lane issues); Q and dO of the
+        // next scores, and of the step that is formed
+        Slot<KV_Q_STAGES> qn, qi;
+        Slot<KV_DO_STAGES> dn, di;
+        int tile_q = 0, tile_d = 0;                                                // of the next step's query tiles
+        const uint32_t k_s = smem_u32(sk), v_s = smem_u32(sv), q_s = smem_u32(sq), d_s = smem_u32(sd);
+        auto scores = [&] {                                                        // S^T = K Q^T
+            if (!wait.warp(q_full(qn.at), qn.parity)) return false;
+            if (tile_q == tiles - 1) clear_rows<DP>(sq + qn.at * TILE, t.nq - (tile0 + tile_q) * ROWS);
             after_sync();
-            if (lane == 0) {
-                product_along<DP>(S, smem_u32(sk), q_at(i));
+            if (elected()) {
+                product_along<DP>(S, k_s, q_s + (uint32_t)qn.at * TILE);
                 commit(s_full);
             }
             __syncwarp();
+            qn.next();
+            if (++tile_q == tiles) tile_q = 0;
             return true;
         };
-        auto values = [&](int i) {                                                 // dP^T = V dO^T
-            const int s = i % KV_DO_STAGES;
-            if (!wait.warp(do_full(s), (uint32_t)(i / KV_DO_STAGES) & 1u)) return false;
-            clear_rows<DP>(sd + s * TILE, valid(i));
+        auto values = [&] {                                                        // dP^T = V dO^T
+            if (!wait.warp(do_full(dn.at), dn.parity)) return false;
+            if (tile_d == tiles - 1) clear_rows<DP>(sd + dn.at * TILE, t.nq - (tile0 + tile_d) * ROWS);
             after_sync();
-            if (lane == 0) {
-                product_along<DP>(dP, smem_u32(sv), do_at(i));
+            if (elected()) {
+                product_along<DP>(dP, v_s, d_s + (uint32_t)dn.at * TILE);
                 commit(dp_full);
             }
             __syncwarp();
+            dn.next();
+            if (++tile_d == tiles) tile_d = 0;
             return true;
         };
-        bool ok = steps > 0 && wait.warp(k_full, 0) && scores(0) && wait.warp(v_full, 0) && values(0);
+        bool ok = steps > 0 && wait.warp(k_full, 0) && scores() && wait.warp(v_full, 0) && values();
         for (int i = 0; ok && i < steps; ++i) {
             if (!(ok = wait.warp(p_ready, (uint32_t)i & 1u))) break;
             after_sync();
-            if (lane == 0) {
-                product_rows<DP, GR_COLS>(dV, S, do_at(i), i > 0);
-                commit(do_empty(i % KV_DO_STAGES));
+            if (elected()) {
+                product_rows<DP, GR_COLS>(dV, S, d_s + (uint32_t)di.at * TILE, i > 0);
+                commit(do_empty(di.at));
             }
             __syncwarp();
-            if (i + 1 < steps && !(ok = scores(i + 1))) break;
+            di.next();
+            if (i + 1 < steps && !(ok = scores())) break;
             if (!(ok = wait.warp(ds_ready, (uint32_t)i & 1u))) break;
             after_sync();
-            if (lane == 0) {
-                product_rows<DP, GR_COLS>(dK, dP, q_at(i), i > 0);
-                commit(q_empty(i % KV_Q_STAGES));
+            if (elected()) {
+                product_rows<DP, GR_COLS>(dK, dP, q_s + (uint32_t)qi.at * TILE, i > 0);
+                commit(q_empty(qi.at));
             }
             __syncwarp();
-            if (i + 1 < steps && !(ok = values(i + 1))) break;
+            qi.next();
+            if (i + 1 < steps && !(ok = values())) break;
         }
         // no product runs on when the tensor memory is freed, after a give-up either
-        if (lane == 0 && steps > 0) {
+        if (steps > 0 && elected()) {
             commit(done);
             wait.drain(done, 0);
         }
@@ -298,9 +304,10 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
         const ulonglong2* const neg_lse = reinterpret_cast<const ulonglong2*>(lse_s + group * GR_COLS);
         const ulonglong2* const neg_delta = reinterpret_cast<const ulonglong2*>(delta_s + group * GR_COLS);
         bool ok = true;
-        for (int i = 0; i < steps; ++i) {
+        const int column0 = tile0 * ROWS + group * GR_COLS;
+        for (int i = 0, n = 0; i < steps; ++i, n = n + 1 == tiles ? 0 : n + 1) {
             const uint32_t ph = (uint32_t)i & 1u;
-            const int q0 = (tile0 + i % tiles) * ROWS + group * GR_COLS;
+            const int q0 = column0 + n * ROWS;
             const int f = from - q0, e = to - q0;                 // this thread's columns that are seen
             const bool masked = !__all_sync(0xFFFFFFFFu, f <= 0 && e >= GR_COLS);
             uint64_t p[GR_COLS / 2];
@@ -422,44 +429,49 @@ k_tc_grad_q(const __grid_constant__ GradMaps maps, const __grid_constant__ GradA
             for (int i = max(0, nv - Q_V_STAGES); i < nv; ++i) wait.drain(v_full(i % Q_V_STAGES), (uint32_t)(i / Q_V_STAGES) & 1u);
         }
     } else if (warp == GR_COMPUTE + 1) {
-        auto k_at = [&](int i) { return smem_u32(sk) + (uint32_t)(i % Q_K_STAGES) * TILE; };
-        auto scores = [&](int i) {                                                 // S = Q K^T
-            const int s = i % Q_K_STAGES;
-            if (!wait.warp(k_full(s), (uint32_t)(i / Q_K_STAGES) & 1u)) return false;
-            clear_rows<DP>(sk + s * TILE, t.nk - (tile0 + i) * ROWS);
+        Slot<Q_K_STAGES> kn, ki;
+        Slot<Q_V_STAGES> vn;
+        const uint32_t q_s = smem_u32(sq), d_s = smem_u32(sd), k_s = smem_u32(sk), v_s = smem_u32(sv);
+        int next = 0;                                                              // the next scores
+        auto scores = [&] {                                                        // S = Q K^T
+            if (!wait.warp(k_full(kn.at), kn.parity)) return false;
+            if (next == steps - 1) clear_rows<DP>(sk + kn.at * TILE, t.nk - (tile0 + next) * ROWS);
             after_sync();
-            if (lane == 0) {
-                product_along<DP>(S + (i & 1) * 128, smem_u32(sq), k_at(i));
-                commit(s_full + 8u * (i & 1));
+            if (elected()) {
+                product_along<DP>(S + (next & 1) * 128, q_s, k_s + (uint32_t)kn.at * TILE);
+                commit(s_full + 8u * (next & 1));
             }
             __syncwarp();
+            kn.next();
+            ++next;
             return true;
         };
-        auto values = [&](int i) {                                                 // dP = dO V^T
-            const int s = i % Q_V_STAGES;
-            if (!wait.warp(v_full(s), (uint32_t)(i / Q_V_STAGES) & 1u)) return false;
+        auto values = [&] {                                                        // dP = dO V^T
+            if (!wait.warp(v_full(vn.at), vn.parity)) return false;
             after_sync();
-            if (lane == 0) {
-                product_along<DP>(dP, smem_u32(sd), smem_u32(sv) + s * TILE);
+            if (elected()) {
+                product_along<DP>(dP, d_s, v_s + (uint32_t)vn.at * TILE);
                 commit(dp_full);
-                commit(v_empty(s));
+                commit(v_empty(vn.at));
             }
             __syncwarp();
+            vn.next();
             return true;
         };
-        bool ok = steps > 0 && wait.warp(q_full, 0) && scores(0) && wait.warp(do_full, 0) && values(0) && (steps < 2 || scores(1));
+        bool ok = steps > 0 && wait.warp(q_full, 0) && scores() && wait.warp(do_full, 0) && values() && (steps < 2 || scores());
         for (int i = 0; ok && i < steps; ++i) {
             if (!(ok = wait.warp(ds_ready, (uint32_t)i & 1u))) break;
-            if (i + 1 < steps && !(ok = values(i + 1))) break;                     // dP(i) has been read
+            if (i + 1 < steps && !(ok = values())) break;                          // dP(i) has been read
             after_sync();
-            if (lane == 0) {
-                product_rows<DP, GR_COLS>(dQ, S + (i & 1) * 128, k_at(i), i > 0);
-                commit(k_empty(i % Q_K_STAGES));
+            if (elected()) {
+                product_rows<DP, GR_COLS>(dQ, S + (i & 1) * 128, k_s + (uint32_t)ki.at * TILE, i > 0);
+                commit(k_empty(ki.at));
             }
             __syncwarp();
-            if (i + 2 < steps && !(ok = scores(i + 2))) break;
+            ki.next();
+            if (i + 2 < steps && !(ok = scores())) break;
         }
-        if (lane == 0 && steps > 0) {
+        if (steps > 0 && elected()) {
             commit(done);
             wait.drain(done, 0);
         }

@@ -63,6 +63,28 @@ __device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b,
         mma_ts(d, a + k * 16 / COLS * COLS + k * 16 % COLS / 2, bl + k * (2048u >> 4), idesc(DP, true), k > 0 ? 1u : accumulate);
 }
 
+// One lane of the warp, the same each time, as the hardware elects it: code under
+// it keeps its descriptors in uniform registers, where a branch on the lane's number
+// moves each there for every product (8192 tokens, 28 heads of 128: dk and dv
+// 935 -> 810 us).  Called by the whole warp.
+__device__ __forceinline__ bool elected() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+// A slot of a ring of copies and the parity of its next phase
+template <int N>
+struct Slot {
+    int at = 0;
+    uint32_t parity = 0;
+    __device__ __forceinline__ void next() {
+        if (++at == N) {
+            at = 0;
+            parity ^= 1u;
+        }
+    }
+};
+
 // arrive on `bar` once the products issued so far are done
 __device__ __forceinline__ void commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
