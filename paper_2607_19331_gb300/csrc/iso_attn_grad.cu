@@ -37,7 +37,7 @@ namespace {
 using namespace tc;
 
 constexpr int GR_COMPUTE = 8;            // warps that compute, four on each GR_COLS columns of a tile
-constexpr int GR_COLS = 128 * 4 / GR_COMPUTE;
+constexpr int GR_COLS = 64;
 constexpr int GR_THREADS = (GR_COMPUTE + 3) * 32;
 constexpr int KV_Q_STAGES = 3, KV_DO_STAGES = 2, Q_K_STAGES = 3, Q_V_STAGES = 2;
 
@@ -296,62 +296,111 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
                 arrive_warp(delta_full);
             }
     } else {
+        // A thread has four rows of a quarter of the columns (as load_rows16 gives
+        // them), so that it needs lse and delta of 16 columns, eight bytes a load: a row of
+        // all columns a thread takes 64 of each, and the loads, broadcasts that cost
+        // shared memory what as many different words would, held the products up
+        // (WITH_ROWS us for dk and dv of 8192 tokens, 28 heads over 4 of 128).
         const int group = warp >> 2, r = (warp & 3) * 32 + lane;
-        const uint32_t at = ((uint32_t)(warp & 3) * 32) << 16, s_at = S + at + group * GR_COLS, d_at = dP + at + group * GR_COLS;
-        int from, to;
-        attn_queries_of(g, t, t.first + min(r, keys - 1), from, to);
+        const uint32_t at = ((uint32_t)(warp & 3) * 32) << 16, low = 16u << 16;
+        const uint32_t s_at = S + at + group * GR_COLS, d_at = dP + at + group * GR_COLS;
+        int from[4], to[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            attn_queries_of(g, t, t.first + min((warp & 3) * 32 + 8 * j + (lane >> 2), keys - 1), from[j], to[j]);
         const uint64_t c = pair_of(a.scale2, a.scale2);
-        const ulonglong2* const neg_lse = reinterpret_cast<const ulonglong2*>(lse_s + group * GR_COLS);
-        const ulonglong2* const neg_delta = reinterpret_cast<const ulonglong2*>(delta_s + group * GR_COLS);
+        const uint64_t* const neg_lse = reinterpret_cast<const uint64_t*>(lse_s + group * GR_COLS) + (lane & 3);
+        const uint64_t* const neg_delta = reinterpret_cast<const uint64_t*>(delta_s + group * GR_COLS) + (lane & 3);
         bool ok = true;
         const int column0 = tile0 * ROWS + group * GR_COLS;
         for (int i = 0, n = 0; i < steps; ++i, n = n + 1 == tiles ? 0 : n + 1) {
             const uint32_t ph = (uint32_t)i & 1u;
             const int q0 = column0 + n * ROWS;
-            const int f = from - q0, e = to - q0;                 // this thread's columns that are seen
-            const bool masked = !__all_sync(0xFFFFFFFFu, f <= 0 && e >= GR_COLS);
-            uint64_t p[GR_COLS / 2];
-            float v[GR_COLS];
-            uint32_t w[GR_COLS / 2];
+            bool whole = true;                                    // every column of every row is seen
+#pragma unroll
+            for (int j = 0; j < 4; ++j) whole = whole && from[j] <= q0 && to[j] >= q0 + GR_COLS;
+            const bool masked = !__all_sync(0xFFFFFFFFu, whole);
+            // of this thread's rows 8 j + lane / 4 and its columns: seen(j, column)
+            auto seen = [&](int j, int col) { return q0 + col >= from[j] && q0 + col < to[j]; };
+            uint64_t p[2][16];
+            float v[2][32];
+            uint32_t w[2][16];
             if (!(ok = wait.warp(lse_full, ph) && wait.warp(s_full, ph))) break;
             after_sync();
-            load_cols<GR_COLS>(s_at, v);
-            auto l = [&](int j) { return j & 1 ? neg_lse[j / 2].y : neg_lse[j / 2].x; };
-            if (masked) weights<true, GR_COLS>(v, p, c, f, e, l);
-            else weights<false, GR_COLS>(v, p, c, f, e, l);
+            load_rows16(s_at, v[0]);
+            load_rows16(s_at + low, v[1]);
+            loaded(v[0]);
+            loaded(v[1]);
+            auto weights = [&](auto mask) {
 #pragma unroll
-            for (int j = 0; j < GR_COLS / 2; ++j) w[j] = bf16_of(p[j]);
-            store_cols<GR_COLS>(s_at, w);
+                for (int k = 0; k < 8; ++k) {
+                    const uint64_t l = neg_lse[4 * k];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float x, y;
+                        parts_of(fma2(pair_of(v[j / 2][4 * k + 2 * (j & 1)], v[j / 2][4 * k + 2 * (j & 1) + 1]), c, l), x, y);
+                        x = ex2(x);
+                        y = ex2(y);
+                        if (decltype(mask)::value && !seen(j, 8 * k + 2 * (lane & 3))) x = 0.0f;
+                        if (decltype(mask)::value && !seen(j, 8 * k + 2 * (lane & 3) + 1)) y = 0.0f;
+                        p[j / 2][2 * k + (j & 1)] = pair_of(x, y);
+                        w[j / 2][2 * k + (j & 1)] = f32_to_bf16x2(x, y);
+                    }
+                }
+            };
+            if (masked) weights(std::true_type{});
+            else weights(std::false_type{});
+            store_rows16(s_at, w[0]);
+            store_rows16(s_at + low, w[1]);
+            stored();
             before_sync();
             arrive_warp(p_ready);
             if (lane == 0) mbar_arrive(lse_empty);
             if (!(ok = wait.warp(delta_full, ph) && wait.warp(dp_full, ph))) break;
             after_sync();
-            load_cols<GR_COLS>(d_at, v);
-            auto d = [&](int j) { return j & 1 ? neg_delta[j / 2].y : neg_delta[j / 2].x; };
-            if (masked) score_grads<true, GR_COLS>(v, p, w, f, e, d);
-            else score_grads<false, GR_COLS>(v, p, w, f, e, d);
-            store_cols<GR_COLS>(d_at, w);
+            load_rows16(d_at, v[0]);
+            load_rows16(d_at + low, v[1]);
+            loaded(v[0]);
+            loaded(v[1]);
+            auto score_grads = [&](auto mask) {                   // (what is not seen is 0 whatever dP is there)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const uint64_t d = neg_delta[4 * k];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float x, y;
+                        parts_of(mul2(add2(pair_of(v[j / 2][4 * k + 2 * (j & 1)], v[j / 2][4 * k + 2 * (j & 1) + 1]), d),
+                                      p[j / 2][2 * k + (j & 1)]), x, y);
+                        if (decltype(mask)::value && !seen(j, 8 * k + 2 * (lane & 3))) x = 0.0f;
+                        if (decltype(mask)::value && !seen(j, 8 * k + 2 * (lane & 3) + 1)) y = 0.0f;
+                        w[j / 2][2 * k + (j & 1)] = f32_to_bf16x2(x, y);
+                    }
+                }
+            };
+            if (masked) score_grads(std::true_type{});
+            else score_grads(std::false_type{});
+            store_rows16(d_at, w[0]);
+            store_rows16(d_at + low, w[1]);
+            stored();
             before_sync();
             arrive_warp(ds_ready);
             if (lane == 0) mbar_arrive(delta_empty);
         }
-        // dV by the first half of the warps, dK by the second: a row a thread, DP / PER columns
-        constexpr int PER = GR_COMPUTE / 8, WIDE = DP / PER;
-        const int half = group / PER, from_col = group % PER * WIDE;
+        // dV by the first half of the warps, dK by the second: a row a thread
+        const int half = group;
         if (steps > 0) ok = ok && wait.warp(done, 0);
         after_sync();
         const bool nan = !ok || (steps > 0 && *gave_up), none = steps == 0;
-        const uint32_t acc = (half ? dK : dV) + at + from_col;
+        const uint32_t acc = (half ? dK : dV) + at;
         const float by = half ? g.scale : 1.0f;
         const long long row = (long long)t.k0 + t.first + r;
         if (a.parts > 1) {
             const long long width = (long long)kv_heads * g.head_dim;
-            float* o = a.part + ((long long)(part * 2 + (half ? 0 : 1)) * g.k_rows + row) * width + (long long)kh * g.head_dim + from_col;
-            if (!write_row<float, WIDE>(acc, o, r < keys, g.head_dim - from_col, true, by, nan, none)) *again = 1;
+            float* o = a.part + ((long long)(part * 2 + (half ? 0 : 1)) * g.k_rows + row) * width + (long long)kh * g.head_dim;
+            if (!write_row<float, DP>(acc, o, r < keys, g.head_dim, true, by, nan, none)) *again = 1;
         } else {
-            __nv_bfloat16* o = static_cast<__nv_bfloat16*>(half ? g.dk : g.dv) + row * (half ? g.lddk : g.lddv) + (long long)kh * g.head_dim + from_col;
-            if (!write_row<__nv_bfloat16, WIDE>(acc, o, r < keys, g.head_dim - from_col, a.vec, by, nan, none)) *again = 1;
+            __nv_bfloat16* o = static_cast<__nv_bfloat16*>(half ? g.dk : g.dv) + row * (half ? g.lddk : g.lddv) + (long long)kh * g.head_dim;
+            if (!write_row<__nv_bfloat16, DP>(acc, o, r < keys, g.head_dim, a.vec, by, nan, none)) *again = 1;
         }
         before_sync();
     }
