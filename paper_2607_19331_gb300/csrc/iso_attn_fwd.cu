@@ -27,7 +27,7 @@ namespace {
 using namespace tc;
 
 constexpr int FW_COMPUTE = 8;
-constexpr int FW_THREADS = (FW_COMPUTE + 2) * 32;
+constexpr int FW_THREADS = (FW_COMPUTE + 3) * 32;
 constexpr int FW_K_STAGES = 2, FW_V_STAGES = 2;
 constexpr int FW_ROWS = 2 * ROWS;
 constexpr float RAISE = 8.0f;
@@ -103,13 +103,13 @@ k_tc_attn(const __grid_constant__ FwdMaps maps, const __grid_constant__ FwdArgs 
     auto p_ready = [&](int x) { return bar + 16u + 8u * x; };
     auto o_done = [&](int x) { return bar + 32u + 8u * x; };
     auto q_full = [&](int x) { return bar + 48u + 8u * x; };
-    const uint32_t done = bar + 64, rings = bar + 72;
+    const uint32_t done = bar + 64 /* two */, cleared = bar + 80, rings = bar + 88;
     auto k_full = [&](int s) { return rings + 8u * s; };
     auto k_empty = [&](int s) { return rings + 8u * (FW_K_STAGES + s); };
     auto v_full = [&](int s) { return rings + 8u * (2 * FW_K_STAGES + s); };
     auto v_empty = [&](int s) { return rings + 8u * (2 * FW_K_STAGES + FW_V_STAGES + s); };
     constexpr int RINGS = 2 * (FW_K_STAGES + FW_V_STAGES);
-    uint32_t* const slot = reinterpret_cast<uint32_t*>(bars + 9 + RINGS);
+    uint32_t* const slot = reinterpret_cast<uint32_t*>(bars + 11 + RINGS);
     volatile int* const gave_up = reinterpret_cast<volatile int*>(slot + 1);
     volatile int* const again = gave_up + 1;           // a sum was not finite
     const AttnArgs& g = a.g;
@@ -136,7 +136,16 @@ k_tc_attn(const __grid_constant__ FwdMaps maps, const __grid_constant__ FwdArgs 
             mbar_init(q_full(x), 1);
         }
         mbar_init(done, 1);
-        for (int s = 0; s < RINGS; ++s) mbar_init(rings + 8u * s, 1);
+        mbar_init(done + 8, 1);
+        mbar_init(cleared, 1);
+        for (int s = 0; s < FW_K_STAGES; ++s) {
+            mbar_init(k_full(s), 1);
+            mbar_init(k_empty(s), 2);            // both tiles' products
+        }
+        for (int s = 0; s < FW_V_STAGES; ++s) {
+            mbar_init(v_full(s), 1);
+            mbar_init(v_empty(s), 2);
+        }
         *gave_up = *again = 0;
         mbar_fence_init();
     }
@@ -170,66 +179,56 @@ k_tc_attn(const __grid_constant__ FwdMaps maps, const __grid_constant__ FwdArgs 
             for (int i = max(0, nk - FW_K_STAGES); i < nk; ++i) wait.drain(k_full(i % FW_K_STAGES), (uint32_t)(i / FW_K_STAGES) & 1u);
             for (int i = max(0, nv - FW_V_STAGES); i < nv; ++i) wait.drain(v_full(i % FW_V_STAGES), (uint32_t)(i / FW_V_STAGES) & 1u);
         }
-    } else if (warp == FW_COMPUTE + 1) {
-        // products (the whole warp waits and clears, one lane issues)
+    } else if (warp > FW_COMPUTE) {
+        // products, a warp for either tile: O(i), then S(i + 1) over its weights.  (The
+        // whole warp waits and clears, one lane issues.)
+        const int x = warp - FW_COMPUTE - 1;
         Slot<FW_K_STAGES> ks;                        // K of the next scores
         Slot<FW_V_STAGES> vs;
-        const uint32_t q_s = smem_u32(sq), k_s = smem_u32(sk), v_s = smem_u32(sv);
-        auto in = [&](int x, int i) { return u0 + i >= begin[x] && u0 + i < end[x]; };
-        auto scores = [&](int x, int i) {                                          // S = Q K^T
-            if (!in(x, i)) return;
-            if (elected()) {
-                product_along<DP>(S(x), q_s + (uint32_t)x * TILE, k_s + (uint32_t)ks.at * TILE);
-                commit(s_full(x));
-            }
-            __syncwarp();
-        };
-        auto sums = [&](int x, int i) {                                            // O += P V
-            if (!in(x, i)) return true;
-            const int j = u0 + i - begin[x];
-            if (!wait.warp(p_ready(x), (uint32_t)j & 1u)) return false;
+        const uint32_t q_s = smem_u32(sq) + (uint32_t)x * TILE, k_s = smem_u32(sk), v_s = smem_u32(sv);
+        auto in = [&](int i) { return u0 + i >= begin[x] && u0 + i < end[x]; };
+        auto scores = [&](int i) {                                                 // S = Q K^T
+            if (!wait.warp(k_full(ks.at), ks.parity)) return false;
             after_sync();
             if (elected()) {
-                product_rows<DP, 128>(O(x), S(x), v_s + (uint32_t)vs.at * TILE, j > 0);
-                commit(o_done(x));
+                if (in(i)) {
+                    product_along<DP>(S(x), q_s, k_s + (uint32_t)ks.at * TILE);
+                    commit(s_full(x));
+                }
+                commit(k_empty(ks.at));
             }
-            __syncwarp();
-            return true;
-        };
-        bool ok = steps > 0 && (!has[0] || wait.warp(q_full(0), 0)) && (!has[1] || wait.warp(q_full(1), 0)) &&
-                  wait.warp(k_full(0), 0);
-        if (ok) {
-            after_sync();
-            scores(0, 0);
-            scores(1, 0);
-            if (elected()) commit(k_empty(0));
             __syncwarp();
             ks.next();
-        }
+            return true;
+        };
+        bool ok = steps > 0 && (!has[x] || wait.warp(q_full(x), 0)) && scores(0);
         for (int i = 0; ok && i < steps; ++i) {
             if (!(ok = wait.warp(v_full(vs.at), vs.parity))) break;
-            if (i == steps - 1) clear_rows<DP>(sv + vs.at * TILE, t.nk - (u0 + i) * ROWS);
-            if (!(ok = sums(0, i))) break;
-            if (i + 1 < steps) {
-                if (!(ok = wait.warp(k_full(ks.at), ks.parity))) break;
+            if (in(i)) {
+                const int j = u0 + i - begin[x];
+                if (i == steps - 1) {
+                    // one warp clears the rows behind the sequence's end, for both
+                    if (x == 0 || !has[0] || u0 + i >= end[0]) clear_rows<DP>(sv + vs.at * TILE, t.nk - (u0 + i) * ROWS);
+                    else if (!(ok = wait.warp(cleared, 0))) break;
+                    if (x == 0) arrive_warp(cleared);
+                }
+                if (!(ok = wait.warp(p_ready(x), (uint32_t)j & 1u))) break;
                 after_sync();
-                scores(0, i + 1);
+                if (elected()) {
+                    product_rows<DP, 128>(O(x), S(x), v_s + (uint32_t)vs.at * TILE, j > 0);   // O += P V
+                    commit(o_done(x));
+                }
+                __syncwarp();
             }
-            if (!(ok = sums(1, i))) break;
             if (elected()) commit(v_empty(vs.at));
             __syncwarp();
             vs.next();
-            if (i + 1 < steps) {
-                scores(1, i + 1);
-                if (elected()) commit(k_empty(ks.at));
-                __syncwarp();
-                ks.next();
-            }
+            if (i + 1 < steps) ok = scores(i + 1);
         }
         // no product runs on when the tensor memory is freed, after a give-up either
         if (steps > 0 && elected()) {
-            commit(done);
-            wait.drain(done, 0);
+            commit(done + 8u * x);
+            wait.drain(done + 8u * x, 0);
         }
     } else {
         const int x = warp >> 2, r = (warp & 3) * 32 + lane, mine = min(ROWS, rows - x * ROWS);

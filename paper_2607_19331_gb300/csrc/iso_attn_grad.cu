@@ -38,7 +38,7 @@ using namespace tc;
 
 constexpr int GR_COMPUTE = 8;            // warps that compute, four on each GR_COLS columns of a tile
 constexpr int GR_COLS = 64;
-constexpr int GR_THREADS = (GR_COMPUTE + 3) * 32;
+constexpr int GR_THREADS = (GR_COMPUTE + 4) * 32;
 constexpr int KV_Q_STAGES = 3, KV_DO_STAGES = 2, Q_K_STAGES = 3, Q_V_STAGES = 2;
 
 struct GradMaps {
@@ -150,13 +150,13 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
     const uint32_t bar = smem_u32(bars);
     const uint32_t k_full = bar, v_full = bar + 8, s_full = bar + 16, dp_full = bar + 24, p_ready = bar + 32,
                    ds_ready = bar + 40, lse_full = bar + 48, lse_empty = bar + 56, delta_full = bar + 64,
-                   delta_empty = bar + 72, done = bar + 80, rings = bar + 88;
+                   delta_empty = bar + 72, done = bar + 80, done2 = bar + 88, cleared = bar + 96 /* two */, rings = bar + 112;
     auto q_full = [&](int s) { return rings + 8u * s; };
     auto q_empty = [&](int s) { return rings + 8u * (KV_Q_STAGES + s); };
     auto do_full = [&](int s) { return rings + 8u * (2 * KV_Q_STAGES + s); };
     auto do_empty = [&](int s) { return rings + 8u * (2 * KV_Q_STAGES + KV_DO_STAGES + s); };
     constexpr int RINGS = 2 * (KV_Q_STAGES + KV_DO_STAGES);
-    uint32_t* const slot = reinterpret_cast<uint32_t*>(bars + 11 + RINGS);
+    uint32_t* const slot = reinterpret_cast<uint32_t*>(bars + 14 + RINGS);
     volatile int* const gave_up = reinterpret_cast<volatile int*>(slot + 1);
     volatile int* const again = gave_up + 1;           // a sum was not finite
     const AttnArgs& g = a.g;
@@ -175,9 +175,18 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
     const int steps = (h1 - h0) * tiles;
 
     if (threadIdx.x == 0) {
-        for (uint32_t b : {k_full, v_full, s_full, dp_full, lse_full, delta_full, done}) mbar_init(b, 1);
+        for (uint32_t b : {k_full, v_full, s_full, dp_full, lse_full, delta_full, done, done2}) mbar_init(b, 1);
         for (uint32_t b : {p_ready, ds_ready, lse_empty, delta_empty}) mbar_init(b, GR_COMPUTE);
-        for (int s = 0; s < RINGS; ++s) mbar_init(rings + 8u * s, 1);
+        mbar_init(cleared, 1);
+        mbar_init(cleared + 8, 1);
+        for (int s = 0; s < KV_Q_STAGES; ++s) {
+            mbar_init(q_full(s), 1);
+            mbar_init(q_empty(s), 1);
+        }
+        for (int s = 0; s < KV_DO_STAGES; ++s) {
+            mbar_init(do_full(s), 1);
+            mbar_init(do_empty(s), 2);           // dP's products and dV's
+        }
         *gave_up = *again = 0;
         mbar_fence_init();
     }
@@ -212,15 +221,15 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
             for (int i = max(0, nd - KV_DO_STAGES); i < nd; ++i) wait.drain(do_full(i % KV_DO_STAGES), (uint32_t)(i / KV_DO_STAGES) & 1u);
         }
     } else if (warp == GR_COMPUTE + 1) {
-        // products (the whole warp waits and clears, one lane issues); Q and dO of the
-        // next scores, and of the step that is formed
-        Slot<KV_Q_STAGES> qn, qi;
-        Slot<KV_DO_STAGES> dn, di;
-        int tile_q = 0, tile_d = 0;                                                // of the next step's query tiles
-        const uint32_t k_s = smem_u32(sk), v_s = smem_u32(sv), q_s = smem_u32(sq), d_s = smem_u32(sd);
+        // products of the weights: dV(i), then S^T(i + 1) over them.  (A whole warp waits
+        // and clears, one lane issues.)
+        Slot<KV_Q_STAGES> qn;                                                      // Q of the next scores
+        Slot<KV_DO_STAGES> di;
+        int tile = 0, tile_i = 0, tails = 0;                                       // its tile, step i's, last tiles so far
+        const uint32_t k_s = smem_u32(sk), q_s = smem_u32(sq), d_s = smem_u32(sd);
         auto scores = [&] {                                                        // S^T = K Q^T
             if (!wait.warp(q_full(qn.at), qn.parity)) return false;
-            if (tile_q == tiles - 1) clear_rows<DP>(sq + qn.at * TILE, t.nq - (tile0 + tile_q) * ROWS);
+            if (tile == tiles - 1) clear_rows<DP>(sq + qn.at * TILE, t.nq - (tile0 + tile) * ROWS);
             after_sync();
             if (elected()) {
                 product_along<DP>(S, k_s, q_s + (uint32_t)qn.at * TILE);
@@ -228,24 +237,18 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
             }
             __syncwarp();
             qn.next();
-            if (++tile_q == tiles) tile_q = 0;
+            if (++tile == tiles) tile = 0;
             return true;
         };
-        auto values = [&] {                                                        // dP^T = V dO^T
-            if (!wait.warp(do_full(dn.at), dn.parity)) return false;
-            if (tile_d == tiles - 1) clear_rows<DP>(sd + dn.at * TILE, t.nq - (tile0 + tile_d) * ROWS);
-            after_sync();
-            if (elected()) {
-                product_along<DP>(dP, v_s, d_s + (uint32_t)dn.at * TILE);
-                commit(dp_full);
-            }
-            __syncwarp();
-            dn.next();
-            if (++tile_d == tiles) tile_d = 0;
-            return true;
-        };
-        bool ok = steps > 0 && wait.warp(k_full, 0) && scores() && wait.warp(v_full, 0) && values();
+        bool ok = steps > 0 && wait.warp(k_full, 0) && scores();
         for (int i = 0; ok && i < steps; ++i) {
+            // dO is there, and where it had to be cleared, cleared (by the other warp)
+            if (!(ok = wait.warp(do_full(di.at), di.parity))) break;
+            if (++tile_i == tiles) {
+                tile_i = 0;
+                if (!(ok = wait.warp(cleared + 8u * (tails & 1), (uint32_t)(tails >> 1) & 1u))) break;
+                ++tails;
+            }
             if (!(ok = wait.warp(p_ready, (uint32_t)i & 1u))) break;
             after_sync();
             if (elected()) {
@@ -254,7 +257,38 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
             }
             __syncwarp();
             di.next();
-            if (i + 1 < steps && !(ok = scores())) break;
+            if (i + 1 < steps) ok = scores();
+        }
+        // no product runs on when the tensor memory is freed, after a give-up either
+        if (steps > 0 && elected()) {
+            commit(done);
+            wait.drain(done, 0);
+        }
+    } else if (warp == GR_COMPUTE + 2) {
+        // products of the scores' gradients: dK(i), then dP^T(i + 1) over them
+        Slot<KV_DO_STAGES> dn;
+        Slot<KV_Q_STAGES> qi;
+        int tile = 0, tails = 0;
+        const uint32_t v_s = smem_u32(sv), q_s = smem_u32(sq), d_s = smem_u32(sd);
+        auto values = [&] {                                                        // dP^T = V dO^T
+            if (!wait.warp(do_full(dn.at), dn.parity)) return false;
+            if (tile == tiles - 1) {
+                clear_rows<DP>(sd + dn.at * TILE, t.nq - (tile0 + tile) * ROWS);
+                arrive_warp(cleared + 8u * (tails++ & 1));
+            }
+            after_sync();
+            if (elected()) {
+                product_along<DP>(dP, v_s, d_s + (uint32_t)dn.at * TILE);
+                commit(dp_full);
+                commit(do_empty(dn.at));
+            }
+            __syncwarp();
+            dn.next();
+            if (++tile == tiles) tile = 0;
+            return true;
+        };
+        bool ok = steps > 0 && wait.warp(v_full, 0) && values();
+        for (int i = 0; ok && i < steps; ++i) {
             if (!(ok = wait.warp(ds_ready, (uint32_t)i & 1u))) break;
             after_sync();
             if (elected()) {
@@ -263,14 +297,13 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
             }
             __syncwarp();
             qi.next();
-            if (i + 1 < steps && !(ok = values())) break;
+            if (i + 1 < steps) ok = values();
         }
-        // no product runs on when the tensor memory is freed, after a give-up either
         if (steps > 0 && elected()) {
-            commit(done);
-            wait.drain(done, 0);
+            commit(done2);
+            wait.drain(done2, 0);
         }
-    } else if (warp == GR_COMPUTE + 2) {
+    } else if (warp == GR_COMPUTE + 3) {
         // -lse log2 e and -delta of a step's queries: four a lane.  A query behind the
         // sequence's end has an infinite lse, so that its weights are 0.
         int i = 0;
@@ -388,7 +421,7 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
         }
         // dV by the first half of the warps, dK by the second: a row a thread
         const int half = group;
-        if (steps > 0) ok = ok && wait.warp(done, 0);
+        if (steps > 0) ok = ok && wait.warp(half ? done2 : done, 0);
         after_sync();
         const bool nan = !ok || (steps > 0 && *gave_up), none = steps == 0;
         const uint32_t acc = (half ? dK : dV) + at;
@@ -422,14 +455,14 @@ k_tc_grad_q(const __grid_constant__ GradMaps maps, const __grid_constant__ GradA
     unsigned char *const sq = smem, *const sd = sq + TILE, *const sk = sd + TILE, *const sv = sk + Q_K_STAGES * TILE;
     uint64_t* const bars = reinterpret_cast<uint64_t*>(sv + Q_V_STAGES * TILE);
     const uint32_t bar = smem_u32(bars);
-    const uint32_t q_full = bar, do_full = bar + 8, s_full = bar + 16 /* two */, dp_full = bar + 32, ds_ready = bar + 40,
-                   done = bar + 48, rings = bar + 56;
+    const uint32_t q_full = bar, do_full = bar + 8, s_full = bar + 16 /* two */, dp_full = bar + 32, ds_ready = bar + 40 /* two */,
+                   done = bar + 56, done2 = bar + 64, rings = bar + 72;
     auto k_full = [&](int s) { return rings + 8u * s; };
     auto k_empty = [&](int s) { return rings + 8u * (Q_K_STAGES + s); };
     auto v_full = [&](int s) { return rings + 8u * (2 * Q_K_STAGES + s); };
     auto v_empty = [&](int s) { return rings + 8u * (2 * Q_K_STAGES + Q_V_STAGES + s); };
     constexpr int RINGS = 2 * (Q_K_STAGES + Q_V_STAGES);
-    uint32_t* const slot = reinterpret_cast<uint32_t*>(bars + 7 + RINGS);
+    uint32_t* const slot = reinterpret_cast<uint32_t*>(bars + 9 + RINGS);
     volatile int* const gave_up = reinterpret_cast<volatile int*>(slot + 1);
     volatile int* const again = gave_up + 1;           // a sum was not finite
     const AttnArgs& g = a.g;
@@ -445,8 +478,9 @@ k_tc_grad_q(const __grid_constant__ GradMaps maps, const __grid_constant__ GradA
     const int tile0 = lo / ROWS, steps = hi > lo ? (hi + ROWS - 1) / ROWS - tile0 : 0;
 
     if (threadIdx.x == 0) {
-        for (uint32_t b : {q_full, do_full, s_full, s_full + 8, dp_full, done}) mbar_init(b, 1);
+        for (uint32_t b : {q_full, do_full, s_full, s_full + 8, dp_full, done, done2}) mbar_init(b, 1);
         mbar_init(ds_ready, GR_COMPUTE);
+        mbar_init(ds_ready + 8, GR_COMPUTE);
         for (int s = 0; s < RINGS; ++s) mbar_init(rings + 8u * s, 1);
         *gave_up = *again = 0;
         mbar_fence_init();
@@ -478,9 +512,10 @@ k_tc_grad_q(const __grid_constant__ GradMaps maps, const __grid_constant__ GradA
             for (int i = max(0, nv - Q_V_STAGES); i < nv; ++i) wait.drain(v_full(i % Q_V_STAGES), (uint32_t)(i / Q_V_STAGES) & 1u);
         }
     } else if (warp == GR_COMPUTE + 1) {
+        // dQ(i), then S(i + 2) over its weights.  (A whole warp waits and clears, one
+        // lane issues.)
         Slot<Q_K_STAGES> kn, ki;
-        Slot<Q_V_STAGES> vn;
-        const uint32_t q_s = smem_u32(sq), d_s = smem_u32(sd), k_s = smem_u32(sk), v_s = smem_u32(sv);
+        const uint32_t q_s = smem_u32(sq), k_s = smem_u32(sk);
         int next = 0;                                                              // the next scores
         auto scores = [&] {                                                        // S = Q K^T
             if (!wait.warp(k_full(kn.at), kn.parity)) return false;
@@ -495,22 +530,9 @@ k_tc_grad_q(const __grid_constant__ GradMaps maps, const __grid_constant__ GradA
             ++next;
             return true;
         };
-        auto values = [&] {                                                        // dP = dO V^T
-            if (!wait.warp(v_full(vn.at), vn.parity)) return false;
-            after_sync();
-            if (elected()) {
-                product_along<DP>(dP, d_s, v_s + (uint32_t)vn.at * TILE);
-                commit(dp_full);
-                commit(v_empty(vn.at));
-            }
-            __syncwarp();
-            vn.next();
-            return true;
-        };
-        bool ok = steps > 0 && wait.warp(q_full, 0) && scores() && wait.warp(do_full, 0) && values() && (steps < 2 || scores());
+        bool ok = steps > 0 && wait.warp(q_full, 0) && scores() && (steps < 2 || scores());
         for (int i = 0; ok && i < steps; ++i) {
-            if (!(ok = wait.warp(ds_ready, (uint32_t)i & 1u))) break;
-            if (i + 1 < steps && !(ok = values())) break;                          // dP(i) has been read
+            if (!(ok = wait.warp(ds_ready + 8u * (i & 1), (uint32_t)(i >> 1) & 1u))) break;
             after_sync();
             if (elected()) {
                 product_rows<DP, GR_COLS>(dQ, S + (i & 1) * 128, k_s + (uint32_t)ki.at * TILE, i > 0);
@@ -518,11 +540,33 @@ k_tc_grad_q(const __grid_constant__ GradMaps maps, const __grid_constant__ GradA
             }
             __syncwarp();
             ki.next();
-            if (i + 2 < steps && !(ok = scores())) break;
+            if (i + 2 < steps) ok = scores();
         }
+        // no product runs on when the tensor memory is freed, after a give-up either
         if (steps > 0 && elected()) {
             commit(done);
             wait.drain(done, 0);
+        }
+    } else if (warp == GR_COMPUTE + 2) {
+        // dP(i + 1) once dP(i) has been read
+        Slot<Q_V_STAGES> vn;
+        const uint32_t d_s = smem_u32(sd), v_s = smem_u32(sv);
+        bool ok = steps > 0 && wait.warp(do_full, 0);
+        for (int i = 0; ok && i < steps; ++i) {
+            if (i > 0 && !(ok = wait.warp(ds_ready + 8u * ((i - 1) & 1), (uint32_t)((i - 1) >> 1) & 1u))) break;
+            if (!(ok = wait.warp(v_full(vn.at), vn.parity))) break;
+            after_sync();
+            if (elected()) {
+                product_along<DP>(dP, d_s, v_s + (uint32_t)vn.at * TILE);          // dP = dO V^T
+                commit(dp_full);
+                commit(v_empty(vn.at));
+            }
+            __syncwarp();
+            vn.next();
+        }
+        if (steps > 0 && elected()) {
+            commit(done2);
+            wait.drain(done2, 0);
         }
     } else if (warp < GR_COMPUTE) {
         const int group = warp >> 2, r = (warp & 3) * 32 + lane;
@@ -553,7 +597,7 @@ k_tc_grad_q(const __grid_constant__ GradMaps maps, const __grid_constant__ GradA
             else score_grads<false, GR_COLS>(v, p, w, f, e, [&](int) { return dd; });
             store_cols<GR_COLS>(s_at, w);
             before_sync();
-            arrive_warp(ds_ready);
+            arrive_warp(ds_ready + 8u * (i & 1));
         }
         if (steps > 0) ok = ok && wait.warp(done, 0);
         after_sync();

@@ -200,28 +200,28 @@ __device__ __forceinline__ bool probe(uint32_t bar, uint32_t parity) {
 }
 // Bounded waits of a CTA.  A wait that gives up sets the flag, and with it every
 // other wait of the CTA ends.
+static __device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity, uint64_t limit_ns, volatile int* gave_up) {
+    WaitClock clock;
+    for (int spin = 0; spin < MBAR_SPIN_LIMIT; ++spin) {
+        if (probe(bar, parity)) return true;
+        if ((spin & 31) == 31 && ((gave_up && *gave_up) || clock.look(now_ns(), limit_ns))) break;
+    }
+    if (gave_up) *gave_up = 1;
+    return false;
+}
 struct Waits {
     uint64_t limit_ns;
     volatile int* gave_up;
-    __device__ __forceinline__ bool one(uint32_t bar, uint32_t parity, uint64_t limit, bool heed) const {
-        WaitClock clock;
-        for (int spin = 0; spin < MBAR_SPIN_LIMIT; ++spin) {
-            if (probe(bar, parity)) return true;
-            if ((spin & 31) == 31 && ((heed && *gave_up) || clock.look(now_ns(), limit))) return false;
-        }
-        return false;
-    }
     __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
-        if (one(bar, parity, limit_ns, true)) return true;
-        *gave_up = 1;
-        return false;
+        return probe(bar, parity) || wait_long(bar, parity, limit_ns, gave_up);
     }
     // one answer for the whole warp
     __device__ __forceinline__ bool warp(uint32_t bar, uint32_t parity) const {
-        return __all_sync(0xFFFFFFFFu, (*this)(bar, parity));
+        if (__all_sync(0xFFFFFFFFu, probe(bar, parity))) return true;
+        return __all_sync(0xFFFFFFFFu, wait_long(bar, parity, limit_ns, gave_up));
     }
     // for what is in flight in any case (a copy, a product): not cut short by the flag
-    __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) const { one(bar, parity, 2000000000u, false); }
+    __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) const { wait_long(bar, parity, 2000000000u, nullptr); }
 };
 
 // two binary32 numbers at a time
