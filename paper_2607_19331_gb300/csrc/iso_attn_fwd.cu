@@ -257,11 +257,15 @@ k_tc_attn(const __grid_constant__ FwdMaps maps, const __grid_constant__ FwdArgs 
                     for (int i = 0; i < 32; ++i)
                         if (!(q * 32 + i >= f && q * 32 + i < e)) v[q][i] = -INFINITY;
             }
-            float top = v[0][0];
+            float tops[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int q = 0; q < 4; ++q) {
+                tops[q] = max3(v[q][0], v[q][1], v[q][2]);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) top = fmaxf(top, v[q][i]);
+                for (int i = 3; i < 31; i += 2) tops[q] = max3(tops[q], v[q][i], v[q][i + 1]);
+                tops[q] = fmaxf(tops[q], v[q][31]);
+            }
+            const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
             // from -Inf any finite maximum is a raise
             const bool raise = (top - m) * c > RAISE;
             if (__any_sync(0xFFFFFFFFu, raise)) {
@@ -282,16 +286,19 @@ k_tc_attn(const __grid_constant__ FwdMaps maps, const __grid_constant__ FwdArgs 
                     }
                 }
             }
-            const float base = m == -INFINITY ? 0.0f : m * c;
-            float sum[4] = {};
+            const float base = m == -INFINITY ? 0.0f : -m * c;
+            const uint64_t cc = pair_of(c, c), bb = pair_of(base, base);
+            uint64_t sum[2] = {};
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 uint32_t w[16];
 #pragma unroll
                 for (int i = 0; i < 32; i += 2) {
-                    const float p0 = ex2(fmaf(v[q][i], c, -base)), p1 = ex2(fmaf(v[q][i + 1], c, -base));
-                    sum[(i / 2) % 4] += p0;
-                    sum[(i / 2 + 1) % 4] += p1;
+                    float p0, p1;
+                    parts_of(fma2(pair_of(v[q][i], v[q][i + 1]), cc, bb), p0, p1);
+                    p0 = ex2(p0);
+                    p1 = ex2(p1);
+                    sum[i / 2 % 2] = add2(sum[i / 2 % 2], pair_of(p0, p1));
                     w[i / 2] = f32_to_bf16x2(p0, p1);
                 }
                 store16(s_at + q * 16, w);
@@ -299,7 +306,9 @@ k_tc_attn(const __grid_constant__ FwdMaps maps, const __grid_constant__ FwdArgs 
             stored();
             before_sync();
             arrive_warp(p_ready(x));
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            float l0, l1;
+            parts_of(add2(sum[0], sum[1]), l0, l1);
+            l += l0 + l1;
         }
         if (n > 0) ok = ok && wait.warp(o_done(x), (uint32_t)(n - 1) & 1u);
         after_sync();

@@ -251,6 +251,12 @@ __device__ __forceinline__ uint32_t bf16_of(uint64_t v) {
     parts_of(v, a, b);
     return f32_to_bf16x2(a, b);
 }
+// the largest of three; a NaN counts as nothing
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
