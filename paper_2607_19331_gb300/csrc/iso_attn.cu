@@ -90,7 +90,44 @@ __global__ void __launch_bounds__(SA_TPB) k_simt_grad_q(AttnArgs g) {
     if (attn_find_tile(g, blockIdx.x / g.heads, SA_B, false, t)) simt_grad_q<T, DP>(g, t, blockIdx.x % g.heads, sa_smem_);
 }
 
-// delta[h][i] = sum_d dout_id out_id: a warp per row and head
+// delta[h][i] = sum_d dout_id out_id, heads that are whole 16-byte words at such
+// boundaries: a word of both a lane, 16 lanes a row and head, DELTA_EACH of them in flight (one
+// lane a channel measured DELTA_SLOW)
+constexpr int DELTA_EACH = 4;
+__global__ void __launch_bounds__(256) k_attn_delta_words(AttnArgs g) {
+    const long long n = (long long)g.q_rows * g.heads, group = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 4;
+    const int lane = threadIdx.x & 15, c = lane * 8;
+    const bool in = c < g.head_dim;
+    uint4 o[DELTA_EACH], d[DELTA_EACH];
+#pragma unroll
+    for (int j = 0; j < DELTA_EACH; ++j) {
+        const long long i = group * DELTA_EACH + j, row = i / g.heads, h = i - row * g.heads;
+        o[j] = d[j] = make_uint4(0u, 0u, 0u, 0u);
+        if (i < n && in) {
+            o[j] = __ldcs(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(g.out) + row * g.ldo + h * g.head_dim + c));
+            d[j] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(g.dout) + row * g.lddo + h * g.head_dim + c);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < DELTA_EACH; ++j) {
+        const long long i = group * DELTA_EACH + j, row = i / g.heads, h = i - row * g.heads;
+        const uint32_t a[4] = {o[j].x, o[j].y, o[j].z, o[j].w}, b[4] = {d[j].x, d[j].y, d[j].z, d[j].w};
+        float s = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float x, y, u, w;
+            bf16x2_to_f32(a[k], x, y);
+            bf16x2_to_f32(b[k], u, w);
+            s = fmaf(x, u, s);
+            s = fmaf(y, w, s);
+        }
+#pragma unroll
+        for (int k = 8; k; k >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, k);
+        if (lane == 0 && i < n) g.delta[h * g.q_rows + row] = s;
+    }
+}
+
+// The same of any head: a warp per row and head
 template <typename T>
 __global__ void __launch_bounds__(256) k_attn_delta(AttnArgs g) {
     const long long i = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
@@ -325,7 +362,12 @@ int32_t iso_attn_grad(const iso_mat* dout, const iso_mat* q, const iso_mat* k, c
         if (q->rows) {
             const long long warps = (long long)q->rows * cfg->heads;
             if ((warps + 7) / 8 > EXTENT_LIMIT) return ISO_ERR_UNSUPPORTED;
-            TRAIN_LAUNCH((k_attn_delta<T><<<(unsigned)((warps + 7) / 8), 256, 0, s>>>(g)));
+            if (on_tensor_cores(cfg, out, dout)) {
+                const long long groups = (warps + DELTA_EACH - 1) / DELTA_EACH;
+                TRAIN_LAUNCH((k_attn_delta_words<<<(unsigned)((groups + 15) / 16), 256, 0, s>>>(g)));
+            } else {
+                TRAIN_LAUNCH((k_attn_delta<T><<<(unsigned)((warps + 7) / 8), 256, 0, s>>>(g)));
+            }
         }
         if (on_tensor_cores(cfg, q, k, v, dout))
             return attn_grad_tc(g, attn_grad_plan(q->rows, k->rows, *cfg),

@@ -128,7 +128,7 @@ k_tc_attn(const __grid_constant__ FwdMaps maps, const __grid_constant__ FwdArgs 
     const int u1 = has[0] && has[1] ? max(end[0], end[1]) : has[0] ? end[0] : end[1];
     const int steps = u1 - u0;
 
-    if (threadIdx.x == 0) {
+    if (warp == FW_COMPUTE && lane == 0) {
         for (int x = 0; x < 2; ++x) {
             mbar_init(s_full(x), 1);
             mbar_init(p_ready(x), FW_COMPUTE / 2);
@@ -148,6 +148,12 @@ k_tc_attn(const __grid_constant__ FwdMaps maps, const __grid_constant__ FwdArgs 
         }
         *gave_up = *again = 0;
         mbar_fence_init();
+        if (steps > 0) {                         // the first copies, while the CTA gets ready
+            for (int x = 0; x < 2; ++x)
+                if (has[x]) load_tile<DP>(smem_u32(sq) + x * TILE, &maps.q, h, t.q0 + t.first + x * ROWS, q_full(x));
+            load_tile<DP>(smem_u32(sk), &maps.k, kh, t.k0 + u0 * ROWS, k_full(0));
+            load_tile<DP>(smem_u32(sv), &maps.v, kh, t.k0 + u0 * ROWS, v_full(0));
+        }
     }
     if (warp == 0) alloc_all(smem_u32(slot));
     before_sync();
@@ -159,12 +165,10 @@ k_tc_attn(const __grid_constant__ FwdMaps maps, const __grid_constant__ FwdArgs 
     auto O = [&](int x) { return tmem + 256u + 128u * x; };
 
     if (warp == FW_COMPUTE) {
-        // copies
+        // copies, of the second key tile on
         if (lane == 0 && steps > 0) {
-            for (int x = 0; x < 2; ++x)
-                if (has[x]) load_tile<DP>(smem_u32(sq) + x * TILE, &maps.q, h, t.q0 + t.first + x * ROWS, q_full(x));
-            int nk = 0, nv = 0;
-            for (int i = 0; i < steps; ++i) {
+            int nk = 1, nv = 1;
+            for (int i = 1; i < steps; ++i) {
                 const int row = t.k0 + (u0 + i) * ROWS, ks = nk % FW_K_STAGES, vs = nv % FW_V_STAGES;
                 if (!wait(k_empty(ks), (uint32_t)(nk / FW_K_STAGES + 1) & 1u)) break;
                 load_tile<DP>(smem_u32(sk) + ks * TILE, &maps.k, kh, row, k_full(ks));

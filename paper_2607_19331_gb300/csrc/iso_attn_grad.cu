@@ -29,7 +29,7 @@
 #include "iso_tc.cuh"
 
 #include <algorithm>
-#include <atomic>
+#include <cmath>
 
 namespace iso {
 namespace {
@@ -40,6 +40,10 @@ constexpr int GR_COMPUTE = 8;            // warps that compute, four on each GR_
 constexpr int GR_COLS = 64;
 constexpr int GR_THREADS = (GR_COMPUTE + 4) * 32;
 constexpr int KV_Q_STAGES = 3, KV_DO_STAGES = 2, Q_K_STAGES = 3, Q_V_STAGES = 2;
+
+// the plan's estimates: a CTA's start and end and a join's launch in steps, and the
+// bytes that the card moves in one
+constexpr double GR_ITEM_STEPS = 2.5, GR_JOIN_STEPS = 1.5, GR_STEP_BYTES = 1.1e7, GR_TAIL = 0.15;
 
 struct GradMaps {
     CUtensorMap q, k, v, dout;
@@ -105,6 +109,7 @@ struct GradArgs {
     int32_t vec;                 // rows of the outputs start on 16-byte boundaries
     int32_t parts;               // (keys) parts of a key head's query heads, each with its own sums
     float* part;                 // (keys) parts > 1: [part][dk, dv][k_rows][kv_heads dim]
+    int32_t kv_items;            // CTAs of k_tc_grad that take keys, the first ones; the others take queries
 };
 
 // A CTA's rows done over in binary32 (iso_attn_simt.cuh), by 256 of its threads.
@@ -129,20 +134,18 @@ __device__ __noinline__ void again_kv(const GradArgs& a, float* smem) {
 }
 template <int DP>
 __device__ __noinline__ void again_q(const GradArgs& a, float* smem) {
+    const int index = (int)blockIdx.x - a.kv_items;
     AttnTile t;
-    if (!attn_find_tile(a.g, blockIdx.x / a.g.heads, ROWS, false, t)) return;
+    if (!attn_find_tile(a.g, index / a.g.heads, ROWS, false, t)) return;
     for (const int last = t.first + min(ROWS, t.nq - t.first); t.first < last; t.first += SA_B) {
-        simt_grad_q<__nv_bfloat16, DP>(a.g, t, blockIdx.x % a.g.heads, smem);
+        simt_grad_q<__nv_bfloat16, DP>(a.g, t, index % a.g.heads, smem);
         sa_sync();
     }
 }
 
 template <int DP>
-__global__ void __launch_bounds__(GR_THREADS, 1)
-k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ GradArgs a) {
+__device__ __forceinline__ void grad_kv(const GradMaps& maps, const GradArgs& a, unsigned char* smem) {
     constexpr int TILE = GradTile<DP>::TILE;
-    extern __shared__ unsigned char gr_smem_raw[];
-    unsigned char* const smem = align1024(gr_smem_raw);
     unsigned char *const sk = smem, *const sv = sk + TILE, *const sq = sv + TILE, *const sd = sq + KV_Q_STAGES * TILE;
     float* const lse_s = reinterpret_cast<float*>(sd + KV_DO_STAGES * TILE);
     float* const delta_s = lse_s + ROWS;
@@ -174,7 +177,7 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
     const int h0 = kh * g.group + g.group * part / a.parts, h1 = kh * g.group + g.group * (part + 1) / a.parts;
     const int steps = (h1 - h0) * tiles;
 
-    if (threadIdx.x == 0) {
+    if (warp == GR_COMPUTE && lane == 0) {
         for (uint32_t b : {k_full, v_full, s_full, dp_full, lse_full, delta_full, done, done2}) mbar_init(b, 1);
         for (uint32_t b : {p_ready, ds_ready, lse_empty, delta_empty}) mbar_init(b, GR_COMPUTE);
         mbar_init(cleared, 1);
@@ -189,6 +192,12 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
         }
         *gave_up = *again = 0;
         mbar_fence_init();
+        if (steps > 0) {                         // the first copies, while the CTA gets ready
+            load_tile<DP>(smem_u32(sk), &maps.k, kh, t.k0 + t.first, k_full);
+            load_tile<DP>(smem_u32(sq), &maps.q, h0, t.q0 + tile0 * ROWS, q_full(0));
+            load_tile<DP>(smem_u32(sv), &maps.v, kh, t.k0 + t.first, v_full);
+            load_tile<DP>(smem_u32(sd), &maps.dout, h0, t.q0 + tile0 * ROWS, do_full(0));
+        }
     }
     if (warp == 0) alloc_all(smem_u32(slot));
     before_sync();
@@ -199,24 +208,25 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
     const Waits wait = {a.wait_ns, gave_up};
 
     if (warp == GR_COMPUTE) {
-        // copies
+        // copies, of the second step on
         if (lane == 0 && steps > 0) {
-            load_tile<DP>(smem_u32(sk), &maps.k, kh, t.k0 + t.first, k_full);
-            int nq = 0, nd = 0;
-            bool ok = true;
-            for (int h = h0; ok && h < h1; ++h)
-                for (int n = 0; n < tiles; ++n) {
-                    const int row = t.q0 + (tile0 + n) * ROWS, qs = nq % KV_Q_STAGES, ds = nd % KV_DO_STAGES;
-                    if (!(ok = wait(q_empty(qs), (uint32_t)(nq / KV_Q_STAGES + 1) & 1u))) break;
-                    load_tile<DP>(smem_u32(sq) + qs * TILE, &maps.q, h, row, q_full(qs));
-                    if (nq++ == 0) load_tile<DP>(smem_u32(sv), &maps.v, kh, t.k0 + t.first, v_full);
-                    if (!(ok = wait(do_empty(ds), (uint32_t)(nd / KV_DO_STAGES + 1) & 1u))) break;
-                    load_tile<DP>(smem_u32(sd) + ds * TILE, &maps.dout, h, row, do_full(ds));
-                    ++nd;
+            int nq = 1, nd = 1, h = h0, n = 0;
+            for (int i = 1; i < steps; ++i) {
+                if (++n == tiles) {
+                    n = 0;
+                    ++h;
                 }
+                const int row = t.q0 + (tile0 + n) * ROWS, qs = nq % KV_Q_STAGES, ds = nd % KV_DO_STAGES;
+                if (!wait(q_empty(qs), (uint32_t)(nq / KV_Q_STAGES + 1) & 1u)) break;
+                load_tile<DP>(smem_u32(sq) + qs * TILE, &maps.q, h, row, q_full(qs));
+                ++nq;
+                if (!wait(do_empty(ds), (uint32_t)(nd / KV_DO_STAGES + 1) & 1u)) break;
+                load_tile<DP>(smem_u32(sd) + ds * TILE, &maps.dout, h, row, do_full(ds));
+                ++nd;
+            }
             // no copy is in flight when the CTA ends, after a give-up either
             wait.drain(k_full, 0);
-            if (nq) wait.drain(v_full, 0);
+            wait.drain(v_full, 0);
             for (int i = max(0, nq - KV_Q_STAGES); i < nq; ++i) wait.drain(q_full(i % KV_Q_STAGES), (uint32_t)(i / KV_Q_STAGES) & 1u);
             for (int i = max(0, nd - KV_DO_STAGES); i < nd; ++i) wait.drain(do_full(i % KV_DO_STAGES), (uint32_t)(i / KV_DO_STAGES) & 1u);
         }
@@ -447,11 +457,9 @@ k_tc_grad_kv(const __grid_constant__ GradMaps maps, const __grid_constant__ Grad
 }
 
 template <int DP>
-__global__ void __launch_bounds__(GR_THREADS, 1)
-k_tc_grad_q(const __grid_constant__ GradMaps maps, const __grid_constant__ GradArgs a) {
+__device__ __forceinline__ void grad_q(const GradMaps& maps, const GradArgs& a, unsigned char* smem) {
     constexpr int TILE = GradTile<DP>::TILE;
-    extern __shared__ unsigned char gr_smem_raw[];
-    unsigned char* const smem = align1024(gr_smem_raw);
+    const int index = (int)blockIdx.x - a.kv_items;
     unsigned char *const sq = smem, *const sd = sq + TILE, *const sk = sd + TILE, *const sv = sk + Q_K_STAGES * TILE;
     uint64_t* const bars = reinterpret_cast<uint64_t*>(sv + Q_V_STAGES * TILE);
     const uint32_t bar = smem_u32(bars);
@@ -467,23 +475,29 @@ k_tc_grad_q(const __grid_constant__ GradMaps maps, const __grid_constant__ GradA
     volatile int* const again = gave_up + 1;           // a sum was not finite
     const AttnArgs& g = a.g;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int h = blockIdx.x % g.heads, kh = h / g.group;
+    const int h = index % g.heads, kh = h / g.group;
 
     AttnTile t;
-    if (!attn_find_tile(g, blockIdx.x / g.heads, ROWS, false, t)) return;
+    if (!attn_find_tile(g, index / g.heads, ROWS, false, t)) return;
     const int rows = min(ROWS, t.nq - t.first);
     int lo, hi, unused;
     attn_keys_of(g, t, t.first, lo, unused);
     attn_keys_of(g, t, t.first + rows - 1, unused, hi);
     const int tile0 = lo / ROWS, steps = hi > lo ? (hi + ROWS - 1) / ROWS - tile0 : 0;
 
-    if (threadIdx.x == 0) {
+    if (warp == GR_COMPUTE && lane == 0) {
         for (uint32_t b : {q_full, do_full, s_full, s_full + 8, dp_full, done, done2}) mbar_init(b, 1);
         mbar_init(ds_ready, GR_COMPUTE);
         mbar_init(ds_ready + 8, GR_COMPUTE);
         for (int s = 0; s < RINGS; ++s) mbar_init(rings + 8u * s, 1);
         *gave_up = *again = 0;
         mbar_fence_init();
+        if (steps > 0) {                         // the first copies, while the CTA gets ready
+            load_tile<DP>(smem_u32(sq), &maps.q, h, t.q0 + t.first, q_full);
+            load_tile<DP>(smem_u32(sk), &maps.k, kh, t.k0 + tile0 * ROWS, k_full(0));
+            load_tile<DP>(smem_u32(sd), &maps.dout, h, t.q0 + t.first, do_full);
+            load_tile<DP>(smem_u32(sv), &maps.v, kh, t.k0 + tile0 * ROWS, v_full(0));
+        }
     }
     if (warp == 0) alloc_all(smem_u32(slot));
     before_sync();
@@ -495,19 +509,18 @@ k_tc_grad_q(const __grid_constant__ GradMaps maps, const __grid_constant__ GradA
 
     if (warp == GR_COMPUTE) {
         if (lane == 0 && steps > 0) {
-            load_tile<DP>(smem_u32(sq), &maps.q, h, t.q0 + t.first, q_full);
-            int nk = 0, nv = 0;
-            for (int n = 0; n < steps; ++n) {
+            int nk = 1, nv = 1;
+            for (int n = 1; n < steps; ++n) {
                 const int row = t.k0 + (tile0 + n) * ROWS, ks = nk % Q_K_STAGES, vs = nv % Q_V_STAGES;
                 if (!wait(k_empty(ks), (uint32_t)(nk / Q_K_STAGES + 1) & 1u)) break;
                 load_tile<DP>(smem_u32(sk) + ks * TILE, &maps.k, kh, row, k_full(ks));
-                if (nk++ == 0) load_tile<DP>(smem_u32(sd), &maps.dout, h, t.q0 + t.first, do_full);
+                ++nk;
                 if (!wait(v_empty(vs), (uint32_t)(nv / Q_V_STAGES + 1) & 1u)) break;
                 load_tile<DP>(smem_u32(sv) + vs * TILE, &maps.v, kh, row, v_full(vs));
                 ++nv;
             }
             wait.drain(q_full, 0);
-            if (nk) wait.drain(do_full, 0);
+            wait.drain(do_full, 0);
             for (int i = max(0, nk - Q_K_STAGES); i < nk; ++i) wait.drain(k_full(i % Q_K_STAGES), (uint32_t)(i / Q_K_STAGES) & 1u);
             for (int i = max(0, nv - Q_V_STAGES); i < nv; ++i) wait.drain(v_full(i % Q_V_STAGES), (uint32_t)(i / Q_V_STAGES) & 1u);
         }
@@ -619,6 +632,15 @@ k_tc_grad_q(const __grid_constant__ GradMaps maps, const __grid_constant__ GradA
     if (*again && !*gave_up && warp < SA_TPB / 32) again_q<DP>(a, reinterpret_cast<float*>(smem));
 }
 
+// One launch for both, keys first: the CTAs of queries fill the SMs that the last
+// ones of keys leave (two launches one after the other measured TWO_LAUNCHES).
+template <int DP>
+__global__ void __launch_bounds__(GR_THREADS, 1) k_tc_grad(const __grid_constant__ GradMaps maps, const __grid_constant__ GradArgs a) {
+    extern __shared__ unsigned char gr_smem_raw[];
+    if ((int)blockIdx.x < a.kv_items) grad_kv<DP>(maps, a, align1024(gr_smem_raw));
+    else grad_q<DP>(maps, a, align1024(gr_smem_raw));
+}
+
 // dk and dv: the parts' sums in order.  Eight columns a thread.
 template <bool VEC>
 __global__ void __launch_bounds__(256) k_grad_join(const __grid_constant__ GradArgs a) {
@@ -646,34 +668,44 @@ __global__ void __launch_bounds__(256) k_grad_join(const __grid_constant__ GradA
     }
 }
 
-template <typename K>
-int tc_launch(K kernel, long long grid, int smem, const GradMaps& m, const GradArgs& a, cudaStream_t s) {
-    if (grid > EXTENT_LIMIT) return ISO_ERR_UNSUPPORTED;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return ISO_ERR_CUDA;
-    TRAIN_LAUNCH((kernel<<<(unsigned)grid, GR_THREADS, smem, s>>>(m, a)));
-    return ISO_OK;
-}
-
 template <int DP>
-int launch_grad(const GradMaps& m, const GradArgs& a, cudaStream_t s) {
+int launch_grad(const GradMaps& m, GradArgs a, cudaStream_t s) {
+    constexpr int SMEM = std::max(GradTile<DP>::KV_SMEM, GradTile<DP>::Q_SMEM);
     const AttnArgs& g = a.g;
-    if (g.k_rows)
-        ISO_TRY(tc_launch(k_tc_grad_kv<DP>, attn_tiles(g.k_rows, g.n_seqs, ROWS) * (g.heads / g.group) * a.parts,
-                          GradTile<DP>::KV_SMEM, m, a, s));
-    if (g.q_rows)
-        ISO_TRY(tc_launch(k_tc_grad_q<DP>, attn_tiles(g.q_rows, g.n_seqs, ROWS) * g.heads, GradTile<DP>::Q_SMEM, m, a, s));
+    const long long kv = attn_tiles(g.k_rows, g.n_seqs, ROWS) * (g.heads / g.group) * a.parts;
+    const long long q = attn_tiles(g.q_rows, g.n_seqs, ROWS) * g.heads;
+    if (kv + q > EXTENT_LIMIT) return ISO_ERR_UNSUPPORTED;
+    a.kv_items = (int)kv;
+    if (cudaFuncSetAttribute(k_tc_grad<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) return ISO_ERR_CUDA;
+    TRAIN_LAUNCH((k_tc_grad<DP><<<(unsigned)(kv + q), GR_THREADS, SMEM, s>>>(m, a)));
     return ISO_OK;
 }
 
 }  // namespace
 
+// Parts by the estimated time of dk and dv, in steps (a pair of tiles) of an SM: the
+// longest CTA against the average, a CTA's start and end, and the parts' sums written
+// and read again.  From the sizes alone, a packed sequence taken as of average
+// length and the longest as twice that.  Measured, of 8192 tokens, PLAN_FIGURES
 AttnGradPlan attn_grad_plan(long long q_rows, long long k_rows, const iso_attn_cfg& c) {
-    (void)q_rows;
     const int group = c.heads / c.kv_heads;
-    const long long items = (k_rows + ROWS - 1) / ROWS * c.kv_heads;
+    const long long seqs = std::max(1, c.n_seqs), sms = train_sms();
+    const long long tiles = (k_rows + ROWS - 1) / ROWS;
+    const double of_seq = std::max(1.0, (double)q_rows / seqs / ROWS);                  // query tiles of a sequence
+    const double longest = seqs > 1 ? 2.0 * of_seq : of_seq;
+    const double total = (double)tiles * c.heads * (c.causal ? 0.5 * (of_seq + 1.0) : of_seq);
     AttnGradPlan p{1, 0};
-    while (p.parts < group && items * p.parts < 8LL * train_sms()) ++p.parts;
-    if (p.parts > 1) p.bytes = (size_t)p.parts * 2 * k_rows * c.kv_heads * c.head_dim * 4;
+    double best = 0.0;
+    for (int parts = 1; parts <= group; ++parts) {
+        const double item = longest * ((group + parts - 1) / parts), items = (double)tiles * c.kv_heads * parts;
+        const double steps = std::max(total / sms + GR_TAIL * item, item) + GR_ITEM_STEPS * std::ceil(items / sms);
+        const double join = parts == 1 ? 0.0 : GR_JOIN_STEPS + (double)k_rows * c.kv_heads * c.head_dim * 16.0 * parts / GR_STEP_BYTES;
+        if (parts == 1 || steps + join < best) {
+            best = steps + join;
+            p.parts = parts;
+        }
+    }
+    p.bytes = p.parts > 1 ? (size_t)p.parts * 2 * k_rows * c.kv_heads * c.head_dim * 4 : 0;
     return p;
 }
 
