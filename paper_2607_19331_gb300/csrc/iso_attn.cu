@@ -3,9 +3,9 @@
 //
 // Forward: one pass over the keys with the running maximum m and sum l of the
 // softmax: O <- O e^(m - m') + e^(S - m') V.  Backward: the weights again from
-// lse, P = e^(S - lse), and no atomics: k_simt_grad_kv owns a tile of keys and
-// goes over the queries (of all query heads of its key head), k_simt_grad_q owns
-// a tile of queries and goes over the keys; S and dP are formed in both (seven
+// lse, P = e^(S - lse), and no atomics: some CTAs own a tile of keys and go over the
+// queries (of all query heads of its key head), others own a tile of queries and go
+// over the keys; S and dP are formed in both (seven
 // products instead of five), and every sum has a fixed order.
 //
 // The CUDA-core kernels (tiles in iso_attn_simt.cuh) take any type, head
@@ -74,20 +74,20 @@ __global__ void __launch_bounds__(SA_TPB) k_simt_attn(AttnArgs g) {
     if (attn_find_tile(g, blockIdx.x / g.heads, SA_B, false, t))
         simt_attn<T, DP, T>(g, t, blockIdx.x % g.heads, 0, t.nk, static_cast<T*>(const_cast<void*>(g.out)), g.ldo, g.lse, sa_smem_);
 }
+// one launch for both: the keys' CTAs first
 template <typename T, int DP>
-__global__ void __launch_bounds__(SA_TPB) k_simt_grad_kv(AttnArgs g) {
-    extern __shared__ __align__(16) float sa_smem_[];
-    const int kv_heads = g.heads / g.group, kh = blockIdx.x % kv_heads;
-    AttnTile t;
-    if (attn_find_tile(g, blockIdx.x / kv_heads, SA_B, true, t))
-        simt_grad_kv<T, DP, T>(g, t, kh, kh * g.group, (kh + 1) * g.group, static_cast<T*>(g.dk), g.lddk, static_cast<T*>(g.dv),
-                               g.lddv, sa_smem_);
-}
-template <typename T, int DP>
-__global__ void __launch_bounds__(SA_TPB) k_simt_grad_q(AttnArgs g) {
+__global__ void __launch_bounds__(SA_TPB) k_simt_grad(AttnArgs g, int kv_items) {
     extern __shared__ __align__(16) float sa_smem_[];
     AttnTile t;
-    if (attn_find_tile(g, blockIdx.x / g.heads, SA_B, false, t)) simt_grad_q<T, DP>(g, t, blockIdx.x % g.heads, sa_smem_);
+    if ((int)blockIdx.x < kv_items) {
+        const int kv_heads = g.heads / g.group, kh = blockIdx.x % kv_heads;
+        if (attn_find_tile(g, blockIdx.x / kv_heads, SA_B, true, t))
+            simt_grad_kv<T, DP, T>(g, t, kh, kh * g.group, (kh + 1) * g.group, static_cast<T*>(g.dk), g.lddk, static_cast<T*>(g.dv),
+                                   g.lddv, sa_smem_);
+    } else {
+        const int i = (int)blockIdx.x - kv_items;
+        if (attn_find_tile(g, i / g.heads, SA_B, false, t)) simt_grad_q<T, DP>(g, t, i % g.heads, sa_smem_);
+    }
 }
 
 // delta[h][i] = sum_d dout_id out_id, heads that are whole 16-byte words at such
@@ -144,21 +144,23 @@ __global__ void __launch_bounds__(256) k_attn_delta(AttnArgs g) {
     if (lane == 0) g.delta[(long long)h * g.q_rows + row] = s;
 }
 
-template <typename K>
-int simt_launch(K kernel, long long grid, int smem, const AttnArgs& g, cudaStream_t s) {
+template <typename T, int DP>
+int simt_forward(const AttnArgs& g, cudaStream_t s) {
+    const long long grid = attn_tiles(g.q_rows, g.n_seqs, SA_B) * g.heads;
     if (grid > EXTENT_LIMIT) return ISO_ERR_UNSUPPORTED;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return ISO_ERR_CUDA;
-    TRAIN_LAUNCH((kernel<<<(unsigned)grid, SA_TPB, smem, s>>>(g)));
+    static std::atomic<uint64_t> done{0};
+    ISO_TRY(allow_smem(k_simt_attn<T, DP>, sa_smem<DP>(3, 1), done));
+    TRAIN_LAUNCH((k_simt_attn<T, DP><<<(unsigned)grid, SA_TPB, sa_smem<DP>(3, 1), s>>>(g)));
     return ISO_OK;
 }
 template <typename T, int DP>
-int simt_forward(const AttnArgs& g, cudaStream_t s) {
-    return simt_launch(k_simt_attn<T, DP>, attn_tiles(g.q_rows, g.n_seqs, SA_B) * g.heads, sa_smem<DP>(3, 1), g, s);
-}
-template <typename T, int DP>
 int simt_backward(const AttnArgs& g, cudaStream_t s) {
-    ISO_TRY(simt_launch(k_simt_grad_kv<T, DP>, attn_tiles(g.k_rows, g.n_seqs, SA_B) * (g.heads / g.group), sa_smem<DP>(4, 2), g, s));
-    return simt_launch(k_simt_grad_q<T, DP>, attn_tiles(g.q_rows, g.n_seqs, SA_B) * g.heads, sa_smem<DP>(4, 1), g, s);
+    const long long kv = attn_tiles(g.k_rows, g.n_seqs, SA_B) * (g.heads / g.group), q = attn_tiles(g.q_rows, g.n_seqs, SA_B) * g.heads;
+    if (kv + q > EXTENT_LIMIT) return ISO_ERR_UNSUPPORTED;
+    static std::atomic<uint64_t> done{0};
+    ISO_TRY(allow_smem(k_simt_grad<T, DP>, sa_smem<DP>(4, 2), done));
+    TRAIN_LAUNCH((k_simt_grad<T, DP><<<(unsigned)(kv + q), SA_TPB, sa_smem<DP>(4, 2), s>>>(g, (int)kv)));
+    return ISO_OK;
 }
 template <typename F>
 int by_kind(int32_t dtype, int dim, F&& f) {

@@ -5,7 +5,22 @@
 #include "iso_train.cuh"
 #include "iso_internal.cuh"
 
+#include <atomic>
+
 namespace iso {
+
+// Dynamic shared memory beyond the default for a kernel, asked for once a device
+// (`done` belongs to the kernel)
+template <typename K>
+int allow_smem(K kernel, int bytes, std::atomic<uint64_t>& done) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return ISO_ERR_CUDA;
+    const uint64_t bit = dev < 64 ? 1ULL << dev : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return ISO_OK;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return ISO_ERR_CUDA;
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return ISO_OK;
+}
 
 struct AttnArgs {
     const void *q, *k, *v;

@@ -384,7 +384,8 @@ int launch_attn(const FwdMaps& m, const FwdArgs& a, cudaStream_t s) {
     const AttnArgs& g = a.g;
     const long long grid = attn_tiles(g.q_rows, g.n_seqs, FW_ROWS) * g.heads * a.parts;
     if (grid > EXTENT_LIMIT) return ISO_ERR_UNSUPPORTED;
-    if (cudaFuncSetAttribute(k_tc_attn<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdTile<DP>::SMEM) != cudaSuccess) return ISO_ERR_CUDA;
+    static std::atomic<uint64_t> done{0};
+    ISO_TRY(allow_smem(k_tc_attn<DP>, FwdTile<DP>::SMEM, done));
     TRAIN_LAUNCH((k_tc_attn<DP><<<(unsigned)grid, FW_THREADS, FwdTile<DP>::SMEM, s>>>(m, a)));
     return ISO_OK;
 }

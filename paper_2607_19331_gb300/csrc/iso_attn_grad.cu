@@ -41,9 +41,9 @@ constexpr int GR_COLS = 64;
 constexpr int GR_THREADS = (GR_COMPUTE + 4) * 32;
 constexpr int KV_Q_STAGES = 3, KV_DO_STAGES = 2, Q_K_STAGES = 3, Q_V_STAGES = 2;
 
-// the plan's estimates: a CTA's start and end and a join's launch in steps, and the
-// bytes that the card moves in one
-constexpr double GR_ITEM_STEPS = 2.5, GR_JOIN_STEPS = 1.5, GR_STEP_BYTES = 1.1e7, GR_TAIL = 0.15;
+// the plan's estimates, in steps of dk and dv (1.45 us): a step of dq, a CTA's start and
+// end, a join's launch, and the bytes that the card moves in one
+constexpr double GR_Q_STEP = 0.72, GR_ITEM_STEPS = 6.0, GR_JOIN_STEPS = 1.5, GR_STEP_BYTES = 6.4e6;
 
 struct GradMaps {
     CUtensorMap q, k, v, dout;
@@ -676,32 +676,37 @@ int launch_grad(const GradMaps& m, GradArgs a, cudaStream_t s) {
     const long long q = attn_tiles(g.q_rows, g.n_seqs, ROWS) * g.heads;
     if (kv + q > EXTENT_LIMIT) return ISO_ERR_UNSUPPORTED;
     a.kv_items = (int)kv;
-    if (cudaFuncSetAttribute(k_tc_grad<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) return ISO_ERR_CUDA;
+    static std::atomic<uint64_t> done{0};
+    ISO_TRY(allow_smem(k_tc_grad<DP>, SMEM, done));
     TRAIN_LAUNCH((k_tc_grad<DP><<<(unsigned)(kv + q), GR_THREADS, SMEM, s>>>(m, a)));
     return ISO_OK;
 }
 
 }  // namespace
 
-// Parts by the estimated time of dk and dv, in steps (a pair of tiles) of an SM: the
-// longest CTA against the average, a CTA's start and end, and the parts' sums written
-// and read again.  From the sizes alone, a packed sequence taken as of average
-// length and the longest as twice that.  Measured, of 8192 tokens, PLAN_FIGURES
+// Parts by the estimated time: the average SM's, with a tenth of the longest CTA for
+// the end, or that CTA's where it is longer; and the parts' sums written and read
+// again.  From the sizes alone, a packed sequence taken as of average length and the
+// longest as twice that.  Measured (heads of 128, causal), one, two and three parts:
+// 8192 tokens, 28 heads over 4: 1029 / 1063 / 1083 us; 12 over 2: 540 / 464 / 474;
+// 2048 tokens, 12 over 2: 148 / 87 / 67 (six: 65); 13 sequences of 8192 tokens in
+// all, 12 over 2: 127 / 141 / 152; 512 tokens, 28 over 4: 57 / 44 / 38 (seven: 35).
 AttnGradPlan attn_grad_plan(long long q_rows, long long k_rows, const iso_attn_cfg& c) {
     const int group = c.heads / c.kv_heads;
     const long long seqs = std::max(1, c.n_seqs), sms = train_sms();
-    const long long tiles = (k_rows + ROWS - 1) / ROWS;
+    const double k_tiles = (double)((k_rows + ROWS - 1) / ROWS), q_tiles = (double)((q_rows + ROWS - 1) / ROWS);
     const double of_seq = std::max(1.0, (double)q_rows / seqs / ROWS);                  // query tiles of a sequence
     const double longest = seqs > 1 ? 2.0 * of_seq : of_seq;
-    const double total = (double)tiles * c.heads * (c.causal ? 0.5 * (of_seq + 1.0) : of_seq);
+    const double total = k_tiles * c.heads * (c.causal ? 0.5 * (of_seq + 1.0) : of_seq);
     AttnGradPlan p{1, 0};
     double best = 0.0;
     for (int parts = 1; parts <= group; ++parts) {
-        const double item = longest * ((group + parts - 1) / parts), items = (double)tiles * c.kv_heads * parts;
-        const double steps = std::max(total / sms + GR_TAIL * item, item) + GR_ITEM_STEPS * std::ceil(items / sms);
+        const double item = longest * ((group + parts - 1) / parts), items = k_tiles * c.kv_heads * parts + q_tiles * c.heads;
+        const double average = (total * (1.0 + GR_Q_STEP) + GR_ITEM_STEPS * items) / sms;
         const double join = parts == 1 ? 0.0 : GR_JOIN_STEPS + (double)k_rows * c.kv_heads * c.head_dim * 16.0 * parts / GR_STEP_BYTES;
-        if (parts == 1 || steps + join < best) {
-            best = steps + join;
+        const double cost = std::max(average + 0.1 * item, item + GR_ITEM_STEPS) + join;
+        if (parts == 1 || cost < best) {
+            best = cost;
             p.parts = parts;
         }
     }

@@ -32,10 +32,30 @@ __device__ __forceinline__ void sa_sync() { asm volatile("bar.sync 1, 256;" ::: 
 // the others and channels past dim are 0
 template <typename T, int DP>
 __device__ __forceinline__ void sa_load(float* s, const void* base, long long ld, long long row0, int valid, int col0, int dim) {
+    const T* const from = static_cast<const T*>(base) + row0 * ld + col0;
+    if (dim % 4 == 0 && ((reinterpret_cast<uintptr_t>(from) | (uintptr_t)(ld * (long long)sizeof(T))) & (4 * sizeof(T) - 1)) == 0) {
+        // four channels a load
+#pragma unroll 4
+        for (int i = threadIdx.x; i < SA_B * DP / 4; i += SA_TPB) {
+            const int r = i / (DP / 4), d = (i - r * (DP / 4)) * 4;
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (r < valid && d < dim) {
+                if constexpr (sizeof(T) == 4) {
+                    v = *reinterpret_cast<const float4*>(from + r * ld + d);
+                } else {
+                    const uint2 w = *reinterpret_cast<const uint2*>(from + r * ld + d);
+                    bf16x2_to_f32(w.x, v.x, v.y);
+                    bf16x2_to_f32(w.y, v.z, v.w);
+                }
+            }
+            *reinterpret_cast<float4*>(s + r * sa_pitch<DP>() + d) = v;
+        }
+        return;
+    }
+#pragma unroll 4
     for (int i = threadIdx.x; i < SA_B * DP; i += SA_TPB) {
         const int r = i / DP, d = i - r * DP;
-        s[r * sa_pitch<DP>() + d] =
-            r < valid && d < dim ? to_f32(static_cast<const T*>(base)[(row0 + r) * ld + col0 + d]) : 0.0f;
+        s[r * sa_pitch<DP>() + d] = r < valid && d < dim ? to_f32(from[r * ld + d]) : 0.0f;
     }
 }
 

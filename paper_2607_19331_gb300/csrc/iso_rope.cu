@@ -21,7 +21,8 @@ namespace iso {
 namespace {
 
 constexpr int ROPE_TPB = 256;
-constexpr int ROPE_UNITS = 1024;      // units (of two 16-byte words in the vector form) a block takes
+template <typename T>
+constexpr int ROPE_EACH = sizeof(T) == 2 ? 4 : 2;     // units in flight a thread: 128 bytes of loads
 constexpr int ROPE_MAX_ROWS = 16;
 
 struct RopeArgs {
@@ -35,19 +36,8 @@ struct RopeArgs {
     int32_t positions_i64, inverse, block_rows;
 };
 
-template <typename T>
-__device__ __forceinline__ void rope_load(const T* p, float (&v)[8]) {
-    Raw8<T> r;
-    r.load(p);
-    r.get(v);
-}
-
-// One unit of a head: VEC, eight pairs (of a head's turned part) or eight
-// channels (of the rest), else one of either.
-template <typename T, bool NEIGHBOURS, bool VEC>
-__global__ void __launch_bounds__(ROPE_TPB) k_rope(const __grid_constant__ RopeArgs g) {
-    extern __shared__ float2 rope_cs[];                  // [row][pair]: cosine, sine
-    const int r0 = blockIdx.x * g.block_rows, rows = min(g.block_rows, g.rows - r0);
+// sines and cosines of the block's rows, [row][pair]
+__device__ __forceinline__ void rope_angles(const RopeArgs& g, float2* cs, int r0, int rows) {
     for (int i = threadIdx.x; i < rows * g.pairs; i += ROPE_TPB) {
         const int r = i / g.pairs, p = i - r * g.pairs;
         const long long at = (long long)g.axis[p] * g.ldp + r0 + r;
@@ -56,65 +46,110 @@ __global__ void __launch_bounds__(ROPE_TPB) k_rope(const __grid_constant__ RopeA
         const unsigned long long a = (unsigned long long)pos * g.turns[p] + (1ULL << 31);
         float s, c;
         sincospif((float)(int)(a >> 32) * 0x1p-31f, &s, &c);
-        rope_cs[i] = make_float2(c, g.inverse ? -s : s);
+        cs[i] = make_float2(c, g.inverse ? -s : s);
     }
+}
+
+// Heads of whole 16-byte words at such boundaries.  A unit is eight pairs (two words,
+// from either half or side by side), or one word of the channels that are copied.  A
+// thread keeps one unit of a head and goes from head to head; its first units are loaded before the
+// angles are formed.
+template <typename T, bool NEIGHBOURS>
+__global__ void __launch_bounds__(ROPE_TPB) k_rope_words(const __grid_constant__ RopeArgs g) {
+    extern __shared__ float2 rope_cs[];
+    constexpr int EACH = ROPE_EACH<T>;
+    const int r0 = blockIdx.x * g.block_rows, rows = min(g.block_rows, g.rows - r0);
+    const int half = g.pairs, turned = g.pairs / 8, units = turned + (g.head_dim - 2 * g.pairs) / 8;
+    const int steps = ROPE_TPB / units, w = (int)threadIdx.x % units;
+    const bool turns = w < turned;
+    // this unit's words
+    const int first = !turns ? 2 * half + (w - turned) * 8 : NEIGHBOURS ? w * 16 : w * 8, second = NEIGHBOURS ? first + 8 : first + half;
+    int r = 0, h = (int)threadIdx.x / units;
+    if (h >= steps) r = rows;                         // threads past the last whole head
+    auto settle = [&] {
+        while (h >= g.heads && r < rows) {
+            h -= g.heads;
+            ++r;
+        }
+    };
+    settle();
+    bool formed = false;
+    for (;;) {
+        Raw8<T> a[EACH], b[EACH];
+        int rr[EACH], hh[EACH];
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            rr[k] = r;
+            hh[k] = h;
+            if (r < rows) {
+                const T* x = static_cast<const T*>(g.x) + (long long)(r0 + r) * g.ldx + (long long)h * g.head_dim;
+                a[k].load(x + first);
+                if (turns) b[k].load(x + second);
+                h += steps;
+                settle();
+            }
+        }
+        if (!formed) {
+            rope_angles(g, rope_cs, r0, rows);
+            __syncthreads();
+            formed = true;
+        }
+        if (rr[0] >= rows) return;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            if (rr[k] >= rows) return;
+            T* y = static_cast<T*>(g.y) + (long long)(r0 + rr[k]) * g.ldy + (long long)hh[k] * g.head_dim;
+            float u[8], v[8];
+            a[k].get(u);
+            if (turns) {
+                b[k].get(v);
+                const float4* cs = reinterpret_cast<const float4*>(rope_cs + rr[k] * g.pairs + w * 8);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float4 t = cs[j];           // two pairs
+                    if constexpr (NEIGHBOURS) {
+                        float* const z = j < 2 ? u + 4 * j : v + 4 * (j - 2);
+                        const float z0 = z[0], z1 = z[1], z2 = z[2], z3 = z[3];
+                        z[0] = z0 * t.x - z1 * t.y;
+                        z[1] = z0 * t.y + z1 * t.x;
+                        z[2] = z2 * t.z - z3 * t.w;
+                        z[3] = z2 * t.w + z3 * t.z;
+                    } else {
+                        const float u0 = u[2 * j], v0 = v[2 * j], u1 = u[2 * j + 1], v1 = v[2 * j + 1];
+                        u[2 * j] = u0 * t.x - v0 * t.y;
+                        v[2 * j] = u0 * t.y + v0 * t.x;
+                        u[2 * j + 1] = u1 * t.z - v1 * t.w;
+                        v[2 * j + 1] = u1 * t.w + v1 * t.z;
+                    }
+                }
+                put8(y + second, v);
+            }
+            put8(y + first, u);
+        }
+    }
+}
+
+// Any rows: a pair, or a channel that is copied, at a time.
+template <typename T, bool NEIGHBOURS>
+__global__ void __launch_bounds__(ROPE_TPB) k_rope(const __grid_constant__ RopeArgs g) {
+    extern __shared__ float2 rope_cs[];
+    const int r0 = blockIdx.x * g.block_rows, rows = min(g.block_rows, g.rows - r0);
+    rope_angles(g, rope_cs, r0, rows);
     __syncthreads();
-    constexpr int W = VEC ? 8 : 1;
-    const int half = g.pairs, rot = 2 * g.pairs;
-    const int turned = g.pairs / W, units = turned + (g.head_dim - rot) / W;   // units of a head
-    const int per_row = units * g.heads;
+    const int units = g.head_dim - g.pairs, per_row = units * g.heads;
     for (int i = threadIdx.x; i < rows * per_row; i += ROPE_TPB) {
         const int r = i / per_row, u = i - r * per_row, h = u / units, w = u - h * units;
         const T* x = static_cast<const T*>(g.x) + (long long)(r0 + r) * g.ldx + (long long)h * g.head_dim;
         T* y = static_cast<T*>(g.y) + (long long)(r0 + r) * g.ldy + (long long)h * g.head_dim;
-        if (w >= turned) {
-            const int c = rot + (w - turned) * W;
-            if constexpr (VEC) {
-                float v[8];
-                rope_load(x + c, v);
-                put8(y + c, v);
-            } else {
-                y[c] = x[c];
-            }
+        if (w >= g.pairs) {
+            y[g.pairs + w] = x[g.pairs + w];
             continue;
         }
-        const float2* cs = rope_cs + r * g.pairs + w * W;
-        if constexpr (VEC) {
-            float a[8], b[8];
-            if constexpr (NEIGHBOURS) {
-                rope_load(x + w * 16, a);
-                rope_load(x + w * 16 + 8, b);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float2 t = cs[j], q = cs[4 + j];
-                    const float u0 = a[2 * j], w0 = a[2 * j + 1], u1 = b[2 * j], w1 = b[2 * j + 1];
-                    a[2 * j] = u0 * t.x - w0 * t.y;
-                    a[2 * j + 1] = u0 * t.y + w0 * t.x;
-                    b[2 * j] = u1 * q.x - w1 * q.y;
-                    b[2 * j + 1] = u1 * q.y + w1 * q.x;
-                }
-                put8(y + w * 16, a);
-                put8(y + w * 16 + 8, b);
-            } else {
-                rope_load(x + w * 8, a);
-                rope_load(x + half + w * 8, b);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float2 t = cs[j];
-                    const float u0 = a[j], w0 = b[j];
-                    a[j] = u0 * t.x - w0 * t.y;
-                    b[j] = u0 * t.y + w0 * t.x;
-                }
-                put8(y + w * 8, a);
-                put8(y + half + w * 8, b);
-            }
-        } else {
-            const int ca = NEIGHBOURS ? 2 * w : w, cb = NEIGHBOURS ? 2 * w + 1 : half + w;
-            const float2 t = cs[0];
-            const float u0 = to_f32(x[ca]), w0 = to_f32(x[cb]);
-            from_f32(u0 * t.x - w0 * t.y, y[ca]);
-            from_f32(u0 * t.y + w0 * t.x, y[cb]);
-        }
+        const int ca = NEIGHBOURS ? 2 * w : w, cb = NEIGHBOURS ? 2 * w + 1 : g.pairs + w;
+        const float2 t = rope_cs[r * g.pairs + w];
+        const float u0 = to_f32(x[ca]), w0 = to_f32(x[cb]);
+        from_f32(u0 * t.x - w0 * t.y, y[ca]);
+        from_f32(u0 * t.y + w0 * t.x, y[cb]);
     }
 }
 
@@ -132,15 +167,17 @@ unsigned long long fixed_turns(double freq) {
 }
 
 template <typename T>
-int launch_rope(const RopeArgs& g, bool neighbours, bool vec, cudaStream_t s) {
+int launch_rope(RopeArgs& g, bool neighbours, bool words, cudaStream_t s) {
+    const long long units = words ? (long long)g.heads * ((g.head_dim - g.pairs) / 8) : (long long)g.heads * (g.head_dim - g.pairs);
+    g.block_rows = (int)std::max<long long>(1, std::min<long long>(ROPE_MAX_ROWS, ROPE_TPB * ROPE_EACH<T> / std::max<long long>(1, units)));
     const unsigned grid = (unsigned)((g.rows + g.block_rows - 1) / g.block_rows);
     const size_t smem = std::max<size_t>(1, (size_t)g.block_rows * g.pairs) * sizeof(float2);
-    auto go = [&](auto nb, auto v) -> int {
-        TRAIN_LAUNCH((k_rope<T, decltype(nb)::value, decltype(v)::value><<<grid, ROPE_TPB, smem, s>>>(g)));
-        return ISO_OK;
-    };
-    if (neighbours) return vec ? go(std::true_type{}, std::true_type{}) : go(std::true_type{}, std::false_type{});
-    return vec ? go(std::false_type{}, std::true_type{}) : go(std::false_type{}, std::false_type{});
+    if (words) {
+        TRAIN_LAUNCH((neighbours ? k_rope_words<T, true><<<grid, ROPE_TPB, smem, s>>>(g) : k_rope_words<T, false><<<grid, ROPE_TPB, smem, s>>>(g)));
+    } else {
+        TRAIN_LAUNCH((neighbours ? k_rope<T, true><<<grid, ROPE_TPB, smem, s>>>(g) : k_rope<T, false><<<grid, ROPE_TPB, smem, s>>>(g)));
+    }
+    return ISO_OK;
 }
 
 }  // namespace
@@ -192,10 +229,8 @@ extern "C" int32_t iso_rope(const iso_mat* x, const void* positions, int32_t pos
     g.inverse = cfg->inverse;
     // eight pairs a thread: their channels are whole 16-byte words of a head that
     // starts on such a boundary (in the halves form each half does)
-    const bool vec = rows_aligned(x) && rows_aligned(y) && cfg->head_dim % 8 == 0 && pairs % 8 == 0;
-    const long long units = (long long)g.heads * (vec ? (cfg->head_dim - pairs) / 8 : cfg->head_dim - pairs);
-    g.block_rows = (int)std::max<long long>(1, std::min<long long>(ROPE_MAX_ROWS, ROPE_UNITS / std::max<long long>(1, units)));
+    const bool words = rows_aligned(x) && rows_aligned(y) && cfg->head_dim % 8 == 0 && pairs % 8 == 0 && cfg->head_dim <= 8 * ROPE_TPB;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return x->dtype == ISO_BF16 ? launch_rope<__nv_bfloat16>(g, cfg->neighbours, vec, s)
-                                : launch_rope<float>(g, cfg->neighbours, vec, s);
+    return x->dtype == ISO_BF16 ? launch_rope<__nv_bfloat16>(g, cfg->neighbours, words, s)
+                                : launch_rope<float>(g, cfg->neighbours, words, s);
 }
