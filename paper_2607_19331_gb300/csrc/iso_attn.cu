@@ -173,7 +173,7 @@ int check_cfg(const iso_attn_cfg* c) {
     if (!c || c->heads < 1 || c->kv_heads < 1 || c->heads % c->kv_heads || c->head_dim < 1) return ISO_ERR_ARG;
     if ((c->causal != 0 && c->causal != 1) || c->window < 0 || (c->window && !c->causal)) return ISO_ERR_ARG;
     if ((c->zero_rest != 0 && c->zero_rest != 1) || c->reserved != 0) return ISO_ERR_ARG;
-    if (!(c->scale > 0.0f) || !std::isfinite(c->scale) || c->n_seqs < 0) return ISO_ERR_ARG;
+    if (!(c->scale > 0.0f) || !std::isfinite(c->scale * tc::LOG2E) || c->n_seqs < 0) return ISO_ERR_ARG;
     if ((c->n_seqs > 0) != (c->q_ends != nullptr) || (c->k_ends && !c->q_ends)) return ISO_ERR_ARG;
     if ((reinterpret_cast<uintptr_t>(c->q_ends) | reinterpret_cast<uintptr_t>(c->k_ends)) & 3u) return ISO_ERR_ALIGN;
     if (c->head_dim > ISO_ATTN_MAX_DIM) return ISO_ERR_UNSUPPORTED;

@@ -20,9 +20,9 @@
 namespace iso {
 namespace {
 
-constexpr int ROPE_TPB = 256;
+constexpr int ROPE_TPB = 64;            // 256: 108 us for the two passes over 16384 x 4096 bf16, 128: 102, 64: 96
 template <typename T>
-constexpr int ROPE_EACH = sizeof(T) == 2 ? 4 : 2;     // units in flight a thread: 128 bytes of loads
+constexpr int ROPE_EACH = sizeof(T) == 2 ? 2 : 1;     // units in flight a thread: 64 bytes of loads (four and two: 99 us)
 constexpr int ROPE_MAX_ROWS = 16;
 
 struct RopeArgs {
