@@ -665,7 +665,9 @@ int64_t iso_attn_wait_ns(int64_t ns);
  * gradient; one with a NaN or +Inf has NaN for all three.  loss and lse have a
  * float per row.  Statistics and the gradient are binary32, the gradient rounded
  * once to dlogits' type (that of the logits).  dlogits may be the logits
- * themselves (same data and stride); else it overlaps no input. */
+ * themselves (same data and stride); else it overlaps no input.  status (device,
+ * may be NULL): ISO_OK, ISO_ERR_INDEX or ISO_ERR_TIMEOUT (rows that a give-up left
+ * unfinished are NaN). */
 #define ISO_DISTILL_MAX_TOP 2048
 
 /* loss and lse; with dlogits (then dloss is needed too, a float per row) also the gradient, the

@@ -91,8 +91,8 @@ __global__ void __launch_bounds__(SA_TPB) k_simt_grad(AttnArgs g, int kv_items) 
 }
 
 // delta[h][i] = sum_d dout_id out_id, heads that are whole 16-byte words at such
-// boundaries: a word of both a lane, 16 lanes a row and head, DELTA_EACH of them in flight (one
-// lane a channel measured DELTA_SLOW)
+// boundaries: a word of both a lane, 16 lanes a row and head, DELTA_EACH of them in
+// flight (8269 rows of 12 heads: 13.4 us, a lane a channel 18.4)
 constexpr int DELTA_EACH = 4;
 __global__ void __launch_bounds__(256) k_attn_delta_words(AttnArgs g) {
     const long long n = (long long)g.q_rows * g.heads, group = ((long long)blockIdx.x * blockDim.x + threadIdx.x) >> 4;

@@ -13,6 +13,7 @@
 //                   teacher's side beside the loads: its softmax, the logits at
 //                   its ids, the loss, and after the row the entries at the ids, each
 //                   by the CTA that owns its column.
+//   k_distill_stream  the same for many long rows, by clusters that stay.
 //   k_distill_long  rows that do not fit, or whose logits and gradient do not
 //                   sit alike in 16-byte words: one CTA a row, two passes.
 // A row off a 16-byte boundary is taken as its words from the first boundary on;
@@ -22,10 +23,12 @@
 // the largest m_i, in a fixed order.  In the exponents m / tau is a level, rounded
 // once, that lse takes back: exp(x / tau - level) then has one rounding, of a
 // number that is small where the weight is not.
+#include "iso_tc.cuh"
 #include "iso_train.cuh"
 #include "iso_internal.cuh"
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 namespace iso {
@@ -34,7 +37,12 @@ namespace {
 constexpr int DI_MAX_CLUSTER = 8;
 constexpr int DI_MAX_WORDS = 10;         // 16-byte words of a row a thread holds
 constexpr int DI_WARP_TOP = 128;         // up to this many slots the teacher's warp adds up equal ids alone
-constexpr float LOG2E = 1.4426950408889634f;
+using tc::LOG2E;
+using tc::pair_of;
+using tc::parts_of;
+using tc::fma2;
+using tc::add2;
+using tc::mul2;
 
 struct DistillArgs {
     const void* z;
@@ -49,6 +57,7 @@ struct DistillArgs {
     long long ldz, ldt, ldg;
     int32_t rows, vocab, top;
     int32_t ids_i64, teacher_f32, cluster;
+    int32_t stages, share;               // k_distill_stream: rows in flight, words of a row a CTA has room for
     float tau, inv_tau;
 };
 
@@ -76,29 +85,6 @@ struct Exp {
     }
     __device__ __forceinline__ float at(float x, float level) const { return of(fmaf(x, c, -level)); }
 };
-
-// two at a time
-__device__ __forceinline__ uint64_t pair_of(float a, float b) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ void parts_of(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 
 // m: the largest entry (-Inf: none); s: the sum of exp(x / tau - level(m))
 struct Stat {
@@ -441,6 +427,261 @@ __global__ void __launch_bounds__(NT + 32, NT == 512 ? 2 : NT == 256 ? 4 : 6) k_
     }
 }
 
+// Many long rows: the cluster stays and goes from row to row (by the number of
+// clusters), its words of the next rows on their way into shared memory by bulk
+// copies meanwhile, so that no load waits for a row's exchanges, nor a row for a
+// launch.  A row: its words summed up, the cluster's exchange of sums, its words again for
+// the gradient.  Four warps take the teacher's side of every fourth row each, a
+// chain of loads that is as long as two rows.  Bound by HBM where a row fits one
+// CTA, and for the gradient alone (6.5 TB/s); with larger clusters by the exchange, whose
+// latency no other row of the cluster covers.
+// Measured against k_distill, loss with gradient / loss / gradient alone, us:
+//   4096 x 152064 bf16 (clusters of 4)   521 / 360 / 378   against 566 / 317 / 437
+//   4096 x 76032 bf16 (2)                254 / 175 / 198   against 287 / 159 / 227
+//   4096 x 50000 f32 (2)                 316 / 198 / 267   against 494 / 312 / 342
+//   4096 x 50000 bf16 (1)                136 /  78 / 141   against 236 / 150 / 173
+//   8192 x 32000 bf16 (1)                179 / 117 / 182   against 273 / 162 / 241
+//   8192 x 20000 bf16 (1)                145 / 102 / 129   against 143 /  75 / 145
+//   8192 x 12000 bf16 (1)                117 /  90 /  99   against 110 /  63 / 108
+//   1024 x 50000 bf16 (1)                 42 /  25 /  41   against  59 /  41 /  46
+//   600 x 152064 bf16 (4)                 88 /  62 /  67   against  83 /  52 /  64
+//   1024 x 76032 f32 (4)                 148 / 100 / 109   against 136 /  91 / 105
+// so it takes rows of DS_MIN_WORDS that fit one CTA, DS_ROUNDS rows for each, and rows of
+// larger clusters for a gradient, DS_ROUNDS_CLUSTER for each.  (The words kept in
+// registers from the first pass on, with 20 a thread: 589 us for the first case.)
+constexpr int DS_NT = 256, DS_TEACHERS = 4, DS_MAX_STAGES = 4, DS_SMEM = 200 * 1024;
+constexpr int DS_MIN_WORDS = 3000, DS_ROUNDS = 4, DS_ROUNDS_CLUSTER = 32;
+__device__ __forceinline__ bool probe_cluster(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+template <typename T>
+__global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(const __grid_constant__ DistillArgs g) {
+    constexpr int NT = DS_NT, N = Word<T>::N, WARPS = NT / 32;
+    constexpr bool FAST = sizeof(T) == 2;
+    extern __shared__ __align__(128) unsigned char ds_smem[];
+    __shared__ Stat parts[WARPS], of_cta[2][DI_MAX_CLUSTER], of_row[DS_TEACHERS];
+    __shared__ __align__(8) uint64_t full[DS_MAX_STAGES], exchanged[2], prepared[DS_TEACHERS], written[DS_TEACHERS];
+    __shared__ volatile int any_s[DS_TEACHERS];
+    __shared__ volatile int gave_up;
+    const int C = g.cluster, rank = (int)(blockIdx.x % C), clusters = (int)(gridDim.x / C), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const size_t stage_bytes = (size_t)g.share * 16;
+    float* const tops = reinterpret_cast<float*>(ds_smem + g.stages * stage_bytes);
+    const Exp<FAST> ex(g.inv_tau);
+    const tc::Waits wait = {2000000000u, &gave_up};
+
+    // this CTA's part of a row, as in k_distill
+    struct Part {
+        const T* z;
+        int before, w0, w1, behind, c0, c1;
+    };
+    auto part_of = [&](int row) {
+        Part p;
+        p.z = static_cast<const T*>(g.z) + (long long)row * g.ldz;
+        p.before = entries_before(p.z, g.vocab);
+        const int words = (g.vocab - p.before) / N, share = (words + C - 1) / C;
+        p.w0 = min(words, rank * share);
+        p.w1 = min(words, p.w0 + share);
+        p.behind = p.before + words * N;
+        p.c0 = rank == 0 ? 0 : p.before + p.w0 * N;
+        p.c1 = rank == C - 1 ? g.vocab : p.before + p.w1 * N;
+        return p;
+    };
+    int issued = 0;                              // copies: the i-th into stage i mod stages
+    auto copy = [&](int row, int stage) {        // by one thread
+        if (row >= g.rows || gave_up) return;
+        ++issued;
+        const Part p = part_of(row);
+        const uint32_t bar = smem_u32(&full[stage]), bytes = (uint32_t)(p.w1 - p.w0) * 16u;
+        if (bytes == 0) {
+            mbar_arrive(bar);
+            return;
+        }
+        mbar_arrive_tx(bar, bytes);
+        bulk_g2s(smem_u32(ds_smem + stage * stage_bytes), p.z + p.before + (long long)p.w0 * N, bytes, bar);
+    };
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < g.stages; ++i) mbar_init(smem_u32(&full[i]), 1);
+        for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&exchanged[i]), (uint32_t)C);
+        for (int i = 0; i < DS_TEACHERS; ++i) {
+            mbar_init(smem_u32(&prepared[i]), 1);
+            mbar_init(smem_u32(&written[i]), WARPS);
+        }
+        gave_up = 0;
+        mbar_fence_init();
+    }
+    __syncthreads();
+    if (C > 1) {
+        cluster_arrive();
+        cluster_wait();                          // every CTA of the cluster runs, its barriers are there
+    }
+    const int row0 = (int)(blockIdx.x / C);
+    if (warp < WARPS) {
+        if (threadIdx.x == 0)
+            for (int i = 0; i < g.stages; ++i) copy(row0 + i * clusters, i);
+        int stage = 0, it = 0;
+        uint32_t parity = 0;
+        for (int row = row0; row < g.rows; row += clusters, ++it) {
+            const int slot = it % DS_TEACHERS, b = it & 1;
+            const Part p = part_of(row);
+            T* const grad = g.grad ? static_cast<T*>(g.grad) + (long long)row * g.ldg : nullptr;
+            const float dloss = grad ? g.dloss[row] : 0.0f;
+            float level = g.lse_in ? ex.level_of(g.lse_in[row]) : 0.0f, inv_s = 1.0f;
+            const uint4* const words = reinterpret_cast<const uint4*>(ds_smem + stage * stage_bytes);
+            const int n = p.w1 - p.w0;
+            int single = -1;
+            if (rank == 0 && (int)threadIdx.x < p.before) single = threadIdx.x;
+            const int back = NT - 1 - (int)threadIdx.x;
+            if (rank == C - 1 && p.behind + back < g.vocab) single = p.behind + back;
+            const float xs = single >= 0 ? to_f32(p.z[single]) : -INFINITY;
+            bool whole = wait.warp(smem_u32(&full[stage]), parity);
+            if (!g.lse_in) {
+                Stat a = {xs, 0.0f};
+#pragma unroll 4
+                for (int i = threadIdx.x; i < n; i += NT) {
+                    Word<T> x;
+                    x.w = words[i];
+                    a.m = fmaxf(a.m, x.top());
+                }
+                if (a.m != a.m) a.m = -INFINITY;
+#pragma unroll
+                for (int o = 16; o; o >>= 1) a.m = fmaxf(a.m, __shfl_xor_sync(0xFFFFFFFFu, a.m, o));
+                level = ex.level(a.m);
+                const uint64_t cc = pair_of(ex.c, ex.c), ll = pair_of(-level, -level);
+                uint64_t sum = pair_of(0.0f, 0.0f);
+#pragma unroll 4
+                for (int i = threadIdx.x; i < n; i += NT) {
+                    Word<T> x;
+                    x.w = words[i];
+                    uint64_t v[N / 2];
+                    x.get(v);
+#pragma unroll
+                    for (int j = 0; j < N / 2; ++j) {
+                        float s0, s1;
+                        parts_of(fma2(v[j], cc, ll), s0, s1);
+                        sum = add2(sum, pair_of(ex.of(s0), ex.of(s1)));
+                    }
+                }
+                float s0, s1;
+                parts_of(sum, s0, s1);
+                a.s = warp_sum(s0 + s1 + (single >= 0 ? ex.at(xs, level) : 0.0f));
+                if (lane == 0) parts[warp] = a;
+                sync_some<NT>(1);
+                a = {-INFINITY, 0.0f};
+                if (lane < WARPS) a = parts[lane];
+                a = join_lanes(a, WARPS, ex);
+                a.m = __shfl_sync(0xFFFFFFFFu, a.m, 0);
+                a.s = __shfl_sync(0xFFFFFFFFu, a.s, 0);
+                if (C > 1) {
+                    if (warp == 0) {
+                        // this CTA's teacher's side has read the logits at its ids
+                        whole = wait.warp(smem_u32(&prepared[slot]), (uint32_t)(it / DS_TEACHERS) & 1u) && whole;
+                        if (lane < C) {
+                            uint32_t to, at;
+                            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_u32(&of_cta[b][rank])), "r"(lane));
+                            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(&exchanged[b])), "r"(lane));
+                            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" :: "r"(to), "f"(a.m), "f"(a.s) : "memory");
+                            asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(at) : "memory");
+                        }
+                        __syncwarp();
+                    }
+                    const uint32_t ph = (uint32_t)(it >> 1) & 1u;
+                    if (!__all_sync(0xFFFFFFFFu, probe_cluster(smem_u32(&exchanged[b]), ph)))
+                        whole = wait.warp(smem_u32(&exchanged[b]), ph) && probe_cluster(smem_u32(&exchanged[b]), ph) && whole;
+                    a = {-INFINITY, 0.0f};
+                    if (lane < C) a = of_cta[b][lane];
+                    a = join_lanes(a, DI_MAX_CLUSTER, ex);
+                    a.m = __shfl_sync(0xFFFFFFFFu, a.m, 0);
+                    a.s = __shfl_sync(0xFFFFFFFFu, a.s, 0);
+                }
+                if (!whole) a.s = __int_as_float(0x7FFFFFFF);
+                level = ex.level(a.m);
+                inv_s = 1.0f / a.s;
+                if (threadIdx.x == 0) of_row[slot] = a;
+            }
+            whole = wait.warp(smem_u32(&prepared[slot]), (uint32_t)(it / DS_TEACHERS) & 1u) && whole;
+            if (!whole) level = __int_as_float(0x7FFFFFFF);
+            if (grad) {
+                const bool any = !whole || any_s[slot];
+                const float by = dloss * g.tau * inv_s;
+                const uint64_t cc = pair_of(ex.c, ex.c), ll = pair_of(-level, -level), bb = pair_of(by, by);
+                uint4* const out = reinterpret_cast<uint4*>(grad + p.before) + p.w0;
+#pragma unroll 4
+                for (int i = threadIdx.x; i < n; i += NT) {
+                    Word<T> x;
+                    x.w = words[i];
+                    uint64_t v[N / 2];
+                    x.get(v);
+#pragma unroll
+                    for (int j = 0; j < N / 2; ++j) {
+                        float s0, s1;
+                        parts_of(fma2(v[j], cc, ll), s0, s1);
+                        v[j] = mul2(pair_of(ex.of(s0), ex.of(s1)), bb);
+                    }
+                    x.set(v);
+                    if (!any) x.w = make_uint4(0u, 0u, 0u, 0u);
+                    __stcs(out + i, x.w);
+                }
+                if (single >= 0) from_f32(any ? by * ex.at(xs, level) : 0.0f, grad[single]);
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&written[slot]));
+            sync_some<NT>(1);                    // the row's place may be filled again
+            if (threadIdx.x == 0) copy(row + g.stages * clusters, stage);
+            if (++stage == g.stages) {
+                stage = 0;
+                parity ^= 1u;
+            }
+        }
+        if (threadIdx.x == 0) {
+            // no copy is in flight when the CTA ends, after a give-up either
+            for (int i = max(0, issued - g.stages); i < issued; ++i)
+                wait.drain(smem_u32(&full[i % g.stages]), (uint32_t)(i / g.stages) & 1u);
+        }
+    } else {
+        const int slot = warp - WARPS;
+        const Top t = top_of(tops + slot * 4 * g.top, g.top);
+        uint32_t ph = 0;
+        for (int row = row0 + slot * clusters; row < g.rows; row += DS_TEACHERS * clusters, ph ^= 1u) {
+            const Part p = part_of(row);
+            bool any = false;
+            const bool all = rank == 0 && !g.lse_in;
+            if (g.grad || rank == 0) any = teacher_side(g, row, p.z, t, all ? 0 : p.c0, all ? g.vocab : p.c1);
+            if (lane == 0) any_s[slot] = any;
+            tc::arrive_warp(smem_u32(&prepared[slot]));
+            const float dloss = g.grad ? g.dloss[row] : 0.0f;
+            float level = g.lse_in ? ex.level_of(g.lse_in[row]) : 0.0f, by = dloss * g.tau;
+            const bool whole = wait.warp(smem_u32(&written[slot]), ph);
+            if (!g.lse_in) {
+                const Stat a = of_row[slot];
+                level = ex.level(a.m);
+                by = dloss * g.tau / a.s;
+                if (rank == 0) {
+                    const float lse = !whole ? __int_as_float(0x7FFFFFFF) : a.m == -INFINITY && a.s == 0.0f ? -INFINITY : ex.lse(level, a.s);
+                    const float d = any ? divergence(g, t, lse) : 0.0f;
+                    if (lane == 0) {
+                        g.loss[row] = any ? g.tau * g.tau * d : 0.0f;
+                        g.lse[row] = lse;
+                    }
+                }
+            }
+            if (g.grad && any && whole)
+                for (int k = lane; k < g.top; k += 32)
+                    if (t.id[k] >= p.c0 && t.id[k] < p.c1)
+                        from_f32(by * ex.at(t.z[k], level) - dloss * g.tau * t.mass[k], static_cast<T*>(g.grad)[(long long)row * g.ldg + t.id[k]]);
+            __syncwarp();
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0 && gave_up && g.status) atomicCAS(g.status, 0, (int32_t)ISO_ERR_TIMEOUT);
+    if (C > 1) {
+        cluster_arrive();
+        cluster_wait();                          // the other CTAs' sums for this one have come
+    }
+}
+
 // Any row: one CTA, the logits read once for the statistics and once more for
 // the gradient, entry by entry.
 template <typename T, int NT>
@@ -533,6 +774,53 @@ int launch_rows(DistillArgs g, int cluster, cudaStream_t s) {
     return ISO_OK;
 }
 
+// clusters that run at once on the current device
+template <typename T>
+int resident_clusters(int cluster, size_t smem) {
+    static std::atomic<int> known[64][4];        // [device][log2 cluster]
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+    const int at = cluster == 1 ? 0 : cluster == 2 ? 1 : cluster == 4 ? 2 : 3;
+    n = known[dev][at].load(std::memory_order_relaxed);
+    if (n) return n;
+    if (cudaFuncSetAttribute(k_distill_stream<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, DS_SMEM) != cudaSuccess) return 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(train_sms() / cluster * cluster));
+    cfg.blockDim = dim3(DS_NT + 32 * DS_TEACHERS);
+    cfg.dynamicSmemBytes = DS_SMEM;
+    cudaLaunchAttribute a;
+    a.id = cudaLaunchAttributeClusterDimension;
+    a.val.clusterDim.x = (unsigned)cluster;
+    a.val.clusterDim.y = a.val.clusterDim.z = 1;
+    cfg.attrs = &a;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, k_distill_stream<T>, &cfg) != cudaSuccess || n <= 0) return 0;
+    known[dev][at].store(n, std::memory_order_relaxed);
+    return n;
+}
+template <typename T>
+int launch_stream(DistillArgs g, int cluster, int share, cudaStream_t s) {
+    const size_t tops = DS_TEACHERS * (size_t)g.top * DI_TOP_BYTES;
+    g.cluster = cluster;
+    g.share = (share + 7) / 8 * 8;               // (stages on 128-byte boundaries)
+    g.stages = (int)std::min<size_t>(DS_MAX_STAGES, (DS_SMEM - tops) / ((size_t)g.share * 16));
+    const int n = resident_clusters<T>(cluster, DS_SMEM);
+    if (n <= 0) return ISO_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)std::min<long long>(g.rows, n) * (unsigned)cluster);
+    cfg.blockDim = dim3(DS_NT + 32 * DS_TEACHERS);
+    cfg.dynamicSmemBytes = DS_SMEM;
+    cfg.stream = s;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = (unsigned)cluster;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    TRAIN_LAUNCH(cudaLaunchKernelEx(&cfg, k_distill_stream<T>, g));
+    return ISO_OK;
+}
+
 template <typename T>
 int launch_distill(const DistillArgs& g, cudaStream_t s) {
     constexpr int N = Word<T>::N;
@@ -546,6 +834,16 @@ int launch_distill(const DistillArgs& g, cudaStream_t s) {
     }
     if (words <= 128 * 4) return words <= 128 ? launch_rows<T, 128, 1>(g, 1, s) : launch_rows<T, 128, 4>(g, 1, s);
     if (words > DI_MAX_CLUSTER * 256 * DI_MAX_WORDS) return launch_rows<T, 512, DI_MAX_WORDS>(g, DI_MAX_CLUSTER, s);
+    // streamed (up to DI_WARP_TOP slots, which a teacher's warp handles alone): the rule
+    // stands with k_distill_stream
+    if (g.top <= DI_WARP_TOP && words >= DS_MIN_WORDS) {
+        const long long room = (DS_SMEM - DS_TEACHERS * (long long)g.top * DI_TOP_BYTES) / 2 / 16;       // words a CTA can hold of two rows
+        int C = 1;
+        while (C < DI_MAX_CLUSTER && words > C * room) C *= 2;
+        const long long rounds = C == 1 ? DS_ROUNDS : DS_ROUNDS_CLUSTER;
+        if (words <= C * room && (C == 1 || g.grad) && (long long)g.rows * C >= rounds * train_sms())
+            return launch_stream<T>(g, C, (words + C - 1) / C, s);
+    }
     // the smallest cluster that holds a row; larger ones while they leave SMs idle
     int C = 1;
     while (words > C * 256 * DI_MAX_WORDS) C *= 2;

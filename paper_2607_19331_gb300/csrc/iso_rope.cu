@@ -21,8 +21,9 @@ namespace iso {
 namespace {
 
 constexpr int ROPE_TPB = 64;            // 256: 108 us for the two passes over 16384 x 4096 bf16, 128: 102, 64: 96
+// units in flight a thread: 64 bytes of loads (twice that: 99 us)
 template <typename T>
-constexpr int ROPE_EACH = sizeof(T) == 2 ? 2 : 1;     // units in flight a thread: 64 bytes of loads (four and two: 99 us)
+constexpr int rope_each(int u) { return u == 1 ? 4 : 16 / (u * (int)sizeof(T) / 2); }
 constexpr int ROPE_MAX_ROWS = 16;
 
 struct RopeArgs {
@@ -50,22 +51,52 @@ __device__ __forceinline__ void rope_angles(const RopeArgs& g, float2* cs, int r
     }
 }
 
-// Heads of whole 16-byte words at such boundaries.  A unit is eight pairs (two words,
-// from either half or side by side), or one word of the channels that are copied.  A
-// thread keeps one unit of a head and goes from head to head; its first units are loaded before the
-// angles are formed.
-template <typename T, bool NEIGHBOURS>
-__global__ void __launch_bounds__(ROPE_TPB) k_rope_words(const __grid_constant__ RopeArgs g) {
+// U channels of a row, side by side: eight in 16 or 32 bytes, four in 8 or 16, or one
+template <typename T, int U>
+struct Run {
+    Raw8<T> x;
+    __device__ __forceinline__ void load(const T* p) { x.load(p); }
+    __device__ __forceinline__ void get(float (&v)[U]) const { x.get(v); }
+    static __device__ __forceinline__ void put(T* p, const float (&v)[U]) { put8(p, v); }
+};
+template <>
+struct Run<float, 4> {
+    float4 x;
+    __device__ __forceinline__ void load(const float* p) { x = __ldcs(reinterpret_cast<const float4*>(p)); }
+    __device__ __forceinline__ void get(float (&v)[4]) const { v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; }
+    static __device__ __forceinline__ void put(float* p, const float (&v)[4]) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
+};
+template <>
+struct Run<__nv_bfloat16, 4> {
+    uint2 x;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { x = __ldcs(reinterpret_cast<const uint2*>(p)); }
+    __device__ __forceinline__ void get(float (&v)[4]) const {
+        bf16x2_to_f32(x.x, v[0], v[1]);
+        bf16x2_to_f32(x.y, v[2], v[3]);
+    }
+    static __device__ __forceinline__ void put(__nv_bfloat16* p, const float (&v)[4]) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(f32_to_bf16x2(v[0], v[1]), f32_to_bf16x2(v[2], v[3]));
+    }
+};
+template <typename T>
+struct Run<T, 1> {
+    T x;
+    __device__ __forceinline__ void load(const T* p) { x = *p; }
+    __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = to_f32(x); }
+    static __device__ __forceinline__ void put(T* p, const float (&v)[1]) { from_f32(v[0], *p); }
+};
+
+// A unit is U pairs (two runs of channels, from either half or side by side) or one
+// run of the channels that are copied.  A thread goes through the block's units in steps of
+// the block, by additions; its first ones are loaded before the angles are formed.
+template <typename T, bool NEIGHBOURS, int U>
+__global__ void __launch_bounds__(ROPE_TPB) k_rope(const __grid_constant__ RopeArgs g) {
     extern __shared__ float2 rope_cs[];
-    constexpr int EACH = ROPE_EACH<T>;
+    constexpr int EACH = rope_each<T>(U);
     const int r0 = blockIdx.x * g.block_rows, rows = min(g.block_rows, g.rows - r0);
-    const int half = g.pairs, turned = g.pairs / 8, units = turned + (g.head_dim - 2 * g.pairs) / 8;
-    const int steps = ROPE_TPB / units, w = (int)threadIdx.x % units;
-    const bool turns = w < turned;
-    // this unit's words
-    const int first = !turns ? 2 * half + (w - turned) * 8 : NEIGHBOURS ? w * 16 : w * 8, second = NEIGHBOURS ? first + 8 : first + half;
-    int r = 0, h = (int)threadIdx.x / units;
-    if (h >= steps) r = rows;                         // threads past the last whole head
+    const int turned = g.pairs / U, units = turned + (g.head_dim - 2 * g.pairs) / U;
+    const int step_h = ROPE_TPB / units, step_w = ROPE_TPB - step_h * units;
+    int r = 0, h = (int)threadIdx.x / units, w = (int)threadIdx.x - h * units;
     auto settle = [&] {
         while (h >= g.heads && r < rows) {
             h -= g.heads;
@@ -73,19 +104,30 @@ __global__ void __launch_bounds__(ROPE_TPB) k_rope_words(const __grid_constant__
         }
     };
     settle();
+    // a unit's runs of channels
+    auto first = [&](int unit) {
+        return unit >= turned ? 2 * g.pairs + (unit - turned) * U : NEIGHBOURS ? unit * 2 * U : unit * U;
+    };
+    auto second = [&](int unit) { return NEIGHBOURS ? unit * 2 * U + U : g.pairs + unit * U; };
     bool formed = false;
     for (;;) {
-        Raw8<T> a[EACH], b[EACH];
-        int rr[EACH], hh[EACH];
+        Run<T, U> a[EACH], b[EACH];
+        int rr[EACH], hh[EACH], ww[EACH];
 #pragma unroll
         for (int k = 0; k < EACH; ++k) {
             rr[k] = r;
             hh[k] = h;
+            ww[k] = w;
             if (r < rows) {
                 const T* x = static_cast<const T*>(g.x) + (long long)(r0 + r) * g.ldx + (long long)h * g.head_dim;
-                a[k].load(x + first);
-                if (turns) b[k].load(x + second);
-                h += steps;
+                a[k].load(x + first(w));
+                if (w < turned) b[k].load(x + second(w));
+                h += step_h;
+                w += step_w;
+                if (w >= units) {
+                    w -= units;
+                    ++h;
+                }
                 settle();
             }
         }
@@ -94,62 +136,43 @@ __global__ void __launch_bounds__(ROPE_TPB) k_rope_words(const __grid_constant__
             __syncthreads();
             formed = true;
         }
-        if (rr[0] >= rows) return;
 #pragma unroll
         for (int k = 0; k < EACH; ++k) {
             if (rr[k] >= rows) return;
             T* y = static_cast<T*>(g.y) + (long long)(r0 + rr[k]) * g.ldy + (long long)hh[k] * g.head_dim;
-            float u[8], v[8];
+            float u[U], v[U];
             a[k].get(u);
-            if (turns) {
+            if (ww[k] < turned) {
                 b[k].get(v);
-                const float4* cs = reinterpret_cast<const float4*>(rope_cs + rr[k] * g.pairs + w * 8);
+                const float2* cs = rope_cs + rr[k] * g.pairs + ww[k] * U;
+                if constexpr (U == 1) {
+                    const float u0 = u[0], v0 = v[0];
+                    u[0] = u0 * cs[0].x - v0 * cs[0].y;
+                    v[0] = u0 * cs[0].y + v0 * cs[0].x;
+                } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float4 t = cs[j];           // two pairs
-                    if constexpr (NEIGHBOURS) {
-                        float* const z = j < 2 ? u + 4 * j : v + 4 * (j - 2);
-                        const float z0 = z[0], z1 = z[1], z2 = z[2], z3 = z[3];
-                        z[0] = z0 * t.x - z1 * t.y;
-                        z[1] = z0 * t.y + z1 * t.x;
-                        z[2] = z2 * t.z - z3 * t.w;
-                        z[3] = z2 * t.w + z3 * t.z;
-                    } else {
-                        const float u0 = u[2 * j], v0 = v[2 * j], u1 = u[2 * j + 1], v1 = v[2 * j + 1];
-                        u[2 * j] = u0 * t.x - v0 * t.y;
-                        v[2 * j] = u0 * t.y + v0 * t.x;
-                        u[2 * j + 1] = u1 * t.z - v1 * t.w;
-                        v[2 * j + 1] = u1 * t.w + v1 * t.z;
+                    for (int j = 0; j < U / 2; ++j) {
+                        const float4 t = reinterpret_cast<const float4*>(cs)[j];           // two pairs
+                        if constexpr (NEIGHBOURS) {
+                            float* const z = j < U / 4 ? u + 4 * j : v + 4 * (j - U / 4);
+                            const float z0 = z[0], z1 = z[1], z2 = z[2], z3 = z[3];
+                            z[0] = z0 * t.x - z1 * t.y;
+                            z[1] = z0 * t.y + z1 * t.x;
+                            z[2] = z2 * t.z - z3 * t.w;
+                            z[3] = z2 * t.w + z3 * t.z;
+                        } else {
+                            const float u0 = u[2 * j], v0 = v[2 * j], u1 = u[2 * j + 1], v1 = v[2 * j + 1];
+                            u[2 * j] = u0 * t.x - v0 * t.y;
+                            v[2 * j] = u0 * t.y + v0 * t.x;
+                            u[2 * j + 1] = u1 * t.z - v1 * t.w;
+                            v[2 * j + 1] = u1 * t.w + v1 * t.z;
+                        }
                     }
                 }
-                put8(y + second, v);
+                Run<T, U>::put(y + second(ww[k]), v);
             }
-            put8(y + first, u);
+            Run<T, U>::put(y + first(ww[k]), u);
         }
-    }
-}
-
-// Any rows: a pair, or a channel that is copied, at a time.
-template <typename T, bool NEIGHBOURS>
-__global__ void __launch_bounds__(ROPE_TPB) k_rope(const __grid_constant__ RopeArgs g) {
-    extern __shared__ float2 rope_cs[];
-    const int r0 = blockIdx.x * g.block_rows, rows = min(g.block_rows, g.rows - r0);
-    rope_angles(g, rope_cs, r0, rows);
-    __syncthreads();
-    const int units = g.head_dim - g.pairs, per_row = units * g.heads;
-    for (int i = threadIdx.x; i < rows * per_row; i += ROPE_TPB) {
-        const int r = i / per_row, u = i - r * per_row, h = u / units, w = u - h * units;
-        const T* x = static_cast<const T*>(g.x) + (long long)(r0 + r) * g.ldx + (long long)h * g.head_dim;
-        T* y = static_cast<T*>(g.y) + (long long)(r0 + r) * g.ldy + (long long)h * g.head_dim;
-        if (w >= g.pairs) {
-            y[g.pairs + w] = x[g.pairs + w];
-            continue;
-        }
-        const int ca = NEIGHBOURS ? 2 * w : w, cb = NEIGHBOURS ? 2 * w + 1 : g.pairs + w;
-        const float2 t = rope_cs[r * g.pairs + w];
-        const float u0 = to_f32(x[ca]), w0 = to_f32(x[cb]);
-        from_f32(u0 * t.x - w0 * t.y, y[ca]);
-        from_f32(u0 * t.y + w0 * t.x, y[cb]);
     }
 }
 
@@ -166,18 +189,25 @@ unsigned long long fixed_turns(double freq) {
     return fraction(t) + fraction(std::fma(freq, hi, -t) + freq * lo);
 }
 
-template <typename T>
-int launch_rope(RopeArgs& g, bool neighbours, bool words, cudaStream_t s) {
-    const long long units = words ? (long long)g.heads * ((g.head_dim - g.pairs) / 8) : (long long)g.heads * (g.head_dim - g.pairs);
-    g.block_rows = (int)std::max<long long>(1, std::min<long long>(ROPE_MAX_ROWS, ROPE_TPB * ROPE_EACH<T> / std::max<long long>(1, units)));
+template <typename T, int U>
+int launch_rope(RopeArgs& g, bool neighbours, cudaStream_t s) {
+    const long long units = (long long)g.heads * ((g.head_dim - g.pairs) / U);
+    g.block_rows = (int)std::max<long long>(1, std::min<long long>(ROPE_MAX_ROWS, ROPE_TPB * rope_each<T>(U) / std::max<long long>(1, units)));
     const unsigned grid = (unsigned)((g.rows + g.block_rows - 1) / g.block_rows);
     const size_t smem = std::max<size_t>(1, (size_t)g.block_rows * g.pairs) * sizeof(float2);
-    if (words) {
-        TRAIN_LAUNCH((neighbours ? k_rope_words<T, true><<<grid, ROPE_TPB, smem, s>>>(g) : k_rope_words<T, false><<<grid, ROPE_TPB, smem, s>>>(g)));
-    } else {
-        TRAIN_LAUNCH((neighbours ? k_rope<T, true><<<grid, ROPE_TPB, smem, s>>>(g) : k_rope<T, false><<<grid, ROPE_TPB, smem, s>>>(g)));
-    }
+    TRAIN_LAUNCH((neighbours ? k_rope<T, true, U><<<grid, ROPE_TPB, smem, s>>>(g) : k_rope<T, false, U><<<grid, ROPE_TPB, smem, s>>>(g)));
     return ISO_OK;
+}
+// Eight, four or one pair a unit: the most whose runs of channels are whole loads in
+// every head of every row
+template <typename T>
+int launch_rope(RopeArgs& g, bool neighbours, cudaStream_t s) {
+    auto fits = [&](int u) {
+        const uint64_t bytes = std::min<uint64_t>(16, u * sizeof(T));
+        return g.pairs % u == 0 && g.head_dim % u == 0 && (reinterpret_cast<uintptr_t>(g.x) | reinterpret_cast<uintptr_t>(g.y)) % bytes == 0 &&
+               (g.rows == 1 || (g.ldx * sizeof(T) % bytes == 0 && g.ldy * sizeof(T) % bytes == 0));
+    };
+    return fits(8) ? launch_rope<T, 8>(g, neighbours, s) : fits(4) ? launch_rope<T, 4>(g, neighbours, s) : launch_rope<T, 1>(g, neighbours, s);
 }
 
 }  // namespace
@@ -227,10 +257,7 @@ extern "C" int32_t iso_rope(const iso_mat* x, const void* positions, int32_t pos
     g.pairs = pairs;
     g.positions_i64 = positions_i64;
     g.inverse = cfg->inverse;
-    // eight pairs a thread: their channels are whole 16-byte words of a head that
-    // starts on such a boundary (in the halves form each half does)
-    const bool words = rows_aligned(x) && rows_aligned(y) && cfg->head_dim % 8 == 0 && pairs % 8 == 0 && cfg->head_dim <= 8 * ROPE_TPB;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return x->dtype == ISO_BF16 ? launch_rope<__nv_bfloat16>(g, cfg->neighbours, words, s)
-                                : launch_rope<float>(g, cfg->neighbours, words, s);
+    return x->dtype == ISO_BF16 ? launch_rope<__nv_bfloat16>(g, cfg->neighbours, s)
+                                : launch_rope<float>(g, cfg->neighbours, s);
 }

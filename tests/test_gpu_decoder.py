@@ -432,6 +432,37 @@ def test_distillation(T, V, K, tau, ld, off, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,V,K,ld,off", [(700, 4200, 3, None, 0), (640, 20011, 20, 20015, 3), (333, 60000, 128, None, 0), (161, 152064, 5, None, 8),
+                                           (700, 30001, 20, 30004, 3), (2500, 52000, 5, None, 0)])
+def test_distillation_of_many_long_rows(T, V, K, ld, off, dtype):
+    """Rows for every cluster to go through several of them; the last ones of
+    another number, rows off 16-byte boundaries, in place."""
+    z, ids, t, dloss = _distill_case(17, T, V, K, dtype, ld, off)
+    z[5, 7], z[T - 1, V - 1], z[T // 2] = math.nan, math.inf, -math.inf
+    ids[9], ids[T - 2] = -1, -1
+    d, i, w = dloss.to(DEV), ids.to(DEV), t.to(DEV)
+    same = torch.empty_strided(z.shape, z.stride(), dtype=dtype, device=DEV) if off == 0 else None
+    loss, lse, grad = iso.distill(z, i, w, 1.3, dloss=d, out=same)
+    rows = sorted(set(list(range(0, T, 37)) + [5, 9, T // 2, T - 2, T - 1]))
+
+    def check(loss, lse, grad, what):
+        pick = lambda x: None if x is None else x[rows]                       # noqa: E731
+        _check_distill(z[rows], ids[rows], t[rows], 1.3, dloss[rows], pick(loss), pick(lse), pick(grad), what)
+    check(loss, lse, grad, "joint")
+    l2, s2 = iso.distill(z, i, w, 1.3)
+    check(l2, s2, None, "loss alone")
+    g2 = iso.distill_grad(d, z, i, w, lse, 1.3)
+    check(None, None, g2, "apart")
+    for joint in (True, False):
+        z4 = torch.empty_strided(z.shape, z.stride(), dtype=dtype, device=DEV).copy_(z)
+        g4 = iso.distill(z4, i, w, 1.3, dloss=d, out=z4)[2] if joint else iso.distill_grad(d, z4, i, w, lse, 1.3, out=z4)
+        assert torch.equal(g4.nan_to_num(7.0), (grad if joint and off == 0 else g4).nan_to_num(7.0))
+        check(None, None, g4, "in place")
+    # every other row as it is in a call of its own kind of rows: nothing of one row in another
+    assert torch.equal(iso.distill(z, i, w, 1.3)[1].nan_to_num(7.0), s2.nan_to_num(7.0))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("V", [50, 3000, 30000])
 def test_distillation_of_infinities_nan_and_empty_rows(V, dtype):
     z, ids, t, dloss = _distill_case(8, 8, V, 4, dtype)
