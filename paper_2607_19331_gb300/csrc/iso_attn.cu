@@ -240,7 +240,7 @@ size_t round256(size_t b) { return (b + 255) & ~(size_t)255; }
 
 // what tensor copies can take: heads and rows on 16-byte boundaries
 bool copies_take(const iso_mat* m) {
-    return (reinterpret_cast<uintptr_t>(m->data) & 15u) == 0 && (m->ld * 2) % 16 == 0;
+    return (reinterpret_cast<uintptr_t>(m->data) & 15u) == 0 && (m->rows == 1 || (m->ld * 2) % 16 == 0);
 }
 template <typename... M>
 bool on_tensor_cores(const iso_attn_cfg* c, const M*... m) {
@@ -273,7 +273,8 @@ int tc::head_map(CUtensorMap* map, const void* base, long long rows, int heads, 
     EncodeTiled fn = encode_tiled();
     if (!fn) return ISO_ERR_CUDA;
     const cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)rows};
-    const cuuint64_t strides[2] = {(cuuint64_t)head_dim * 2, (cuuint64_t)ld * 2};
+    // (of a single row any stride does)
+    const cuuint64_t strides[2] = {(cuuint64_t)head_dim * 2, (cuuint64_t)(rows == 1 ? (long long)heads * head_dim : ld) * 2};
     const cuuint32_t box[3] = {(cuuint32_t)BOX, 1, (cuuint32_t)ROWS};
     const cuuint32_t estr[3] = {1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,

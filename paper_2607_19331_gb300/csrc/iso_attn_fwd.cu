@@ -359,13 +359,14 @@ __global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ FwdAr
         const int s = (int)(i % segs), h = (int)(i / segs % g.heads);
         const long long row = first + i / segs / g.heads;
         float m = -INFINITY, sum = 0.0f, acc[8] = {};
+#pragma unroll 8
         for (int p = 0; p < a.parts; ++p) m = fmaxf(m, lses[((long long)p * g.heads + h) * g.q_rows + row]);
         const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll 4
         for (int p = 0; p < a.parts; ++p) {
             const float w = expf(lses[((long long)p * g.heads + h) * g.q_rows + row] - base);
             sum += w;
-            if (w == 0.0f) continue;             // a part without a seen key (or one that does not count)
-            float x[8];
+            float x[8];                          // (of a part without a seen key: zeros, of weight 0)
             load8<true>(a.part + ((long long)p * g.q_rows + row) * width + (long long)h * g.head_dim, s * 8, g.head_dim, x);
 #pragma unroll
             for (int j = 0; j < 8; ++j) acc[j] = fmaf(w, x[j], acc[j]);

@@ -744,7 +744,7 @@ int check_distill(const iso_mat* z, const void* ids, int32_t ids_i64, const iso_
     ISO_TRY(check_mat(z));
     ISO_TRY(check_mat(teacher));
     if (grad) ISO_TRY(check_mat(grad));
-    if ((ids_i64 != 0 && ids_i64 != 1) || !(tau > 0.0f) || !std::isfinite(tau) || !std::isfinite(1.0f / tau)) return ISO_ERR_ARG;
+    if ((ids_i64 != 0 && ids_i64 != 1) || !(tau > 0.0f) || !std::isfinite(tau) || !std::isfinite(1.0f / tau * LOG2E)) return ISO_ERR_ARG;
     if (teacher->rows != z->rows || (grad && (grad->rows != z->rows || grad->cols != z->cols))) return ISO_ERR_SHAPE;
     if (grad && grad->dtype != z->dtype) return ISO_ERR_DTYPE;
     if (teacher->cols > ISO_DISTILL_MAX_TOP) return ISO_ERR_UNSUPPORTED;

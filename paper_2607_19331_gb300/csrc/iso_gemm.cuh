@@ -77,7 +77,7 @@ int gemm_tensor_map(CUtensorMap* map, const float* base, long long rows, long lo
 // library (iso_api.cu): kind 0 = the tensor-core products, 1 = the other
 // frame-merge and optimizer kernels, 2 = the range selection kernels
 // (iso_range.cu), 3 = the training-step operators (iso_act.cu, iso_wgrad.cu,
-// iso_embed.cu).  prof_begin returns a slot (or -1 when profiling is
+// iso_embed.cu, iso_rope.cu, iso_attn*.cu, iso_distill.cu).  prof_begin returns a slot (or -1 when profiling is
 // off); prof_end records the end event and counts the launch.
 int prof_begin(int frame_kind, cudaStream_t s);
 void prof_end(int slot, cudaStream_t s);

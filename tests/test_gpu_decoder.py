@@ -268,6 +268,16 @@ def test_attention_of_odd_heads_strides_and_addresses(D, gap, off, dtype):
     Case([90, 40], [95, 130], 2, 1, D, dtype=dtype, gap=gap, off=off, pad=2).run()
 
 
+@pytest.mark.parametrize("n,m", [(1, 1), (1, 700), (90, 1)])
+def test_a_single_row_of_any_stride(n, m):
+    """One query, or one key, out of rows off 16-byte boundaries."""
+    q, do = (_rand(i, max(n, 2), 128, BF, 131 if n == 1 else 128) for i in (1, 2))
+    k, v = (_rand(i, max(m, 2), 64, BF, 67 if m == 1 else 64) for i in (3, 4))
+    c = Case([n], [m], 2, 1, 64)
+    c.q, c.dout, c.k, c.v, c.tc = q[:n], do[:n], k[:m], v[:m], True
+    c.run()
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("amp,scale", [(8.0, None), (1.0, 2.0), (0.01, None)])
 def test_attention_of_sharp_and_flat_weights(amp, scale, dtype):
