@@ -36,7 +36,7 @@ namespace {
 
 constexpr int DI_MAX_CLUSTER = 8;
 constexpr int DI_MAX_WORDS = 10;         // 16-byte words of a row a thread holds
-constexpr int DI_WARP_TOP = 128;         // up to this many slots the teacher's warp adds up equal ids alone
+constexpr int DI_WARP_TOP = 256;         // up to this many slots the teacher's warp adds up equal ids alone
 using tc::LOG2E;
 using tc::pair_of;
 using tc::parts_of;
@@ -115,16 +115,42 @@ struct Top {
     float* p;                // probabilities
     float* z;                // logits at the ids
     float* mass;             // probabilities of all slots of the id together
+    uint16_t* bucket;        // of ids, by a hash: the slot of one, or DI_SEVERAL
 };
+constexpr int DI_BUCKET_BITS = 11;
+constexpr uint16_t DI_SEVERAL = 0xFFFF;
+constexpr int top_floats(int n) { return 4 * n + (1 << DI_BUCKET_BITS) / 2; }
 __device__ __forceinline__ Top top_of(float* smem, int n) {
-    return {reinterpret_cast<int*>(smem), smem + n, smem + 2 * n, smem + 3 * n};
+    return {reinterpret_cast<int*>(smem), smem + n, smem + 2 * n, smem + 3 * n, reinterpret_cast<uint16_t*>(smem + 4 * n)};
 }
-constexpr int DI_TOP_BYTES = 16;
 
-__device__ __forceinline__ float mass_of(const Top& t, int top, int id) {
-    float p = 0.0f;
-    for (int j = 0; j < top; ++j) p += t.id[j] == id ? t.p[j] : 0.0f;
-    return p;
+// p of every slot's id, by one warp.  An id that shares its bucket with no other slot's
+// has that slot alone; for the few others the warp goes through all slots.  (All slots
+// against all: 200 slots of 4096 rows of 152064 cost 370 us more than 64.)
+__device__ __forceinline__ void masses(const Top& t, int top) {
+    const int lane = threadIdx.x & 31;
+    auto bucket_of = [&](int id) { return (uint32_t)id * 2654435761u >> (32 - DI_BUCKET_BITS); };
+    for (int k = lane; k < top; k += 32)
+        if (t.id[k] >= 0) t.bucket[bucket_of(t.id[k])] = (uint16_t)k;
+    __syncwarp();
+    for (int k = lane; k < top; k += 32)
+        if (t.id[k] >= 0 && t.bucket[bucket_of(t.id[k])] != k) t.bucket[bucket_of(t.id[k])] = DI_SEVERAL;
+    __syncwarp();
+    for (int k0 = 0; k0 < top; k0 += 32) {
+        const int k = k0 + lane, id = k < top ? t.id[k] : -1;
+        float mass = id >= 0 ? t.p[k] : 0.0f;
+        unsigned several = __ballot_sync(0xFFFFFFFFu, id >= 0 && t.bucket[bucket_of(id)] == DI_SEVERAL);
+        while (several) {
+            const int l = __ffs(several) - 1;
+            several &= several - 1;
+            const int want = __shfl_sync(0xFFFFFFFFu, id, l);
+            float p = 0.0f;
+            for (int j = lane; j < top; j += 32) p += t.id[j] == want ? t.p[j] : 0.0f;
+            p = warp_sum(p);
+            if (lane == l) mass = p;
+        }
+        if (k < top) t.mass[k] = mass;
+    }
 }
 
 // By one warp; z is read at the ids in [from, to).  Whether the row has a used slot
@@ -161,8 +187,7 @@ __device__ __forceinline__ bool teacher_side(const DistillArgs& g, int row, cons
     s = warp_sum(s);
     for (int k = lane; k < g.top; k += 32) t.p[k] = t.p[k] / s;
     __syncwarp();
-    if (g.grad && g.top <= DI_WARP_TOP)
-        for (int k = lane; k < g.top; k += 32) t.mass[k] = mass_of(t, g.top, t.id[k]);
+    if (g.grad && g.top <= DI_WARP_TOP) masses(t, g.top);
     return true;
 }
 
@@ -449,7 +474,7 @@ __global__ void __launch_bounds__(NT + 32, NT == 512 ? 2 : NT == 256 ? 4 : 6) k_
 // so it takes rows of DS_MIN_WORDS that fit one CTA, DS_ROUNDS rows for each, and rows of
 // larger clusters for a gradient, DS_ROUNDS_CLUSTER for each.  (The words kept in
 // registers from the first pass on, with 20 a thread: 589 us for the first case.)
-constexpr int DS_NT = 256, DS_TEACHERS = 4, DS_MAX_STAGES = 4, DS_SMEM = 200 * 1024;
+constexpr int DS_NT = 256, DS_TEACHERS = 4, DS_MAX_STAGES = 4, DS_SMEM = 220 * 1024;
 constexpr int DS_MIN_WORDS = 3000, DS_ROUNDS = 4, DS_ROUNDS_CLUSTER = 32;
 __device__ __forceinline__ bool probe_cluster(uint32_t bar, uint32_t parity) {
     uint32_t ok;
@@ -642,7 +667,7 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
         }
     } else {
         const int slot = warp - WARPS;
-        const Top t = top_of(tops + slot * 4 * g.top, g.top);
+        const Top t = top_of(tops + slot * top_floats(g.top), g.top);
         uint32_t ph = 0;
         for (int row = row0 + slot * clusters; row < g.rows; row += DS_TEACHERS * clusters, ph ^= 1u) {
             const Part p = part_of(row);
@@ -762,7 +787,7 @@ int launch_rows(DistillArgs g, int cluster, cudaStream_t s) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)g.rows * (unsigned)cluster);
     cfg.blockDim = dim3(NT + 32);
-    cfg.dynamicSmemBytes = (size_t)g.top * DI_TOP_BYTES;
+    cfg.dynamicSmemBytes = (size_t)top_floats(g.top) * 4;
     cfg.stream = s;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeClusterDimension;
@@ -800,7 +825,7 @@ int resident_clusters(int cluster, size_t smem) {
 }
 template <typename T>
 int launch_stream(DistillArgs g, int cluster, int share, cudaStream_t s) {
-    const size_t tops = DS_TEACHERS * (size_t)g.top * DI_TOP_BYTES;
+    const size_t tops = DS_TEACHERS * (size_t)top_floats(g.top) * 4;
     g.cluster = cluster;
     g.share = (share + 7) / 8 * 8;               // (stages on 128-byte boundaries)
     g.stages = (int)std::min<size_t>(DS_MAX_STAGES, (DS_SMEM - tops) / ((size_t)g.share * 16));
@@ -829,7 +854,7 @@ int launch_distill(const DistillArgs& g, cudaStream_t s) {
                                    (g.rows == 1 || (g.ldz - g.ldg) * (long long)sizeof(T) % 16 == 0));
     const int words = g.vocab / N;
     if (!alike || words > DI_MAX_CLUSTER * 512 * DI_MAX_WORDS || (long long)g.rows * DI_MAX_CLUSTER > EXTENT_LIMIT) {
-        TRAIN_LAUNCH((k_distill_long<T, 1024><<<(unsigned)g.rows, 1024, (size_t)g.top * DI_TOP_BYTES, s>>>(g)));
+        TRAIN_LAUNCH((k_distill_long<T, 1024><<<(unsigned)g.rows, 1024, (size_t)top_floats(g.top) * 4, s>>>(g)));
         return ISO_OK;
     }
     if (words <= 128 * 4) return words <= 128 ? launch_rows<T, 128, 1>(g, 1, s) : launch_rows<T, 128, 4>(g, 1, s);
@@ -837,7 +862,7 @@ int launch_distill(const DistillArgs& g, cudaStream_t s) {
     // streamed (up to DI_WARP_TOP slots, which a teacher's warp handles alone): the rule
     // stands with k_distill_stream
     if (g.top <= DI_WARP_TOP && words >= DS_MIN_WORDS) {
-        const long long room = (DS_SMEM - DS_TEACHERS * (long long)g.top * DI_TOP_BYTES) / 2 / 16;       // words a CTA can hold of two rows
+        const long long room = (DS_SMEM - DS_TEACHERS * 4LL * top_floats(g.top)) / 2 / 16;       // words a CTA can hold of two rows
         int C = 1;
         while (C < DI_MAX_CLUSTER && words > C * room) C *= 2;
         const long long rounds = C == 1 ? DS_ROUNDS : DS_ROUNDS_CLUSTER;

@@ -51,14 +51,9 @@ __device__ __forceinline__ void rope_angles(const RopeArgs& g, float2* cs, int r
     }
 }
 
-// U channels of a row, side by side: eight in 16 or 32 bytes, four in 8 or 16, or one
+// U channels of a row, side by side: four in 8 or 16 bytes, or one
 template <typename T, int U>
-struct Run {
-    Raw8<T> x;
-    __device__ __forceinline__ void load(const T* p) { x.load(p); }
-    __device__ __forceinline__ void get(float (&v)[U]) const { x.get(v); }
-    static __device__ __forceinline__ void put(T* p, const float (&v)[U]) { put8(p, v); }
-};
+struct Run;
 template <>
 struct Run<float, 4> {
     float4 x;
@@ -85,6 +80,14 @@ struct Run<T, 1> {
     __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = to_f32(x); }
     static __device__ __forceinline__ void put(T* p, const float (&v)[1]) { from_f32(v[0], *p); }
 };
+
+// (u, w) turned, in the same operations for every unit, so that a row's bits do not
+// depend on how it lies
+__device__ __forceinline__ void turn(float& u, float& w, float c, float s) {
+    const float a = __fmaf_rn(u, c, -__fmul_rn(w, s)), b = __fmaf_rn(u, s, __fmul_rn(w, c));
+    u = a;
+    w = b;
+}
 
 // A unit is U pairs (two runs of channels, from either half or side by side) or one
 // run of the channels that are copied.  A thread goes through the block's units in steps of
@@ -146,26 +149,18 @@ __global__ void __launch_bounds__(ROPE_TPB) k_rope(const __grid_constant__ RopeA
                 b[k].get(v);
                 const float2* cs = rope_cs + rr[k] * g.pairs + ww[k] * U;
                 if constexpr (U == 1) {
-                    const float u0 = u[0], v0 = v[0];
-                    u[0] = u0 * cs[0].x - v0 * cs[0].y;
-                    v[0] = u0 * cs[0].y + v0 * cs[0].x;
+                    turn(u[0], v[0], cs[0].x, cs[0].y);
                 } else {
 #pragma unroll
                     for (int j = 0; j < U / 2; ++j) {
                         const float4 t = reinterpret_cast<const float4*>(cs)[j];           // two pairs
                         if constexpr (NEIGHBOURS) {
-                            float* const z = j < U / 4 ? u + 4 * j : v + 4 * (j - U / 4);
-                            const float z0 = z[0], z1 = z[1], z2 = z[2], z3 = z[3];
-                            z[0] = z0 * t.x - z1 * t.y;
-                            z[1] = z0 * t.y + z1 * t.x;
-                            z[2] = z2 * t.z - z3 * t.w;
-                            z[3] = z2 * t.w + z3 * t.z;
+                            float* const z = j == 0 ? u : v;
+                            turn(z[0], z[1], t.x, t.y);
+                            turn(z[2], z[3], t.z, t.w);
                         } else {
-                            const float u0 = u[2 * j], v0 = v[2 * j], u1 = u[2 * j + 1], v1 = v[2 * j + 1];
-                            u[2 * j] = u0 * t.x - v0 * t.y;
-                            v[2 * j] = u0 * t.y + v0 * t.x;
-                            u[2 * j + 1] = u1 * t.z - v1 * t.w;
-                            v[2 * j + 1] = u1 * t.w + v1 * t.z;
+                            turn(u[2 * j], v[2 * j], t.x, t.y);
+                            turn(u[2 * j + 1], v[2 * j + 1], t.z, t.w);
                         }
                     }
                 }
@@ -198,16 +193,14 @@ int launch_rope(RopeArgs& g, bool neighbours, cudaStream_t s) {
     TRAIN_LAUNCH((neighbours ? k_rope<T, true, U><<<grid, ROPE_TPB, smem, s>>>(g) : k_rope<T, false, U><<<grid, ROPE_TPB, smem, s>>>(g)));
     return ISO_OK;
 }
-// Eight, four or one pair a unit: the most whose runs of channels are whole loads in
-// every head of every row
+// Four pairs a unit where their runs of channels are whole loads in every head of
+// every row, else one (16384 x 4096 bf16, one way: 46 us; eight pairs 51, one 102)
 template <typename T>
 int launch_rope(RopeArgs& g, bool neighbours, cudaStream_t s) {
-    auto fits = [&](int u) {
-        const uint64_t bytes = std::min<uint64_t>(16, u * sizeof(T));
-        return g.pairs % u == 0 && g.head_dim % u == 0 && (reinterpret_cast<uintptr_t>(g.x) | reinterpret_cast<uintptr_t>(g.y)) % bytes == 0 &&
-               (g.rows == 1 || (g.ldx * sizeof(T) % bytes == 0 && g.ldy * sizeof(T) % bytes == 0));
-    };
-    return fits(8) ? launch_rope<T, 8>(g, neighbours, s) : fits(4) ? launch_rope<T, 4>(g, neighbours, s) : launch_rope<T, 1>(g, neighbours, s);
+    constexpr uint64_t bytes = 4 * sizeof(T);
+    const bool four = g.pairs % 4 == 0 && g.head_dim % 4 == 0 && (reinterpret_cast<uintptr_t>(g.x) | reinterpret_cast<uintptr_t>(g.y)) % bytes == 0 &&
+                      (g.rows == 1 || (g.ldx * sizeof(T) % bytes == 0 && g.ldy * sizeof(T) % bytes == 0));
+    return four ? launch_rope<T, 4>(g, neighbours, s) : launch_rope<T, 1>(g, neighbours, s);
 }
 
 }  // namespace
