@@ -12,6 +12,10 @@
 // run.  The maximum is only moved when it grows by more than 2^RAISE (in the
 // weights): until then e = 1, weights are up to 2^RAISE and the sums grow with
 // them, which binary32 and bf16 hold as well; O is read and written back rarely.
+// Measured: 8192 tokens, 28 heads over 4 of 128, causal, 394 us, 1.22 PFLOP/s (without
+// causal 1.32).  What bounds it is a tile's chain: of 3600 clocks a step 1900 form the
+// weights (960 of them exponentials, 512 at the least), the rest waits for two products
+// and for the other tile's; sixteen warps with half a row a thread spill (899 us).
 // Few queries over many keys: the key tiles are cut into parts for CTAs of their
 // own, whose outputs and log-sum-exps k_attn_join puts together.
 #include "iso_attn.cuh"

@@ -4,25 +4,27 @@
 // The weights are formed again from lse, and both kernels own what they write, so
 // there are no atomics and no binary32 gradients in memory; that takes seven products of
 // 128 x 128 x dim a pair of tiles instead of five.
-//   k_tc_grad_kv   128 keys: over the query tiles (and query heads) that see them
-//                    S^T = K Q^T       P^T = exp2(c S^T - lse2)      dV += P^T dO
-//                    dP^T = V dO^T     dS^T = P^T (dP^T - delta)     dK += dS^T Q
-//                  Keys are rows, so that P^T and dS^T, rounded to bf16, go back
-//                  to tensor memory over the scores they came from and are the A
-//                  operands of the second products as they are; Q and dO serve
-//                  both as rows to contract along and as rows to contract over.
-//                  The products are issued as
-//                    dV(i) S(i+1) | dK(i) dP(i+1) | dV(i+1) ...
-//                  so that while the warps form P(i+1) from S(i+1) the pair dK(i),
-//                  dP(i+1) runs, and while they form dS(i+1), the pair dV(i+1),
-//                  S(i+2): one buffer each for scores and dP keeps both busy.
-//   k_tc_grad_q    128 queries: over the key tiles that they see
-//                    S = Q K^T, dP = dO V^T, dS = P (dP - delta), dQ += dS K
-//                  with two buffers of scores; dS lies over its scores.
-// Tensor memory is full in both (4 x 128 columns).
-// GR_COMPUTE warps compute, four on each GR_COLS of a tile's columns; one warp
-// copies, one issues products; in k_tc_grad_kv one more brings lse and delta, which
-// are per column there.
+//   grad_kv   128 keys: over the query tiles (and query heads) that see them
+//               S^T = K Q^T       P^T = exp2(c S^T - lse2)      dV += P^T dO
+//               dP^T = V dO^T     dS^T = P^T (dP^T - delta)     dK += dS^T Q
+//             Keys are rows, so that P^T and dS^T, rounded to bf16, go back to
+//             tensor memory over the scores they came from and are the A operands of the
+//             second products as they are; Q and dO serve both as rows to contract
+//             along and as rows to contract over.  Two warps issue products, dV(i)
+//             S(i+1) the one and dK(i) dP(i+1) the other: while the warps form P(i+1)
+//             the second pair runs, and while they form dS(i+1) the first, with one buffer each
+//             for scores and dP.  (One warp for both waited for either's turn: 1312
+//             against 1160 us.)
+//   grad_q    128 queries: over the key tiles that they see
+//               S = Q K^T, dP = dO V^T, dS = P (dP - delta), dQ += dS K
+//             with two buffers of scores; dS lies over its scores.
+// Tensor memory is full in both (4 x 128 columns).  Eight warps compute, four on each
+// GR_COLS columns of a tile; one warp copies, two issue products, and in grad_kv
+// one more brings lse and delta, which are per column there.
+// Measured: 8192 tokens, 28 heads over 4 of 128, causal, 1.03 - 1.11 ms (1.09 - 1.17
+// PFLOP/s of the five products, 7/5 of that issued); tensor pipe 66 % active.  What
+// bounds it is a step's chain: 300 - 700 clocks of waiting for its products, 1300 -
+// 1900 of forming weights and gradients, against 1536 (grad_q) and 2048 of products.
 #include "iso_attn.cuh"
 #include "iso_attn_simt.cuh"
 #include "iso_attn_tc.cuh"

@@ -160,19 +160,38 @@ __device__ __forceinline__ bool teacher_side(const DistillArgs& g, int row, cons
     const int lane = threadIdx.x & 31;
     float m = -INFINITY;
     bool nan = false;
-    for (int k = lane; k < g.top; k += 32) {
-        const long long v = id_at(g, (long long)row * g.top + k), at = (long long)row * g.ldt + k;
-        const bool used = v >= 0 && v < g.vocab;
-        if (!used && v != -1 && g.status) atomicCAS(g.status, 0, (int32_t)ISO_ERR_INDEX);
-        float x = -INFINITY;
-        if (used)
-            x = (g.teacher_f32 ? static_cast<const float*>(g.teacher)[at]
-                               : __bfloat162float(static_cast<const __nv_bfloat16*>(g.teacher)[at])) * g.inv_tau;
-        t.id[k] = used ? (int)v : -1;
-        t.p[k] = x;
-        t.z[k] = v >= from && v < to ? to_f32(z[v]) : 0.0f;
-        m = fmaxf(m, x);
-        nan |= x != x;
+    constexpr int EACH = 4;                      // slots a lane reads at once: ids and teacher's logits, then z
+    for (int k0 = lane; k0 < g.top; k0 += 32 * EACH) {
+        long long v[EACH];
+        float x[EACH], y[EACH];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int k = k0 + 32 * i;
+            const long long at = (long long)row * g.ldt + k;
+            v[i] = -1;
+            x[i] = y[i] = 0.0f;
+            if (k < g.top) {
+                v[i] = id_at(g, (long long)row * g.top + k);
+                x[i] = g.teacher_f32 ? static_cast<const float*>(g.teacher)[at]
+                                     : __bfloat162float(static_cast<const __nv_bfloat16*>(g.teacher)[at]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+            if (v[i] >= from && v[i] < to) y[i] = to_f32(z[v[i]]);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int k = k0 + 32 * i;
+            if (k >= g.top) continue;
+            const bool used = v[i] >= 0 && v[i] < g.vocab;
+            if (!used && v[i] != -1 && g.status) atomicCAS(g.status, 0, (int32_t)ISO_ERR_INDEX);
+            const float w = used ? x[i] * g.inv_tau : -INFINITY;
+            t.id[k] = used ? (int)v[i] : -1;
+            t.p[k] = w;
+            t.z[k] = y[i];
+            m = fmaxf(m, w);
+            nan |= w != w;
+        }
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
