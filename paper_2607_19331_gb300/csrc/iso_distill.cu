@@ -581,8 +581,8 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
             if (rank == C - 1 && p.behind + back < g.vocab) single = p.behind + back;
             const float xs = single >= 0 ? to_f32(p.z[single]) : -INFINITY;
             bool whole = wait.warp(smem_u32(&full[stage]), parity);
+            Stat a = {xs, 0.0f};
             if (!g.lse_in) {
-                Stat a = {xs, 0.0f};
 #pragma unroll 4
                 for (int i = threadIdx.x; i < n; i += NT) {
                     Word<T> x;
@@ -643,9 +643,10 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
                 if (!whole) a.s = __int_as_float(0x7FFFFFFF);
                 level = ex.level(a.m);
                 inv_s = 1.0f / a.s;
-                if (threadIdx.x == 0) of_row[slot] = a;
             }
             whole = wait.warp(smem_u32(&prepared[slot]), (uint32_t)(it / DS_TEACHERS) & 1u) && whole;
+            // (not before: until then the slot's warp may be reading those of its last row)
+            if (threadIdx.x == 0 && !g.lse_in) of_row[slot] = a;
             if (!whole) level = __int_as_float(0x7FFFFFFF);
             if (grad) {
                 const bool any = !whole || any_s[slot];
