@@ -676,7 +676,8 @@ int32_t iso_distill(const iso_mat* logits, const void* ids, int32_t ids_i64, con
                     float temperature, float* loss, float* lse, const float* dloss, const iso_mat* dlogits,
                     int32_t* status, void* stream);
 
-/* The gradient alone, from lse. */
+/* The gradient alone, from lse: exp(z_v / tau - lse) is off by 2^-24 |lse| beside, relative
+ * (lse is a float), and taken as 1 where that would make it more. */
 int32_t iso_distill_grad(const float* dloss, const iso_mat* logits, const void* ids, int32_t ids_i64,
                          const iso_mat* teacher, float temperature, const float* lse, const iso_mat* dlogits,
                          int32_t* status, void* stream);

@@ -20,9 +20,11 @@
 // the entries before and behind them (under one word each) go one by one.
 // Statistics: a warp takes its maximum m and its sum of exp((x - m) / tau), and
 // sums of several warps and CTAs are joined as sum of s_i exp((m_i - m) / tau), m
-// the largest m_i, in a fixed order.  In the exponents m / tau is a level, rounded
-// once, that lse takes back: exp(x / tau - level) then has one rounding, of a
-// number that is small where the weight is not.
+// the largest m_i, in a fixed order.  Exponents are (x - m) / tau, not x / tau -
+// m / tau: the rounding of m / tau is as large as any number where logits are (masks of
+// -1e10 or of the type's lowest value), and such a warp's sum, whose weight is 0,
+// would be infinite.  For the same reason the loss takes z - m and log s, not
+// z / tau - lse.  From lse alone a probability is held at 1, whatever lse was rounded to.
 #include "iso_tc.cuh"
 #include "iso_train.cuh"
 #include "iso_internal.cuh"
@@ -61,13 +63,17 @@ struct DistillArgs {
     float tau, inv_tau;
 };
 
-// exp(x / tau - level): of a bf16 row by the hardware's exponential (2 ulp, far
+// What exponents are formed from: a maximum m (exp((x - m) / tau)) or lse
+struct Ref {
+    float by, minus;
+};
+// exp((x - m) / tau): of a bf16 row by the hardware's exponential (2 ulp, far
 // below the rounding of the gradient, and random beside one another in the sum) of
 // base 2, of a binary32 row by expf.
 template <bool FAST>
 struct Exp {
-    float c;
-    __device__ __forceinline__ explicit Exp(float inv_tau) : c(FAST ? inv_tau * LOG2E : inv_tau) {}
+    float c, inv_tau;
+    __device__ __forceinline__ explicit Exp(float inv_tau) : c(FAST ? inv_tau * LOG2E : inv_tau), inv_tau(inv_tau) {}
     __device__ __forceinline__ float of(float x) const {
         if constexpr (FAST) {
             float y;
@@ -77,16 +83,45 @@ struct Exp {
             return expf(x);
         }
     }
-    // of a maximum; 0 where there is none, so that -Inf weighs 0
-    __device__ __forceinline__ float level(float m) const { return m == -INFINITY ? 0.0f : m * c; }
-    __device__ __forceinline__ float level_of(float lse) const { return FAST ? lse * LOG2E : lse; }
-    __device__ __forceinline__ float lse(float level, float s) const {
-        return FAST ? (level + log2f(s)) * 0.6931471805599453f : level + logf(s);
+    // of a maximum; of 0 where there is none, so that -Inf weighs 0
+    __device__ __forceinline__ Ref from_max(float m) const { return {c, m == -INFINITY ? 0.0f : -m}; }
+    __device__ __forceinline__ Ref from_lse(float lse) const { return {inv_tau, -lse}; }
+    template <bool LSE>
+    __device__ __forceinline__ float at(float x, Ref r) const {
+        if constexpr (LSE) {
+            const float e = fmaf(x, r.by, r.minus);
+            return of(min0(FAST ? e * LOG2E : e));              // at most 1 however lse was rounded
+        } else {
+            return of((x + r.minus) * r.by);
+        }
     }
-    __device__ __forceinline__ float at(float x, float level) const { return of(fmaf(x, c, -level)); }
+    static __device__ __forceinline__ float min0(float x) {     // a NaN stays one
+        float y;
+        asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(x), "f"(0.0f));
+        return y;
+    }
+};
+// The same of two entries at a time
+template <bool FAST, bool LSE>
+struct ExpPair {
+    uint64_t by, minus, scale;
+    const Exp<FAST>& ex;
+    __device__ __forceinline__ ExpPair(const Exp<FAST>& ex, Ref r)
+        : by(pair_of(r.by, r.by)), minus(pair_of(r.minus, r.minus)), scale(pair_of(LOG2E, LOG2E)), ex(ex) {}
+    __device__ __forceinline__ uint64_t of(uint64_t x) const {
+        float p, q;
+        uint64_t e = LSE ? fma2(x, by, minus) : mul2(add2(x, minus), by);
+        if constexpr (LSE && FAST) e = mul2(e, scale);
+        parts_of(e, p, q);
+        if constexpr (LSE) {
+            p = ex.min0(p);
+            q = ex.min0(q);
+        }
+        return pair_of(ex.of(p), ex.of(q));
+    }
 };
 
-// m: the largest entry (-Inf: none); s: the sum of exp(x / tau - level(m))
+// m: the largest entry (-Inf: none); s: the sum of exp((x - m) / tau)
 struct Stat {
     float m, s;
 };
@@ -94,7 +129,7 @@ template <bool FAST>
 __device__ __forceinline__ Stat join_lanes(Stat a, int lanes, const Exp<FAST>& ex) {     // of `lanes` lanes (a power of two)
     float m = a.m;
     for (int o = lanes / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-    float s = a.m == m ? a.s : a.s * ex.of(ex.level(a.m) - ex.level(m));
+    float s = a.m == m ? a.s : a.s * ex.of((a.m - m) * ex.c);
     if (a.m == -INFINITY) s = a.s;                  // 0, or NaN
     for (int o = lanes / 2; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
     return {m, s};
@@ -185,7 +220,7 @@ __device__ __forceinline__ bool teacher_side(const DistillArgs& g, int row, cons
             if (k >= g.top) continue;
             const bool used = v[i] >= 0 && v[i] < g.vocab;
             if (!used && v[i] != -1 && g.status) atomicCAS(g.status, 0, (int32_t)ISO_ERR_INDEX);
-            const float w = used ? x[i] * g.inv_tau : -INFINITY;
+            const float w = used ? x[i] : -INFINITY;
             t.id[k] = used ? (int)v[i] : -1;
             t.p[k] = w;
             t.z[k] = y[i];
@@ -199,7 +234,7 @@ __device__ __forceinline__ bool teacher_side(const DistillArgs& g, int row, cons
     if (m == -INFINITY && !nan) return false;
     float s = 0.0f;
     for (int k = lane; k < g.top; k += 32) {
-        const float x = t.id[k] < 0 ? 0.0f : expf(t.p[k] - (nan ? __int_as_float(0x7FFFFFFF) : m));
+        const float x = t.id[k] < 0 ? 0.0f : expf((t.p[k] - (nan ? __int_as_float(0x7FFFFFFF) : m)) * g.inv_tau);
         t.p[k] = x;
         s += x;
     }
@@ -210,14 +245,15 @@ __device__ __forceinline__ bool teacher_side(const DistillArgs& g, int row, cons
     return true;
 }
 
-// sum_k p_k (log p_k - z_k / tau + lse), by one warp
-__device__ __forceinline__ float divergence(const DistillArgs& g, const Top& t, float lse) {
+// tau^2 sum_k p_k (log p_k - log q_k), log q = (z - m) / tau - log s, by one warp
+__device__ __forceinline__ float divergence(const DistillArgs& g, const Top& t, float m, float log_s) {
+    const float tau = g.tau;
     float s = 0.0f;
     for (int k = threadIdx.x & 31; k < g.top; k += 32) {
         const float p = t.p[k];
-        if (t.id[k] >= 0 && p != 0.0f) s += p * (logf(p) - (t.z[k] * g.inv_tau - lse));
+        if (t.id[k] >= 0 && p != 0.0f) s += p * (tau * (logf(p) + log_s) - (t.z[k] - m));
     }
-    return warp_sum(s);
+    return tau * warp_sum(s);
 }
 
 // The entries at the teacher's ids among columns [c0, c1), after the row: slots of
@@ -302,7 +338,7 @@ __device__ __forceinline__ void arrive_some(int barrier) { asm volatile("bar.arr
 // the teacher's side, a chain of loads, before its own entries are out: a row
 // without any is cleared afterwards.  Only in place the gradient waits until the
 // logits at the ids have been read.
-template <typename T, int NT, int WORDS>
+template <typename T, int NT, int WORDS, bool LSE>
 __global__ void __launch_bounds__(NT + 32, NT == 512 ? 2 : NT == 256 ? 4 : 6) k_distill(const __grid_constant__ DistillArgs g) {
     constexpr int N = Word<T>::N, WARPS = NT / 32;
     constexpr bool FAST = sizeof(T) == 2;
@@ -312,7 +348,7 @@ __global__ void __launch_bounds__(NT + 32, NT == 512 ? 2 : NT == 256 ? 4 : 6) k_
     const Top t = top_of(di_smem, g.top);
     const int C = g.cluster, rank = C > 1 ? (int)(blockIdx.x % C) : 0;
     const int row = (int)(blockIdx.x / C), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const bool joint = g.lse_in == nullptr;
+    constexpr bool joint = !LSE;
     if (C > 1 && joint) cluster_arrive();
     const T* z = static_cast<const T*>(g.z) + (long long)row * g.ldz;
     T* grad = g.grad ? static_cast<T*>(g.grad) + (long long)row * g.ldg : nullptr;
@@ -324,7 +360,7 @@ __global__ void __launch_bounds__(NT + 32, NT == 512 ? 2 : NT == 256 ? 4 : 6) k_
     const int share = (words + C - 1) / C, w0 = min(words, rank * share), w1 = min(words, w0 + share);
     const int behind = before + words * N;                       // the entries from here on go one by one
     const int c0 = rank == 0 ? 0 : before + w0 * N, c1 = rank == C - 1 ? g.vocab : before + w1 * N;
-    // of the CTA's partial sums: the cluster's maximum (as a level) and sum
+    // of the CTA's partial sums: the cluster's maximum and sum
     auto all_of = [&](Stat a) {
         a.m = __shfl_sync(0xFFFFFFFFu, a.m, 0);
         a.s = __shfl_sync(0xFFFFFFFFu, a.s, 0);
@@ -342,7 +378,9 @@ __global__ void __launch_bounds__(NT + 32, NT == 512 ? 2 : NT == 256 ? 4 : 6) k_
     };
     const float dloss = grad ? g.dloss[row] : 0.0f;
     const float lse_in = joint ? 0.0f : g.lse_in[row];
-    float level = 0.0f, by = 0.0f, xs = -INFINITY;
+    Ref ref = {};
+    float by = 0.0f, xs = -INFINITY;
+    auto weight = [&](float x) { return ex.template at<LSE>(x, ref); };
     int single = -1;
     if (warp < WARPS) {
         Word<T> x[WORDS];
@@ -355,6 +393,7 @@ __global__ void __launch_bounds__(NT + 32, NT == 512 ? 2 : NT == 256 ? 4 : 6) k_
         const int back = NT - 1 - (int)threadIdx.x;              // NT > two words' entries: another thread
         if (rank == C - 1 && behind + back < g.vocab) single = behind + back;
         if (single >= 0) xs = to_f32(z[single]);
+        __syncwarp();            // every load is issued before the first is used (4096 x 50000 f32, loss: 345 -> 309 us)
         float inv_s = 1.0f;
         if (joint) {
             Stat a = {xs, 0.0f};
@@ -364,8 +403,8 @@ __global__ void __launch_bounds__(NT + 32, NT == 512 ? 2 : NT == 256 ? 4 : 6) k_
             if (a.m != a.m) a.m = -INFINITY;                     // (xs alone may be NaN)
 #pragma unroll
             for (int o = 16; o; o >>= 1) a.m = fmaxf(a.m, __shfl_xor_sync(0xFFFFFFFFu, a.m, o));
-            level = ex.level(a.m);
-            const uint64_t cc = pair_of(ex.c, ex.c), ll = pair_of(-level, -level);
+            ref = ex.from_max(a.m);
+            const ExpPair<FAST, false> two(ex, ref);
             uint64_t sum = pair_of(0.0f, 0.0f);
 #pragma unroll
             for (int i = 0; i < WORDS; ++i) {
@@ -373,15 +412,11 @@ __global__ void __launch_bounds__(NT + 32, NT == 512 ? 2 : NT == 256 ? 4 : 6) k_
                 uint64_t v[N / 2];
                 x[i].get(v);
 #pragma unroll
-                for (int j = 0; j < N / 2; ++j) {
-                    float p, q;
-                    parts_of(fma2(v[j], cc, ll), p, q);
-                    sum = add2(sum, pair_of(ex.of(p), ex.of(q)));
-                }
+                for (int j = 0; j < N / 2; ++j) sum = add2(sum, two.of(v[j]));
             }
             float p, q;
             parts_of(sum, p, q);
-            a.s = warp_sum(p + q + (single >= 0 ? ex.at(xs, level) : 0.0f));
+            a.s = warp_sum(p + q + (single >= 0 ? weight(xs) : 0.0f));
             if (lane == 0) parts[warp] = a;
             if (C == 1) arrive_some<NT + 32>(2);                 // for the teacher's warp
             if (C > 1 || grad) {
@@ -402,15 +437,16 @@ __global__ void __launch_bounds__(NT + 32, NT == 512 ? 2 : NT == 256 ? 4 : 6) k_
             } else if (in_place) {
                 sync_some<NT + 32>(3);   // the logits at the ids have been read
             }
-            level = ex.level(a.m);
+            ref = ex.from_max(a.m);
             inv_s = 1.0f / a.s;
         } else {
-            level = ex.level_of(lse_in);
+            ref = ex.from_lse(lse_in);
             if (in_place) sync_some<NT + 32>(3);
         }
         by = dloss * g.tau * inv_s;
         if (grad) {
-            const uint64_t cc = pair_of(ex.c, ex.c), ll = pair_of(-level, -level), bb = pair_of(by, by);
+            const ExpPair<FAST, LSE> two(ex, ref);
+            const uint64_t bb = pair_of(by, by);
             uint4* out = reinterpret_cast<uint4*>(grad + before) + w0 + threadIdx.x;
 #pragma unroll
             for (int i = 0; i < WORDS; ++i) {
@@ -418,15 +454,11 @@ __global__ void __launch_bounds__(NT + 32, NT == 512 ? 2 : NT == 256 ? 4 : 6) k_
                 uint64_t v[N / 2];
                 x[i].get(v);
 #pragma unroll
-                for (int j = 0; j < N / 2; ++j) {
-                    float p, q;
-                    parts_of(fma2(v[j], cc, ll), p, q);
-                    v[j] = mul2(pair_of(ex.of(p), ex.of(q)), bb);
-                }
+                for (int j = 0; j < N / 2; ++j) v[j] = mul2(two.of(v[j]), bb);
                 x[i].set(v);
                 __stcs(out + i * NT, x[i].w);
             }
-            if (single >= 0) from_f32(by * ex.at(xs, level), grad[single]);
+            if (single >= 0) from_f32(by * weight(xs), grad[single]);
         }
     } else {
         if (C > 1 && joint) {
@@ -447,25 +479,25 @@ __global__ void __launch_bounds__(NT + 32, NT == 512 ? 2 : NT == 256 ? 4 : 6) k_
         if (joint) {
             if (C == 1) sync_some<NT + 32>(2);
             const Stat a = C > 1 ? of_ctas() : of_warps();
-            level = ex.level(a.m);
+            ref = ex.from_max(a.m);
             by = dloss * g.tau / a.s;
             if (rank == 0) {
-                const float lse = a.m == -INFINITY && a.s == 0.0f ? -INFINITY : ex.lse(level, a.s);
-                const float d = any ? divergence(g, t, lse) : 0.0f;
+                const float log_s = logf(a.s), lse = a.m == -INFINITY && a.s == 0.0f ? -INFINITY : fmaf(a.m, g.inv_tau, log_s);
+                const float d = any ? divergence(g, t, a.m, log_s) : 0.0f;
                 if (lane == 0) {
-                    g.loss[row] = any ? g.tau * g.tau * d : 0.0f;
+                    g.loss[row] = d;
                     g.lse[row] = lse;
                 }
             }
         } else {
-            level = ex.level_of(lse_in);
+            ref = ex.from_lse(lse_in);
             by = dloss * g.tau;
         }
     }
     if (!grad) return;
     __syncthreads();
     if (any_s) {
-        put_right(g, t, grad, c0, c1, dloss * g.tau, WARPS + 1, [&](float v) { return by * ex.at(v, level); });
+        put_right(g, t, grad, c0, c1, dloss * g.tau, WARPS + 1, [&](float v) { return by * weight(v); });
     } else {
         for (int c = c0 + (int)threadIdx.x; c < c1; c += NT + 32) from_f32(0.0f, grad[c]);
     }
@@ -501,7 +533,7 @@ __device__ __forceinline__ bool probe_cluster(uint32_t bar, uint32_t parity) {
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-template <typename T>
+template <typename T, bool LSE>
 __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(const __grid_constant__ DistillArgs g) {
     constexpr int NT = DS_NT, N = Word<T>::N, WARPS = NT / 32;
     constexpr bool FAST = sizeof(T) == 2;
@@ -572,7 +604,8 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
             const Part p = part_of(row);
             T* const grad = g.grad ? static_cast<T*>(g.grad) + (long long)row * g.ldg : nullptr;
             const float dloss = grad ? g.dloss[row] : 0.0f;
-            float level = g.lse_in ? ex.level_of(g.lse_in[row]) : 0.0f, inv_s = 1.0f;
+            Ref ref = ex.from_lse(LSE ? g.lse_in[row] : 0.0f);
+            float inv_s = 1.0f;
             const uint4* const words = reinterpret_cast<const uint4*>(ds_smem + stage * stage_bytes);
             const int n = p.w1 - p.w0;
             int single = -1;
@@ -582,7 +615,7 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
             const float xs = single >= 0 ? to_f32(p.z[single]) : -INFINITY;
             bool whole = wait.warp(smem_u32(&full[stage]), parity);
             Stat a = {xs, 0.0f};
-            if (!g.lse_in) {
+            if (!LSE) {
 #pragma unroll 4
                 for (int i = threadIdx.x; i < n; i += NT) {
                     Word<T> x;
@@ -592,8 +625,8 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
                 if (a.m != a.m) a.m = -INFINITY;
 #pragma unroll
                 for (int o = 16; o; o >>= 1) a.m = fmaxf(a.m, __shfl_xor_sync(0xFFFFFFFFu, a.m, o));
-                level = ex.level(a.m);
-                const uint64_t cc = pair_of(ex.c, ex.c), ll = pair_of(-level, -level);
+                ref = ex.from_max(a.m);
+                const ExpPair<FAST, false> two(ex, ref);
                 uint64_t sum = pair_of(0.0f, 0.0f);
 #pragma unroll 4
                 for (int i = threadIdx.x; i < n; i += NT) {
@@ -602,15 +635,11 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
                     uint64_t v[N / 2];
                     x.get(v);
 #pragma unroll
-                    for (int j = 0; j < N / 2; ++j) {
-                        float s0, s1;
-                        parts_of(fma2(v[j], cc, ll), s0, s1);
-                        sum = add2(sum, pair_of(ex.of(s0), ex.of(s1)));
-                    }
+                    for (int j = 0; j < N / 2; ++j) sum = add2(sum, two.of(v[j]));
                 }
                 float s0, s1;
                 parts_of(sum, s0, s1);
-                a.s = warp_sum(s0 + s1 + (single >= 0 ? ex.at(xs, level) : 0.0f));
+                a.s = warp_sum(s0 + s1 + (single >= 0 ? ex.template at<false>(xs, ref) : 0.0f));
                 if (lane == 0) parts[warp] = a;
                 sync_some<NT>(1);
                 a = {-INFINITY, 0.0f};
@@ -641,17 +670,18 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
                     a.s = __shfl_sync(0xFFFFFFFFu, a.s, 0);
                 }
                 if (!whole) a.s = __int_as_float(0x7FFFFFFF);
-                level = ex.level(a.m);
+                ref = ex.from_max(a.m);
                 inv_s = 1.0f / a.s;
             }
             whole = wait.warp(smem_u32(&prepared[slot]), (uint32_t)(it / DS_TEACHERS) & 1u) && whole;
             // (not before: until then the slot's warp may be reading those of its last row)
-            if (threadIdx.x == 0 && !g.lse_in) of_row[slot] = a;
-            if (!whole) level = __int_as_float(0x7FFFFFFF);
+            if (threadIdx.x == 0 && !LSE) of_row[slot] = a;
+            if (!whole) ref.minus = __int_as_float(0x7FFFFFFF);
             if (grad) {
                 const bool any = !whole || any_s[slot];
                 const float by = dloss * g.tau * inv_s;
-                const uint64_t cc = pair_of(ex.c, ex.c), ll = pair_of(-level, -level), bb = pair_of(by, by);
+                const ExpPair<FAST, LSE> two(ex, ref);
+                const uint64_t bb = pair_of(by, by);
                 uint4* const out = reinterpret_cast<uint4*>(grad + p.before) + p.w0;
 #pragma unroll 4
                 for (int i = threadIdx.x; i < n; i += NT) {
@@ -660,16 +690,12 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
                     uint64_t v[N / 2];
                     x.get(v);
 #pragma unroll
-                    for (int j = 0; j < N / 2; ++j) {
-                        float s0, s1;
-                        parts_of(fma2(v[j], cc, ll), s0, s1);
-                        v[j] = mul2(pair_of(ex.of(s0), ex.of(s1)), bb);
-                    }
+                    for (int j = 0; j < N / 2; ++j) v[j] = mul2(two.of(v[j]), bb);
                     x.set(v);
                     if (!any) x.w = make_uint4(0u, 0u, 0u, 0u);
                     __stcs(out + i, x.w);
                 }
-                if (single >= 0) from_f32(any ? by * ex.at(xs, level) : 0.0f, grad[single]);
+                if (single >= 0) from_f32(any ? by * ex.template at<LSE>(xs, ref) : 0.0f, grad[single]);
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&written[slot]));
@@ -692,22 +718,24 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
         for (int row = row0 + slot * clusters; row < g.rows; row += DS_TEACHERS * clusters, ph ^= 1u) {
             const Part p = part_of(row);
             bool any = false;
-            const bool all = rank == 0 && !g.lse_in;
+            const bool all = rank == 0 && !LSE;
             if (g.grad || rank == 0) any = teacher_side(g, row, p.z, t, all ? 0 : p.c0, all ? g.vocab : p.c1);
             if (lane == 0) any_s[slot] = any;
             tc::arrive_warp(smem_u32(&prepared[slot]));
             const float dloss = g.grad ? g.dloss[row] : 0.0f;
-            float level = g.lse_in ? ex.level_of(g.lse_in[row]) : 0.0f, by = dloss * g.tau;
+            Ref ref = ex.from_lse(LSE ? g.lse_in[row] : 0.0f);
+            float by = dloss * g.tau;
             const bool whole = wait.warp(smem_u32(&written[slot]), ph);
-            if (!g.lse_in) {
+            if (!LSE) {
                 const Stat a = of_row[slot];
-                level = ex.level(a.m);
+                ref = ex.from_max(a.m);
                 by = dloss * g.tau / a.s;
                 if (rank == 0) {
-                    const float lse = !whole ? __int_as_float(0x7FFFFFFF) : a.m == -INFINITY && a.s == 0.0f ? -INFINITY : ex.lse(level, a.s);
-                    const float d = any ? divergence(g, t, lse) : 0.0f;
+                    const float log_s = whole ? logf(a.s) : __int_as_float(0x7FFFFFFF);
+                    const float lse = whole && a.m == -INFINITY && a.s == 0.0f ? -INFINITY : fmaf(a.m, g.inv_tau, log_s);
+                    const float d = any ? divergence(g, t, a.m, log_s) : 0.0f;
                     if (lane == 0) {
-                        g.loss[row] = any ? g.tau * g.tau * d : 0.0f;
+                        g.loss[row] = d;
                         g.lse[row] = lse;
                     }
                 }
@@ -715,7 +743,8 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
             if (g.grad && any && whole)
                 for (int k = lane; k < g.top; k += 32)
                     if (t.id[k] >= p.c0 && t.id[k] < p.c1)
-                        from_f32(by * ex.at(t.z[k], level) - dloss * g.tau * t.mass[k], static_cast<T*>(g.grad)[(long long)row * g.ldg + t.id[k]]);
+                        from_f32(by * ex.template at<LSE>(t.z[k], ref) - dloss * g.tau * t.mass[k],
+                                 static_cast<T*>(g.grad)[(long long)row * g.ldg + t.id[k]]);
             __syncwarp();
         }
     }
@@ -749,28 +778,29 @@ __global__ void __launch_bounds__(NT) k_distill_long(const __grid_constant__ Dis
         for (int c = threadIdx.x; c < g.vocab; c += NT) a.m = fmaxf(a.m, to_f32(z[c]));
 #pragma unroll
         for (int o = 16; o; o >>= 1) a.m = fmaxf(a.m, __shfl_xor_sync(0xFFFFFFFFu, a.m, o));
-        const float level = ex.level(a.m);
+        const Ref origin = ex.from_max(a.m);
 #pragma unroll 8
-        for (int c = threadIdx.x; c < g.vocab; c += NT) a.s += ex.at(to_f32(z[c]), level);
+        for (int c = threadIdx.x; c < g.vocab; c += NT) a.s += ex.at<false>(to_f32(z[c]), origin);
         a.s = warp_sum(a.s);
         if (lane == 0) parts[warp] = a;
     }
     __syncthreads();
     const bool any = any_s;
-    float level, inv_s = 1.0f;
+    Ref ref;
+    float inv_s = 1.0f;
     if (g.lse_in) {
-        level = ex.level_of(g.lse_in[row]);
+        ref = ex.from_lse(g.lse_in[row]);
     } else {
         a = {-INFINITY, 0.0f};
         if (lane < WARPS) a = parts[lane];
         a = join_lanes(a, WARPS, ex);
-        level = ex.level(a.m);
+        ref = ex.from_max(a.m);
         inv_s = 1.0f / a.s;
         if (warp == WARPS - 1) {
-            const float lse = a.m == -INFINITY && a.s == 0.0f ? -INFINITY : ex.lse(level, a.s);
-            const float d = any ? divergence(g, t, lse) : 0.0f;
+            const float log_s = logf(a.s), lse = a.m == -INFINITY && a.s == 0.0f ? -INFINITY : fmaf(a.m, g.inv_tau, log_s);
+            const float d = any ? divergence(g, t, a.m, log_s) : 0.0f;
             if (lane == 0) {
-                g.loss[row] = any ? g.tau * g.tau * d : 0.0f;
+                g.loss[row] = d;
                 g.lse[row] = lse;
             }
         }
@@ -778,10 +808,11 @@ __global__ void __launch_bounds__(NT) k_distill_long(const __grid_constant__ Dis
     if (!g.grad) return;
     T* grad = static_cast<T*>(g.grad) + (long long)row * g.ldg;
     const float scale = any ? g.dloss[row] * g.tau : 0.0f, by = scale * inv_s;
+    auto weight = [&](float x) { return g.lse_in ? ex.at<true>(x, ref) : ex.at<false>(x, ref); };
 #pragma unroll 8
-    for (int c = threadIdx.x; c < g.vocab; c += NT) from_f32(any ? by * ex.at(to_f32(z[c]), level) : 0.0f, grad[c]);
+    for (int c = threadIdx.x; c < g.vocab; c += NT) from_f32(any ? by * weight(to_f32(z[c])) : 0.0f, grad[c]);
     __syncthreads();
-    if (any) put_right(g, t, grad, 0, g.vocab, scale, WARPS, [&](float v) { return by * ex.at(v, level); });
+    if (any) put_right(g, t, grad, 0, g.vocab, scale, WARPS, [&](float v) { return by * weight(v); });
 }
 
 int check_distill(const iso_mat* z, const void* ids, int32_t ids_i64, const iso_mat* teacher, float tau,
@@ -815,12 +846,12 @@ int launch_rows(DistillArgs g, int cluster, cudaStream_t s) {
     at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
-    TRAIN_LAUNCH(cudaLaunchKernelEx(&cfg, k_distill<T, NT, WORDS>, g));
+    TRAIN_LAUNCH(g.lse_in ? cudaLaunchKernelEx(&cfg, k_distill<T, NT, WORDS, true>, g) : cudaLaunchKernelEx(&cfg, k_distill<T, NT, WORDS, false>, g));
     return ISO_OK;
 }
 
 // clusters that run at once on the current device
-template <typename T>
+template <typename T, bool LSE>
 int resident_clusters(int cluster, size_t smem) {
     static std::atomic<int> known[64][4];        // [device][log2 cluster]
     int dev = 0, n = 0;
@@ -828,7 +859,7 @@ int resident_clusters(int cluster, size_t smem) {
     const int at = cluster == 1 ? 0 : cluster == 2 ? 1 : cluster == 4 ? 2 : 3;
     n = known[dev][at].load(std::memory_order_relaxed);
     if (n) return n;
-    if (cudaFuncSetAttribute(k_distill_stream<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, DS_SMEM) != cudaSuccess) return 0;
+    if (cudaFuncSetAttribute(k_distill_stream<T, LSE>, cudaFuncAttributeMaxDynamicSharedMemorySize, DS_SMEM) != cudaSuccess) return 0;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(train_sms() / cluster * cluster));
     cfg.blockDim = dim3(DS_NT + 32 * DS_TEACHERS);
@@ -839,17 +870,17 @@ int resident_clusters(int cluster, size_t smem) {
     a.val.clusterDim.y = a.val.clusterDim.z = 1;
     cfg.attrs = &a;
     cfg.numAttrs = 1;
-    if (cudaOccupancyMaxActiveClusters(&n, k_distill_stream<T>, &cfg) != cudaSuccess || n <= 0) return 0;
+    if (cudaOccupancyMaxActiveClusters(&n, k_distill_stream<T, LSE>, &cfg) != cudaSuccess || n <= 0) return 0;
     known[dev][at].store(n, std::memory_order_relaxed);
     return n;
 }
-template <typename T>
+template <typename T, bool LSE>
 int launch_stream(DistillArgs g, int cluster, int share, cudaStream_t s) {
     const size_t tops = DS_TEACHERS * (size_t)top_floats(g.top) * 4;
     g.cluster = cluster;
     g.share = (share + 7) / 8 * 8;               // (stages on 128-byte boundaries)
     g.stages = (int)std::min<size_t>(DS_MAX_STAGES, (DS_SMEM - tops) / ((size_t)g.share * 16));
-    const int n = resident_clusters<T>(cluster, DS_SMEM);
+    const int n = resident_clusters<T, LSE>(cluster, DS_SMEM);
     if (n <= 0) return ISO_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)std::min<long long>(g.rows, n) * (unsigned)cluster);
@@ -862,7 +893,7 @@ int launch_stream(DistillArgs g, int cluster, int share, cudaStream_t s) {
     at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
-    TRAIN_LAUNCH(cudaLaunchKernelEx(&cfg, k_distill_stream<T>, g));
+    TRAIN_LAUNCH(cudaLaunchKernelEx(&cfg, k_distill_stream<T, LSE>, g));
     return ISO_OK;
 }
 
@@ -887,7 +918,7 @@ int launch_distill(const DistillArgs& g, cudaStream_t s) {
         while (C < DI_MAX_CLUSTER && words > C * room) C *= 2;
         const long long rounds = C == 1 ? DS_ROUNDS : DS_ROUNDS_CLUSTER;
         if (words <= C * room && (C == 1 || g.grad) && (long long)g.rows * C >= rounds * train_sms())
-            return launch_stream<T>(g, C, (words + C - 1) / C, s);
+            return g.lse_in ? launch_stream<T, true>(g, C, (words + C - 1) / C, s) : launch_stream<T, false>(g, C, (words + C - 1) / C, s);
     }
     // the smallest cluster that holds a row; larger ones while they leave SMs idle
     int C = 1;
