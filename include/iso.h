@@ -646,7 +646,8 @@ int32_t iso_attn_grad(const iso_mat* dout, const iso_mat* q, const iso_mat* k, c
 
 /* Diagnostics: the time after which a wait of the attention kernels gives up, for
  * the calls that follow (2 s; the time that another process has the GPU counts
- * little).  ns < 0 changes nothing.  Returns the limit before the call. */
+ * little; 0: a wait gives up unless it is over at its first look).  ns < 0 changes
+ * nothing.  Returns the limit before the call. */
 int64_t iso_attn_wait_ns(int64_t ns);
 
 /* ---- Training step: distillation from a teacher's top logits ---------------

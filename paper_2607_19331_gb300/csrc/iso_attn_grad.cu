@@ -614,11 +614,13 @@ __device__ __forceinline__ void grad_q(const GradMaps& maps, const GradArgs& a, 
             before_sync();
             arrive_warp(ds_ready + 8u * (i & 1));
         }
-        if (steps > 0) ok = ok && wait.warp(done, 0);
+        if (steps > 0 && ok) wait.warp(done, 0);
         after_sync();
-        // dQ: a row a thread, some columns of it each group
+        // dQ: a row a thread, some columns of it each group; both groups know whether one of
+        // them gave up, so that a row is whole or NaN
+        sa_sync();
         constexpr int WIDE = DP * 4 / GR_COMPUTE;
-        const bool nan = !ok || (steps > 0 && *gave_up), none = steps == 0;
+        const bool nan = *gave_up, none = steps == 0;
         const int from_col = group * WIDE;
         __nv_bfloat16* o = static_cast<__nv_bfloat16*>(g.dq) + ((long long)t.q0 + t.first + r) * g.lddq + (long long)h * g.head_dim + from_col;
         if (!write_row<__nv_bfloat16, WIDE>(dQ + at + from_col, o, r < rows, g.head_dim - from_col, a.vec, g.scale, nan, none))

@@ -199,10 +199,11 @@ __device__ __forceinline__ bool probe(uint32_t bar, uint32_t parity) {
     return ok != 0;
 }
 // Bounded waits of a CTA.  A wait that gives up sets the flag, and with it every
-// other wait of the CTA ends.
+// other wait of the CTA ends.  With a limit of 0 only what has happened by the first
+// probe counts.
 static __device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity, uint64_t limit_ns, volatile int* gave_up) {
     WaitClock clock;
-    for (int spin = 0; spin < MBAR_SPIN_LIMIT; ++spin) {
+    for (int spin = 0; limit_ns && spin < MBAR_SPIN_LIMIT; ++spin) {
         if (probe(bar, parity)) return true;
         if ((spin & 31) == 31 && ((gave_up && *gave_up) || clock.look(now_ns(), limit_ns))) break;
     }
