@@ -667,8 +667,8 @@ int64_t iso_attn_wait_ns(int64_t ns);
  * float per row.  Statistics and the gradient are binary32, the gradient rounded
  * once to dlogits' type (that of the logits).  dlogits may be the logits
  * themselves (same data and stride); else it overlaps no input.  status (device,
- * may be NULL): ISO_OK, ISO_ERR_INDEX or ISO_ERR_TIMEOUT (rows that a give-up left
- * unfinished are NaN). */
+ * may be NULL): ISO_OK, ISO_ERR_INDEX or ISO_ERR_TIMEOUT (every loss, lse and entry of
+ * the gradient is whole or, where a give-up left it unfinished, NaN). */
 #define ISO_DISTILL_MAX_TOP 2048
 
 /* loss and lse; with dlogits (then dloss is needed too, a float per row) also the gradient, the
@@ -682,6 +682,9 @@ int32_t iso_distill(const iso_mat* logits, const void* ids, int32_t ids_i64, con
 int32_t iso_distill_grad(const float* dloss, const iso_mat* logits, const void* ids, int32_t ids_i64,
                          const iso_mat* teacher, float temperature, const float* lse, const iso_mat* dlogits,
                          int32_t* status, void* stream);
+
+/* Diagnostics: as iso_attn_wait_ns, for the distillation kernels. */
+int64_t iso_distill_wait_ns(int64_t ns);
 
 /* Static description of a status code. */
 const char* iso_error_string(int32_t status);

@@ -147,6 +147,7 @@ PROTOTYPES = [
     ("iso_attn_grad_workspace_size", I32, [PM, PM, PC, ctypes.POINTER(SZ)]),
     ("iso_attn_grad", I32, [PM, PM, PM, PM, PM, P, PC, PM, PM, PM, P, SZ, P, P]),
     ("iso_attn_wait_ns", I64, [I64]),
+    ("iso_distill_wait_ns", I64, [I64]),
     ("iso_distill", I32, [PM, P, I32, PM, ctypes.c_float, P, P, P, PM, P, P]),
     ("iso_distill_grad", I32, [P, PM, P, I32, PM, ctypes.c_float, P, PM, P, P]),
     ("iso_error_string", ctypes.c_char_p, [I32]),

@@ -31,6 +31,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <climits>
 #include <cmath>
 
 namespace iso {
@@ -61,6 +62,7 @@ struct DistillArgs {
     int32_t ids_i64, teacher_f32, cluster;
     int32_t stages, share;               // k_distill_stream: rows in flight, words of a row a CTA has room for
     float tau, inv_tau;
+    uint64_t wait_ns;
 };
 
 // What exponents are formed from: a maximum m (exp((x - m) / tau)) or lse
@@ -542,11 +544,12 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
     __shared__ __align__(8) uint64_t full[DS_MAX_STAGES], exchanged[2], prepared[DS_TEACHERS], written[DS_TEACHERS];
     __shared__ volatile int any_s[DS_TEACHERS];
     __shared__ volatile int gave_up;
+    __shared__ int first_bad;                    // rows of this cluster from here on are not whole
     const int C = g.cluster, rank = (int)(blockIdx.x % C), clusters = (int)(gridDim.x / C), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const size_t stage_bytes = (size_t)g.share * 16;
     float* const tops = reinterpret_cast<float*>(ds_smem + g.stages * stage_bytes);
     const Exp<FAST> ex(g.inv_tau);
-    const tc::Waits wait = {2000000000u, &gave_up};
+    const tc::Waits wait = {g.wait_ns, &gave_up};
 
     // this CTA's part of a row, as in k_distill
     struct Part {
@@ -586,6 +589,7 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
             mbar_init(smem_u32(&written[i]), WARPS);
         }
         gave_up = 0;
+        first_bad = INT_MAX;
         mbar_fence_init();
     }
     __syncthreads();
@@ -604,16 +608,17 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
             const Part p = part_of(row);
             T* const grad = g.grad ? static_cast<T*>(g.grad) + (long long)row * g.ldg : nullptr;
             const float dloss = grad ? g.dloss[row] : 0.0f;
+            const bool stop = gave_up;           // after a give-up no row is whole: its stage may hold an earlier one
             Ref ref = ex.from_lse(LSE ? g.lse_in[row] : 0.0f);
             float inv_s = 1.0f;
             const uint4* const words = reinterpret_cast<const uint4*>(ds_smem + stage * stage_bytes);
-            const int n = p.w1 - p.w0;
             int single = -1;
             if (rank == 0 && (int)threadIdx.x < p.before) single = threadIdx.x;
             const int back = NT - 1 - (int)threadIdx.x;
             if (rank == C - 1 && p.behind + back < g.vocab) single = p.behind + back;
             const float xs = single >= 0 ? to_f32(p.z[single]) : -INFINITY;
             bool whole = wait.warp(smem_u32(&full[stage]), parity);
+            const int n = p.w1 - p.w0;
             Stat a = {xs, 0.0f};
             if (!LSE) {
 #pragma unroll 4
@@ -640,7 +645,8 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
                 float s0, s1;
                 parts_of(sum, s0, s1);
                 a.s = warp_sum(s0 + s1 + (single >= 0 ? ex.template at<false>(xs, ref) : 0.0f));
-                if (lane == 0) parts[warp] = a;
+                whole = __all_sync(0xFFFFFFFFu, whole && !stop);
+                if (lane == 0) parts[warp] = whole ? a : Stat{a.m, __int_as_float(0x7FFFFFFF)};
                 sync_some<NT>(1);
                 a = {-INFINITY, 0.0f};
                 if (lane < WARPS) a = parts[lane];
@@ -650,7 +656,8 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
                 if (C > 1) {
                     if (warp == 0) {
                         // this CTA's teacher's side has read the logits at its ids
-                        whole = wait.warp(smem_u32(&prepared[slot]), (uint32_t)(it / DS_TEACHERS) & 1u) && whole;
+                        whole = whole && wait.warp(smem_u32(&prepared[slot]), (uint32_t)(it / DS_TEACHERS) & 1u);
+                        if (!whole) a.m = a.s = __int_as_float(0x7FFFFFFF);      // for every CTA
                         if (lane < C) {
                             uint32_t to, at;
                             asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_u32(&of_cta[b][rank])), "r"(lane));
@@ -661,24 +668,27 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
                         __syncwarp();
                     }
                     const uint32_t ph = (uint32_t)(it >> 1) & 1u;
-                    if (!__all_sync(0xFFFFFFFFu, probe_cluster(smem_u32(&exchanged[b]), ph)))
-                        whole = wait.warp(smem_u32(&exchanged[b]), ph) && probe_cluster(smem_u32(&exchanged[b]), ph) && whole;
+                    if (whole && !__all_sync(0xFFFFFFFFu, probe_cluster(smem_u32(&exchanged[b]), ph)))
+                        whole = wait.warp(smem_u32(&exchanged[b]), ph) && __all_sync(0xFFFFFFFFu, probe_cluster(smem_u32(&exchanged[b]), ph));
                     a = {-INFINITY, 0.0f};
                     if (lane < C) a = of_cta[b][lane];
                     a = join_lanes(a, DI_MAX_CLUSTER, ex);
                     a.m = __shfl_sync(0xFFFFFFFFu, a.m, 0);
                     a.s = __shfl_sync(0xFFFFFFFFu, a.s, 0);
                 }
-                if (!whole) a.s = __int_as_float(0x7FFFFFFF);
                 ref = ex.from_max(a.m);
                 inv_s = 1.0f / a.s;
             }
-            whole = wait.warp(smem_u32(&prepared[slot]), (uint32_t)(it / DS_TEACHERS) & 1u) && whole;
+            if (LSE) whole = __all_sync(0xFFFFFFFFu, whole && !stop);
+            whole = whole && wait.warp(smem_u32(&prepared[slot]), (uint32_t)(it / DS_TEACHERS) & 1u);
+            if (!whole && lane == 0) {
+                gave_up = 1;
+                atomicMin(&first_bad, it);
+            }
             // (not before: until then the slot's warp may be reading those of its last row)
-            if (threadIdx.x == 0 && !LSE) of_row[slot] = a;
-            if (!whole) ref.minus = __int_as_float(0x7FFFFFFF);
-            if (grad) {
-                const bool any = !whole || any_s[slot];
+            if (threadIdx.x == 0 && !LSE && whole) of_row[slot] = a;
+            if (grad && whole) {                 // (in place, what is not whole may still be read as logits)
+                const bool any = any_s[slot];
                 const float by = dloss * g.tau * inv_s;
                 const ExpPair<FAST, LSE> two(ex, ref);
                 const uint64_t bb = pair_of(by, by);
@@ -714,8 +724,9 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
     } else {
         const int slot = warp - WARPS;
         const Top t = top_of(tops + slot * top_floats(g.top), g.top);
+        int it = slot;
         uint32_t ph = 0;
-        for (int row = row0 + slot * clusters; row < g.rows; row += DS_TEACHERS * clusters, ph ^= 1u) {
+        for (int row = row0 + slot * clusters; row < g.rows; row += DS_TEACHERS * clusters, it += DS_TEACHERS, ph ^= 1u) {
             const Part p = part_of(row);
             bool any = false;
             const bool all = rank == 0 && !LSE;
@@ -725,14 +736,16 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
             const float dloss = g.grad ? g.dloss[row] : 0.0f;
             Ref ref = ex.from_lse(LSE ? g.lse_in[row] : 0.0f);
             float by = dloss * g.tau;
-            const bool whole = wait.warp(smem_u32(&written[slot]), ph);
+            if (!wait.warp(smem_u32(&written[slot]), ph) || *static_cast<volatile int*>(&first_bad) <= it) {
+                if (lane == 0) atomicMin(&first_bad, it);
+                break;
+            }
             if (!LSE) {
                 const Stat a = of_row[slot];
                 ref = ex.from_max(a.m);
                 by = dloss * g.tau / a.s;
                 if (rank == 0) {
-                    const float log_s = whole ? logf(a.s) : __int_as_float(0x7FFFFFFF);
-                    const float lse = whole && a.m == -INFINITY && a.s == 0.0f ? -INFINITY : fmaf(a.m, g.inv_tau, log_s);
+                    const float log_s = logf(a.s), lse = a.m == -INFINITY && a.s == 0.0f ? -INFINITY : fmaf(a.m, g.inv_tau, log_s);
                     const float d = any ? divergence(g, t, a.m, log_s) : 0.0f;
                     if (lane == 0) {
                         g.loss[row] = d;
@@ -740,7 +753,7 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
                     }
                 }
             }
-            if (g.grad && any && whole)
+            if (g.grad && any)
                 for (int k = lane; k < g.top; k += 32)
                     if (t.id[k] >= p.c0 && t.id[k] < p.c1)
                         from_f32(by * ex.template at<LSE>(t.z[k], ref) - dloss * g.tau * t.mass[k],
@@ -750,6 +763,17 @@ __global__ void __launch_bounds__(DS_NT + 32 * DS_TEACHERS, 1) k_distill_stream(
     }
     __syncthreads();
     if (threadIdx.x == 0 && gave_up && g.status) atomicCAS(g.status, 0, (int32_t)ISO_ERR_TIMEOUT);
+    if (first_bad != INT_MAX) {
+        // what a give-up left unfinished, in this CTA's columns; where it came before a
+        // row's sums went out, the cluster's other CTAs have NaN from those
+        for (long long row = row0 + (long long)first_bad * clusters; row < g.rows; row += clusters) {
+            const Part p = part_of((int)row);
+            if (g.grad)
+                for (int c = p.c0 + (int)threadIdx.x; c < p.c1; c += NT + 32 * DS_TEACHERS)
+                    from_f32(__int_as_float(0x7FFFFFFF), static_cast<T*>(g.grad)[row * g.ldg + c]);
+            if (!LSE && rank == 0 && threadIdx.x == 0) g.loss[row] = g.lse[row] = __int_as_float(0x7FFFFFFF);
+        }
+    }
     if (C > 1) {
         cluster_arrive();
         cluster_wait();                          // the other CTAs' sums for this one have come
@@ -830,6 +854,9 @@ int check_distill(const iso_mat* z, const void* ids, int32_t ids_i64, const iso_
     }
     return ISO_OK;
 }
+constexpr uint64_t DISTILL_WAIT_NS = 2000000000;   // a wait gives up after this long, unless told otherwise
+std::atomic<uint64_t> g_distill_wait_ns{DISTILL_WAIT_NS};
+
 Bytes2D flat(const void* p, uint64_t bytes) { return {reinterpret_cast<uintptr_t>(p), 1, bytes, bytes}; }
 
 template <typename T, int NT, int WORDS>
@@ -946,6 +973,7 @@ int run_distill(DistillArgs& g, const iso_mat* z, const void* ids, int32_t ids_i
     g.teacher_f32 = teacher->dtype == ISO_F32;
     g.tau = tau;
     g.inv_tau = 1.0f / tau;
+    g.wait_ns = g_distill_wait_ns.load(std::memory_order_relaxed);
     return z->dtype == ISO_BF16 ? launch_distill<__nv_bfloat16>(g, s) : launch_distill<float>(g, s);
 }
 
@@ -955,6 +983,11 @@ int run_distill(DistillArgs& g, const iso_mat* z, const void* ids, int32_t ids_i
 using namespace iso;
 
 extern "C" {
+
+int64_t iso_distill_wait_ns(int64_t ns) {
+    return (int64_t)(ns < 0 ? g_distill_wait_ns.load(std::memory_order_relaxed)
+                            : g_distill_wait_ns.exchange((uint64_t)ns, std::memory_order_relaxed));
+}
 
 int32_t iso_distill(const iso_mat* logits, const void* ids, int32_t ids_i64, const iso_mat* teacher,
                     float temperature, float* loss, float* lse, const float* dloss, const iso_mat* dlogits,
