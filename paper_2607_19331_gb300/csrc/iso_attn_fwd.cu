@@ -333,7 +333,9 @@ k_tc_attn(const __grid_constant__ FwdMaps maps, const __grid_constant__ FwdArgs 
             finite = write_row<__nv_bfloat16, DP>(o_at, o, r < mine, g.head_dim, a.vec, inv, nan, none);
             if (r < mine) g.lse[(long long)h * g.q_rows + row] = lse;
         }
-        if (!finite) *again = 1;
+        // l counts the row's largest weight, 1 or more, times 2 to the rounding of m c: with
+        // scores of 1e9 and beyond that is any power, and what it leaves of l no sum
+        if (!finite || (r < mine && m > -INFINITY && !(l > 0.25f && l < 0x1p100f))) *again = 1;
         before_sync();
     }
     __syncthreads();
