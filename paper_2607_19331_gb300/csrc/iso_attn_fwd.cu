@@ -17,7 +17,8 @@
 // weights (960 of them exponentials, 512 at the least), the rest waits for two products
 // and for the other tile's; sixteen warps with half a row a thread spill (899 us).
 // Few queries over many keys: the key tiles are cut into parts for CTAs of their
-// own, whose outputs and log-sum-exps k_attn_join puts together.
+// own, whose outputs, maxima and sums k_attn_join puts together.  (Not their
+// log-sum-exps: those of large scores say nothing of the sums any more.)
 #include "iso_attn.cuh"
 #include "iso_attn_simt.cuh"
 #include "iso_attn_tc.cuh"
@@ -52,7 +53,7 @@ struct FwdArgs {
     float scale2;                // scale log2 e
     int32_t vec;                 // rows of out start on 16-byte boundaries
     int32_t parts;               // parts of the key tiles
-    float* part;                 // parts > 1: out as binary32, [part][q_rows][heads dim], then lse [part][heads][q_rows]
+    float* part;                 // parts > 1: out as binary32, [part][q_rows][heads dim], then maxima and sums [part][heads][q_rows] each
 };
 
 // The key tiles [begin, end) of 128 queries from `first` on, those of a part
@@ -82,10 +83,11 @@ __device__ __noinline__ void again_rows(const FwdArgs& a, float* smem) {
         int begin, end;
         key_tiles(a, t, t.first, min(ROWS, last - t.first), part, begin, end);
         for (const int stop = min(last, t.first + ROWS); t.first < stop; t.first += SA_B) {
-            if (a.parts > 1)
+            if (a.parts > 1) {
+                float* const maxima = a.part + (long long)a.parts * g.q_rows * width + (long long)part * g.heads * g.q_rows;
                 simt_attn<__nv_bfloat16, DP, float>(g, t, h, begin * ROWS, end * ROWS, a.part + (long long)part * g.q_rows * width, width,
-                                                    a.part + (long long)a.parts * g.q_rows * width + (long long)part * g.heads * g.q_rows, smem);
-            else
+                                                    maxima, smem, maxima + (long long)a.parts * g.heads * g.q_rows);
+            } else
                 simt_attn<__nv_bfloat16, DP, __nv_bfloat16>(g, t, h, begin * ROWS, end * ROWS, static_cast<__nv_bfloat16*>(const_cast<void*>(g.out)),
                                                             g.ldo, g.lse, smem);
             sa_sync();
@@ -327,7 +329,12 @@ k_tc_attn(const __grid_constant__ FwdMaps maps, const __grid_constant__ FwdArgs 
         if (a.parts > 1) {
             float* o = a.part + ((long long)part * g.q_rows + row) * width + (long long)h * g.head_dim;
             finite = write_row<float, DP>(o_at, o, r < mine, g.head_dim, true, inv, nan, none);
-            if (r < mine) a.part[(long long)a.parts * g.q_rows * width + ((long long)part * g.heads + h) * g.q_rows + row] = lse;
+            if (r < mine) {
+                float* const maxima = a.part + (long long)a.parts * g.q_rows * width + ((long long)part * g.heads + h) * g.q_rows + row;
+                maxima[0] = nan ? lse : m * g.scale;
+                // (without the rounding of m c, which is in every weight)
+                maxima[(long long)a.parts * g.heads * g.q_rows] = m == -INFINITY ? 0.0f : l * ex2(-fmaf(m, c, -__fmul_rn(m, c)));
+            }
         } else {
             __nv_bfloat16* o = static_cast<__nv_bfloat16*>(const_cast<void*>(g.out)) + row * g.ldo + (long long)h * g.head_dim;
             finite = write_row<__nv_bfloat16, DP>(o_at, o, r < mine, g.head_dim, a.vec, inv, nan, none);
@@ -347,8 +354,8 @@ k_tc_attn(const __grid_constant__ FwdMaps maps, const __grid_constant__ FwdArgs 
     if (*again && !*gave_up && warp < SA_TPB / 32) again_rows<DP>(a, reinterpret_cast<float*>(smem));
 }
 
-// The parts of a row of one head put together: lse = log sum e^lse_p, out = sum
-// e^(lse_p - lse) out_p.  Eight columns a thread.
+// The parts of a row of one head put together: with m the largest m_p, l = sum l_p
+// e^(m_p - m), lse = m + log l, out = sum l_p e^(m_p - m) out_p / l.  Eight columns a thread.
 template <bool VEC>
 __global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ FwdArgs a) {
     const AttnArgs& g = a.g;
@@ -360,17 +367,19 @@ __global__ void __launch_bounds__(256) k_attn_join(const __grid_constant__ FwdAr
         last = min(max(g.q_ends[g.n_seqs], 0), g.q_rows);
     }
     const long long n = (long long)max(last - first, 0) * g.heads * segs;
-    const float* lses = a.part + (long long)a.parts * g.q_rows * width;
+    const float* maxima = a.part + (long long)a.parts * g.q_rows * width;
+    const float* sums = maxima + (long long)a.parts * g.heads * g.q_rows;
     for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (long long)gridDim.x * blockDim.x) {
         const int s = (int)(i % segs), h = (int)(i / segs % g.heads);
         const long long row = first + i / segs / g.heads;
         float m = -INFINITY, sum = 0.0f, acc[8] = {};
 #pragma unroll 8
-        for (int p = 0; p < a.parts; ++p) m = fmaxf(m, lses[((long long)p * g.heads + h) * g.q_rows + row]);
+        for (int p = 0; p < a.parts; ++p) m = fmaxf(m, maxima[((long long)p * g.heads + h) * g.q_rows + row]);
         const float base = m == -INFINITY ? 0.0f : m;
 #pragma unroll 4
         for (int p = 0; p < a.parts; ++p) {
-            const float w = expf(lses[((long long)p * g.heads + h) * g.q_rows + row] - base);
+            const long long at = ((long long)p * g.heads + h) * g.q_rows + row;
+            const float w = sums[at] * expf(maxima[at] - base);
             sum += w;
             float x[8];                          // (of a part without a seen key: zeros, of weight 0)
             load8<true>(a.part + ((long long)p * g.q_rows + row) * width + (long long)h * g.head_dim, s * 8, g.head_dim, x);
@@ -405,7 +414,7 @@ AttnPlan attn_plan(long long q_rows, long long k_rows, const iso_attn_cfg& c) {
     AttnPlan p{1, 0};
     // CTAs for every SM, two key tiles or more in each
     p.parts = (int)std::max<long long>(1, std::min<long long>({train_sms() / std::max<long long>(1, items), tiles / 2, 64}));
-    if (p.parts > 1) p.bytes = (size_t)p.parts * q_rows * c.heads * (c.head_dim + 1) * 4;
+    if (p.parts > 1) p.bytes = (size_t)p.parts * q_rows * c.heads * (c.head_dim + 2) * 4;
     return p;
 }
 

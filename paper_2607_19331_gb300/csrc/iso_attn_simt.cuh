@@ -153,10 +153,11 @@ __device__ __forceinline__ float row_sum(float x) {
 }
 
 // out and lse of 64 queries (from t.first on) of head h over the keys [begin, end),
-// into rows of their own matrix and vector
+// into rows of their own matrix and vector; with `sums` a row's maximum and sum
+// instead of lse
 template <typename T, int DP, typename O>
 __device__ __noinline__ void simt_attn(const AttnArgs& g, const AttnTile& t, int h, int begin, int end, O* out, long long ldo,
-                                       float* lse, float* smem) {
+                                       float* lse, float* smem, float* sums = nullptr) {
     constexpr int TILE = SA_B * sa_pitch<DP>();
     float *const sq = smem, *const sk = sq + TILE, *const sv = sk + TILE, *const sp = sv + TILE;
     const int kh = h / g.group, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
@@ -218,7 +219,11 @@ __device__ __noinline__ void simt_attn(const AttnArgs& g, const AttnTile& t, int
     for (int i = 0; i < 4; ++i) {
         inv[i] = l[i] == 0.0f ? 0.0f : 1.0f / l[i];
         const int r = ty + 16 * i;
-        if (tx == 0 && r < rows) lse[(long long)h * g.q_rows + t.q0 + t.first + r] = m[i] + logf(l[i]);
+        if (tx == 0 && r < rows) {
+            const long long at = (long long)h * g.q_rows + t.q0 + t.first + r;
+            lse[at] = sums ? m[i] : m[i] + logf(l[i]);
+            if (sums) sums[at] = l[i];
+        }
     }
     sa_store<O, DP>(out, ldo, (long long)t.q0 + t.first, rows, h * g.head_dim, g.head_dim, ty, tx, acc, inv);
 }

@@ -31,7 +31,7 @@ def _cuda():
 
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("b", [-1.0, -3e6, -1e9, -1e10, 1e10, -7e15, 3e20, -1e30, 1e30])
-@pytest.mark.parametrize("n,m,heads,kv,D,every", [(300, 300, 4, 2, 64, 3), (130, 130, 2, 2, 40, 5)])
+@pytest.mark.parametrize("n,m,heads,kv,D,every", [(300, 300, 4, 2, 64, 3), (40, 700, 2, 1, 128, 1), (1, 9000, 4, 1, 128, 2), (130, 130, 2, 2, 40, 5)])
 def test_scores_of_any_size(n, m, heads, kv, D, every, b, dtype):
     g = torch.Generator(DEV).manual_seed(m)
     q, k = torch.zeros(n, heads * D, device=DEV, dtype=dtype), torch.zeros(m, kv * D, device=DEV, dtype=dtype)
