@@ -564,9 +564,9 @@ int32_t iso_embed_grad(const iso_mat* dY, const void* ids, int32_t ids_i64, int6
  *   (u, w) -> (u cos a - w sin a, u sin a + w cos a);
  * further channels are copied.  inverse = 1 turns by -a, which is the gradient
  * of the turn.  The angle is taken modulo a whole turn in 64-bit fixed point, so
- * it is as exact for far positions as for near ones (|error| <= 2^-30 +
- * |p| 2^-63 turns beside freq's own); products and sums are binary32, rounded
- * once.  positions holds axes rows of x->rows positions (int32, or int64 with
+ * it is as exact for far positions as for near ones (|error| <= 2^-26 + 2^-33 +
+ * |p| 2^-63 turns beside freq's own: the fraction as a binary32 number of half turns);
+ * products and sums are binary32, rounded once.  positions holds axes rows of x->rows positions (int32, or int64 with
  * positions_i64 = 1), ld_positions apart, any sign.  y has x's shape and dtype; it
  * is x itself (same data and stride) or shares no byte with it. */
 #define ISO_ROPE_MAX_PAIRS 128
@@ -637,7 +637,8 @@ int32_t iso_attn(const iso_mat* q, const iso_mat* k, const iso_mat* v, const iso
  * dk and dv summed over the query heads of their key head.  Shapes and dtype are
  * those of q, k and v.  Sums are binary32 in an order fixed by the sizes and
  * offsets, so equal inputs give equal bits; for BF16 P and dS are rounded to
- * bfloat16 before their products, and each gradient once.  Gradients overlap no
+ * bfloat16 before their products, and each gradient once.  lse being a float, P is off
+ * by 2^-24 |lse| beside, relative.  Gradients overlap no
  * input, nor each other; they may be column ranges of one buffer. */
 int32_t iso_attn_grad_workspace_size(const iso_mat* q, const iso_mat* k, const iso_attn_cfg* cfg, size_t* bytes);
 int32_t iso_attn_grad(const iso_mat* dout, const iso_mat* q, const iso_mat* k, const iso_mat* v, const iso_mat* out,
