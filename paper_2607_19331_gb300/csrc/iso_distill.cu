@@ -340,6 +340,10 @@ __device__ __forceinline__ void arrive_some(int barrier) { asm volatile("bar.arr
 // the teacher's side, a chain of loads, before its own entries are out: a row
 // without any is cleared afterwards.  Only in place the gradient waits until the
 // logits at the ids have been read.
+// 128 threads for short rows (4096 x 4000 bf16 with its gradient: 18 us, 256 threads 28;
+// 4096 x 2000 f32: 20, 29), five words a thread where they hold the row (2000 x 8000 bf16:
+// 16.4 us, ten 18.2), larger clusters while rows leave SMs idle (8 x 32000 f32: 4.8 us, one
+// no larger than needed 5.5).
 template <typename T, int NT, int WORDS, bool LSE>
 __global__ void __launch_bounds__(NT + 32, NT == 512 ? 2 : NT == 256 ? 4 : 6) k_distill(const __grid_constant__ DistillArgs g) {
     constexpr int N = Word<T>::N, WARPS = NT / 32;
@@ -511,21 +515,21 @@ __global__ void __launch_bounds__(NT + 32, NT == 512 ? 2 : NT == 256 ? 4 : 6) k_
 // launch.  A row: its words summed up, the cluster's exchange of sums, its words again for
 // the gradient.  Four warps take the teacher's side of every fourth row each, a
 // chain of loads that is as long as two rows.  Bound by HBM where a row fits one
-// CTA, and for the gradient alone (6.5 TB/s); with larger clusters by the exchange, whose
+// CTA, and for the gradient alone (6.3 TB/s); with larger clusters by the exchange, whose
 // latency no other row of the cluster covers.
 // Measured against k_distill, loss with gradient / loss / gradient alone, us:
-//   4096 x 152064 bf16 (clusters of 4)   521 / 360 / 378   against 566 / 317 / 437
-//   4096 x 76032 bf16 (2)                254 / 175 / 198   against 287 / 159 / 227
-//   4096 x 50000 f32 (2)                 316 / 198 / 267   against 494 / 312 / 342
-//   4096 x 50000 bf16 (1)                136 /  78 / 141   against 236 / 150 / 173
-//   8192 x 32000 bf16 (1)                179 / 117 / 182   against 273 / 162 / 241
-//   8192 x 20000 bf16 (1)                145 / 102 / 129   against 143 /  75 / 145
-//   8192 x 12000 bf16 (1)                117 /  90 /  99   against 110 /  63 / 108
-//   1024 x 50000 bf16 (1)                 42 /  25 /  41   against  59 /  41 /  46
-//   600 x 152064 bf16 (4)                 88 /  62 /  67   against  83 /  52 /  64
-//   1024 x 76032 f32 (4)                 148 / 100 / 109   against 136 /  91 / 105
+//   4096 x 152064 bf16 (clusters of 4)   527 / 360 / 395   against 524 / 313 / 378
+//   4096 x 76032 bf16 (2)                256 / 175 / 205   against 265 / 156 / 191
+//   4096 x 50000 f32 (2)                 321 / 203 / 267   against 444 / 309 / 294
+//   4096 x 50000 bf16 (1)                130 /  79 / 139   against 219 / 144 / 151
+//   8192 x 32000 bf16 (1)                187 / 120 / 176   against 253 / 150 / 197
+//   8192 x 20000 bf16 (1)                161 / 103 / 108   against 132 /  65 / 125
+//   8192 x 12000 bf16 (1)                145 /  89 /  81   against  98 /  55 /  79
+//   1024 x 50000 bf16 (1)                 42 /  25 /  41   against  58 /  41 /  41
+//   600 x 152064 bf16 (4)                 88 /  61 /  69   against  80 /  52 /  58
+//   1024 x 76032 f32 (4)                 150 / 104 / 109   against 135 /  90 /  94
 // so it takes rows of DS_MIN_WORDS that fit one CTA, DS_ROUNDS rows for each, and rows of
-// larger clusters for a gradient, DS_ROUNDS_CLUSTER for each.  (The words kept in
+// larger clusters for a gradient, DS_ROUNDS_CLUSTER for each (clusters of 8 for the first case: 913).  (The words kept in
 // registers from the first pass on, with 20 a thread: 589 us for the first case.)
 constexpr int DS_NT = 256, DS_TEACHERS = 4, DS_MAX_STAGES = 4, DS_SMEM = 220 * 1024;
 constexpr int DS_MIN_WORDS = 3000, DS_ROUNDS = 4, DS_ROUNDS_CLUSTER = 32;

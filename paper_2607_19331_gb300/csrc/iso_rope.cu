@@ -20,8 +20,9 @@
 namespace iso {
 namespace {
 
-constexpr int ROPE_TPB = 64;            // 256: 108 us for the two passes over 16384 x 4096 bf16, 128: 102, 64: 96
-// units in flight a thread: 64 bytes of loads (twice that: 99 us)
+// 64: 91 us there and back over 16384 x 4096 bf16, 128: 100, 256: 109 (binary32: 168, 164, 161)
+constexpr int ROPE_TPB = 64;
+// units in flight a thread: 64 bytes of loads (twice that: 107 us)
 template <typename T>
 constexpr int rope_each(int u) { return u == 1 ? 4 : 16 / (u * (int)sizeof(T) / 2); }
 constexpr int ROPE_MAX_ROWS = 16;

@@ -25,7 +25,7 @@ def _stated(p):
 
 @pytest.mark.parametrize("inverse", [False, True])
 def test_angles_are_as_near_as_stated(inverse):
-    n, rows = 64, 400
+    n, rows = 64, 120
     g = torch.Generator().manual_seed(11)
     # fractions of a turn 0.4999 .. 0.5001 at position 1; further odd positions stay near half a turn for those next to it
     freq = [2 * math.pi * (0.5 + (float(x) - 0.5) * 10 ** -(4 + i % 6)) for i, x in enumerate(torch.rand(n, generator=g))]
